@@ -292,6 +292,139 @@ ta_status blocksparse_attn_fwd(const void *q, const void *k, const void *v,
                                size_t workspace_bytes, void *stream);
 
 /*
+ * Prefill attention with modified scores.  For a kept pair of row i and key j
+ * (positions in the sequence) the score
+ *   x = softmax_scale <q_i, k_j>
+ * becomes softcap * tanh(x / softcap) where softcap > 0, and then
+ * x - slopes[h] * (i - j) where slopes is not NULL; o and lse are those of the
+ * softmax over the modified scores.  At least one of the two must be given.
+ *   sched_dev, info  a schedule of any kind; which pairs are kept, the
+ *                layouts and the workspace (ta_workspace_bytes) are those of
+ *                that kind's forward function.
+ *   softcap      0 (none) to 1024; a score's absolute error is at most
+ *                2^-22 softcap beside that of the product.
+ *   slopes       [hq] fp32 device array of finite values, or NULL.  The last
+ *                keys weigh most where a slope is positive.
+ * A key that a row does not keep adds nothing to it, whatever its value
+ * (infinities and NaN included).  Errors as triangle_attn_fwd.
+ */
+ta_status scored_attn_fwd(const void *q, const void *k, const void *v, void *o,
+                          int32_t o_dtype, float *lse, const int32_t *sched_dev,
+                          const ta_schedule_info *info, int64_t total_tokens,
+                          int32_t hq, int32_t hkv, int32_t head_dim,
+                          float softmax_scale, float softcap,
+                          const float *slopes, void *workspace,
+                          size_t workspace_bytes, void *stream);
+
+/*
+ * The paged K/V cache: what follows the prefill.
+ *   k_cache and v_cache are [num_pages, hkv, page_size, head_dim] bf16,
+ *   contiguous, page_size in {16, 32, 64, 128, 256}.  Slot s is place
+ *   s % page_size of page s / page_size.  Position p of request b is place
+ *   p % page_size of page block_table[b * table_width + p / page_size].
+ *   A call takes at most TA_MAX_BATCH requests.
+ */
+#define TA_MAX_BATCH 1024
+
+/* Status bits of ta_page_map (state[1]); 0: done. */
+#define TA_MAP_NO_PAGES 1     /* fewer free pages than the step needs */
+#define TA_MAP_TABLE_WIDTH 2  /* a request outgrows its table row */
+#define TA_MAP_BAD_LENGTH 4   /* a negative length */
+#define TA_MAP_SLOT_COUNT 8   /* more new tokens than slots */
+#define TA_MAP_BAD_FREE 16    /* n_free outside 0 .. free_capacity */
+
+/*
+ * Pages and slots of one step, from request lengths alone, on the device
+ * (a captured call follows the lengths).  Request b holds cached_lens[b]
+ * tokens and gets new_lens[b] more.  The pages it then lacks are taken from
+ * the end of the free list, request by request: the r-th of the call is
+ * free_pages[n_free - 1 - r].
+ *   cached_lens, new_lens  [batch] int32.
+ *   block_table  [batch, table_width] int32, in and out: the entries of the
+ *                new pages are written, all others left as they are.
+ *   free_pages   [free_capacity] int32, read only; n_free [1] int32: how many
+ *                of its first entries are free pages.
+ *   kv_lens      [batch] out: cached + new.
+ *   cu_new       [batch + 1] out: where each request's new tokens begin.
+ *   slots        [slot_count] out: the slot of each new token, request by
+ *                request; -1 from the last one on (and for a token whose
+ *                table entry holds no page).
+ *   state        [2] out: the number of free pages left, and status bits.
+ * All or nothing: where a status bit is set, no page is taken, kv_lens is
+ * cached_lens, cu_new is 0 and every slot -1.  Outputs must not overlap
+ * inputs or one another (the next step's n_free may be this one's state, with
+ * another state for its output).
+ */
+ta_status ta_page_map(const int32_t *cached_lens, const int32_t *new_lens,
+                      int32_t batch, int32_t page_size, int32_t *block_table,
+                      int32_t table_width, const int32_t *free_pages,
+                      int32_t free_capacity, const int32_t *n_free,
+                      int32_t *kv_lens, int32_t *cu_new, int32_t *slots,
+                      int64_t slot_count, int32_t *state, void *stream);
+
+/*
+ * Rows of new tokens into their slots of the cache.
+ *   k, v         bf16 [total_tokens, hkv, head_dim] with the given strides in
+ *                elements (multiples of 8; the last dimension contiguous), as
+ *                views of a fused projection have; 16-byte aligned.
+ *   slots        [total_tokens] int32; rows whose slot is negative or past
+ *                the cache are skipped.  Slots of one call are distinct (what
+ *                a slot named twice then holds is not specified).
+ */
+ta_status kv_cache_write(const void *k, const void *v, int64_t k_token_stride,
+                         int64_t k_head_stride, int64_t v_token_stride,
+                         int64_t v_head_stride, const int32_t *slots,
+                         int64_t total_tokens, void *k_cache, void *v_cache,
+                         int64_t num_pages, int32_t hkv, int32_t page_size,
+                         int32_t head_dim, void *stream);
+
+/*
+ * Attention over the paged cache: single tokens, drafted tokens, or pieces of
+ * prompts, optionally behind a prefix that the whole batch shares.
+ *   q, o, lse    as for the forward passes: [total_tokens, hq, head_dim], the
+ *                requests' query rows one after another; lse [hq,
+ *                total_tokens] or NULL.
+ *   kv_lens      [batch] int32 device array: keys of request b in its own
+ *                pages, this call's tokens among them (they are written
+ *                first).  0 or less: none.
+ *   cu_q         [batch + 1] int32 device array: rows cu_q[b] .. cu_q[b + 1)
+ *                are request b's last tokens; NULL: one row a request
+ *                (total_tokens = batch).  Rows from cu_q[batch] on are left
+ *                as they are.
+ *   prefix_pages pages of the shared prefix's prefix_len keys (0: none),
+ *                which come before every request's own ones; any length.
+ * Row t of request b has position p = kv_lens[b] - (cu_q[b + 1] - cu_q[b]) + t
+ * among its own keys and keeps the whole prefix and the own keys up to p; a
+ * row whose p is negative keeps nothing (o = 0, lse = -inf).  Scores, softcap
+ * and slopes as for scored_attn_fwd, both optional here, positions counted
+ * from the start of the prefix.  Values behind a row's last key, in the pages
+ * or past them, are never used, whatever they are.
+ *   workspace    at least ta_paged_workspace_bytes() bytes, 16-byte aligned,
+ *                ragged = cu_q is given, prefix = prefix_len > 0; its contents
+ *                on entry do not matter.  Calls that may overlap (other
+ *                streams) need workspaces of their own.
+ * Device data that cannot be followed shows as NaN: a page id outside the
+ * cache in the rows that need it, a length past the block table in its
+ * request's rows, cu_q that is not 0 <= ... <= total_tokens from 0 on in every
+ * row.  No access leaves the caller's buffers.  Unsupported: more than 2048
+ * row tiles, total_tokens * (hq / hkv) / 128 + batch with long query lengths.
+ */
+size_t ta_paged_workspace_bytes(int32_t batch, int64_t total_tokens,
+                                int32_t ragged, int32_t prefix, int32_t hq,
+                                int32_t hkv, int32_t head_dim);
+ta_status paged_attn_fwd(const void *q, const void *k_cache,
+                         const void *v_cache, void *o, int32_t o_dtype,
+                         float *lse, const int32_t *kv_lens,
+                         const int32_t *cu_q, const int32_t *block_table,
+                         int32_t batch, int32_t table_width,
+                         const int32_t *prefix_pages, int32_t prefix_len,
+                         int64_t total_tokens, int32_t hq, int32_t hkv,
+                         int32_t head_dim, int64_t num_pages, int32_t page_size,
+                         float softmax_scale, float softcap,
+                         const float *slopes, void *workspace,
+                         size_t workspace_bytes, void *stream);
+
+/*
  * Region-contribution probe (Sec. 2.2, Grad(M-hat, l); the sections of
  * Appendix A.3).  A probing variable theta scales the attention
  * probabilities elementwise (A_theta = theta (.) A, O = A_theta V); for an

@@ -122,6 +122,20 @@ def lib():
     L.region_grad_sums.argtypes = [vp, vp, vp, vp, vp, pinfo, i64, i32, i32, i32,
                                    ctypes.c_float, i32, i32, i32, vp, vp,
                                    ctypes.c_size_t, vp]
+    L.scored_attn_fwd.restype = ctypes.c_int
+    L.scored_attn_fwd.argtypes = [vp, vp, vp, vp, i32, vp, vp, pinfo, i64, i32, i32, i32,
+                                  ctypes.c_float, ctypes.c_float, vp, vp, ctypes.c_size_t, vp]
+    L.ta_page_map.restype = ctypes.c_int
+    L.ta_page_map.argtypes = [vp, vp, i32, i32, vp, i32, vp, i32, vp, vp, vp, vp, i64, vp, vp]
+    L.kv_cache_write.restype = ctypes.c_int
+    L.kv_cache_write.argtypes = [vp, vp, i64, i64, i64, i64, vp, i64, vp, vp, i64, i32, i32, i32,
+                                 vp]
+    L.ta_paged_workspace_bytes.restype = ctypes.c_size_t
+    L.ta_paged_workspace_bytes.argtypes = [i32, i64, i32, i32, i32, i32, i32]
+    L.paged_attn_fwd.restype = ctypes.c_int
+    L.paged_attn_fwd.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, vp, i32, i32, vp, i32, i64, i32,
+                                 i32, i32, i64, i32, ctypes.c_float, ctypes.c_float, vp, vp,
+                                 ctypes.c_size_t, vp]
     L.ta_region_counts.restype = ctypes.c_int
     L.ta_region_counts.argtypes = [vp, i32, i32, i32, i32, vp]
     L.ta_region_grad_mean.restype = ctypes.c_int
@@ -370,6 +384,234 @@ def causal_attn_fwd(q, k, v, o, lse, sched_dev, info, softmax_scale,
         float(softmax_scale), _stream(stream)))
 
 
+class _OnDevice:
+    """Makes a tensor's GPU current for a call, and checks that the stream it
+    is enqueued on (the GPU's current one if None) belongs to that GPU."""
+
+    def __init__(self, device, stream):
+        import torch
+        self.guard = torch.cuda.device(device)
+        if stream is None:
+            stream = torch.cuda.current_stream(device)
+        elif stream.device != device:
+            raise ValueError(f"stream is on {stream.device}, operands on {device}")
+        self.stream = ctypes.c_void_p(stream.cuda_stream)
+
+    def __enter__(self):
+        self.guard.__enter__()
+        return self.stream
+
+    def __exit__(self, *exc):
+        return self.guard.__exit__(*exc)
+
+
+def _check_operands(named, dev):
+    """named: (name, tensor, dtype, shape); a None in a shape leaves that
+    length open, a None in place of the shape leaves it all open."""
+    import torch
+    for name, t, dtype, shape in named:
+        if not isinstance(t, torch.Tensor):
+            raise ValueError(f"{name} must be a torch tensor")
+        if t.dtype != dtype:
+            raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+        if shape is not None and (t.dim() != len(shape) or any(
+                b is not None and a != b for a, b in zip(t.shape, shape))):
+            raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        if t.device != dev:
+            raise ValueError(f"{name} is on {t.device}, not on {dev}: all operands must be on "
+                             "one device")
+    if dev.type != "cuda":
+        raise ValueError(f"operands must be on a GPU, got {dev}")
+
+
+def _nbytes(t):
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def scored_attn_fwd(q, k, v, o, lse, sched_dev, info, softmax_scale, softcap, slopes, workspace,
+                    stream=None):
+    """Enqueue prefill attention with modified scores over a schedule of any
+    kind: softcap * tanh(x / softcap) where softcap is given, minus slopes[h]
+    times the distance from key to row where slopes (float32 [Hq]) are.  Other
+    arguments as triangle_attn_fwd."""
+    _check_tensors(q, k, v, o, lse, sched_dev, info, workspace)
+    total, hq, d = q.shape
+    if slopes is not None:
+        import torch
+        _check_operands([("slopes", slopes, torch.float32, (hq,))], q.device)
+    cap = 0.0 if softcap is None else float(softcap)
+    with _OnDevice(q.device, stream) as s:
+        _check(lib().scored_attn_fwd(
+            _ptr(q), _ptr(k), _ptr(v), _ptr(o), _out_dtype(o), _ptr(lse), _ptr(sched_dev),
+            ctypes.byref(info), total, hq, k.shape[1], d, float(softmax_scale), cap,
+            _ptr(slopes), _ptr(workspace), _nbytes(workspace), s))
+
+
+# status bits of page_map (state[1])
+MAP_NO_PAGES = 1
+MAP_TABLE_WIDTH = 2
+MAP_BAD_LENGTH = 4
+MAP_SLOT_COUNT = 8
+MAP_BAD_FREE = 16
+
+
+def page_map(cached_lens, new_lens, block_table, free_pages, n_free, page_size, kv_lens, cu_new,
+             slots, state, stream=None):
+    """Enqueue the pages and slots of one step, all int32 cuda tensors.
+
+    cached_lens, new_lens [B]: tokens that the requests hold and get;
+    block_table [B, W]: gets the pages taken; free_pages [F] with its first
+    n_free [1] entries free, taken from the end.  Outputs: kv_lens [B], cu_new
+    [B + 1], slots [any length >= the new tokens; -1 behind the last] and
+    state [2]: free pages left, and MAP_* status bits (0: done; otherwise
+    nothing was taken and every slot is -1).  Nothing is read back to the host.
+    """
+    import torch
+    i32 = torch.int32
+    if not isinstance(cached_lens, torch.Tensor) or cached_lens.dim() != 1:
+        raise ValueError("cached_lens must be a tensor [requests]")
+    b, dev = cached_lens.shape[0], cached_lens.device
+    _check_operands([("cached_lens", cached_lens, i32, (b,)), ("new_lens", new_lens, i32, (b,)),
+                     ("block_table", block_table, i32, (b, None)),
+                     ("free_pages", free_pages, i32, (None,)), ("n_free", n_free, i32, (1,)),
+                     ("kv_lens", kv_lens, i32, (b,)), ("cu_new", cu_new, i32, (b + 1,)),
+                     ("slots", slots, i32, (None,)), ("state", state, i32, (2,))], dev)
+    with _OnDevice(dev, stream) as s:
+        _check(lib().ta_page_map(
+            _ptr(cached_lens), _ptr(new_lens), b, int(page_size), _ptr(block_table),
+            block_table.shape[1], _ptr(free_pages), free_pages.shape[0], _ptr(n_free),
+            _ptr(kv_lens), _ptr(cu_new), _ptr(slots), slots.shape[0], _ptr(state), s))
+
+
+def _cache_shape(k_cache):
+    import torch
+    if not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
+        raise ValueError("k_cache must be a tensor [pages, heads, page_size, head_dim]")
+    return tuple(k_cache.shape)
+
+
+def kv_cache_write(k, v, slots, k_cache, v_cache, stream=None):
+    """Enqueue the write of k, v [T, Hkv, d] bf16 (views with any token and
+    head stride that is a multiple of 8) into the slots [T] int32 of the caches
+    [pages, Hkv, page_size, d] bf16.  Rows with a negative slot are skipped;
+    the slots of one call are distinct."""
+    import torch
+    for name, t in (("k", k), ("v", v)):
+        if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16:
+            raise ValueError(f"{name} must be a bfloat16 tensor")
+        if t.dim() != 3:
+            raise ValueError(f"{name} must be [tokens, heads, head_dim], got {tuple(t.shape)}")
+        if t.shape[2] > 1 and t.stride(2) != 1:
+            raise ValueError(f"the last dimension of {name} must be contiguous")
+    if k.shape != v.shape:
+        raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} differ")
+    total, hkv, d = k.shape
+    dev = k.device
+    if v.device != dev:
+        raise ValueError(f"v is on {v.device}, k on {dev}")
+    shape = _cache_shape(k_cache)
+    pages, ch, page_size, cd = shape
+    if (ch, cd) != (hkv, d):
+        raise ValueError(f"the caches have {ch} heads of {cd}, k has {hkv} of {d}")
+    _check_operands([("k_cache", k_cache, torch.bfloat16, shape),
+                     ("v_cache", v_cache, torch.bfloat16, shape),
+                     ("slots", slots, torch.int32, (total,))], dev)
+    with _OnDevice(dev, stream) as s:
+        _check(lib().kv_cache_write(
+            _ptr(k), _ptr(v), k.stride(0), k.stride(1), v.stride(0), v.stride(1), _ptr(slots),
+            total, _ptr(k_cache), _ptr(v_cache), pages, hkv, page_size, d, s))
+
+
+def ta_paged_workspace_bytes(batch, total_tokens, ragged, prefix, hq, hkv, head_dim) -> int:
+    return int(lib().ta_paged_workspace_bytes(batch, total_tokens, int(ragged), int(prefix), hq,
+                                              hkv, head_dim))
+
+
+def paged_attn_fwd(q, k_cache, v_cache, o, lse, kv_lens, cu_q, block_table, prefix_pages,
+                   prefix_len, softmax_scale, softcap, slopes, workspace, stream=None):
+    """Enqueue attention of q [T, Hq, d] over the caches [pages, Hkv,
+    page_size, d], all bf16 (o bf16 or fp32).
+
+    kv_lens [B] int32: own keys of each request, this call's tokens among
+    them; cu_q [B + 1] int32 or None (one row a request); block_table [B, W]
+    int32; prefix_pages [>= ceil(prefix_len / page_size)] int32 and prefix_len:
+    keys that come before every request's own (None and 0: none); lse [Hq, T]
+    fp32 or None; softcap and slopes as scored_attn_fwd, or None; workspace
+    uint8 of >= ta_paged_workspace_bytes bytes.
+    """
+    import torch
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must be a tensor [tokens, heads, head_dim]")
+    total, hq, d = q.shape
+    dev = q.device
+    if not isinstance(o, torch.Tensor):
+        raise ValueError("o must be a torch tensor")
+    out = _out_dtype(o)
+    shape = _cache_shape(k_cache)
+    pages, hkv, page_size, cd = shape
+    if cd != d:
+        raise ValueError(f"the caches have head_dim {cd}, q {d}")
+    if not isinstance(kv_lens, torch.Tensor) or kv_lens.dim() != 1:
+        raise ValueError("kv_lens must be a tensor [requests]")
+    b = kv_lens.shape[0]
+    i32 = torch.int32
+    named = [("q", q, torch.bfloat16, None), ("k_cache", k_cache, torch.bfloat16, shape),
+             ("v_cache", v_cache, torch.bfloat16, shape), ("o", o, o.dtype, (total, hq, d)),
+             ("kv_lens", kv_lens, i32, (b,)), ("block_table", block_table, i32, (b, None))]
+    if lse is not None:
+        named.append(("lse", lse, torch.float32, (hq, total)))
+    if cu_q is not None:
+        named.append(("cu_q", cu_q, i32, (b + 1,)))
+    elif total != b:
+        raise ValueError(f"q has {total} rows for {b} requests of one each (pass cu_q)")
+    prefix_len = int(prefix_len)
+    if prefix_len < 0:
+        raise ValueError(f"prefix_len {prefix_len} < 0")
+    if prefix_len > 0:
+        named.append(("prefix_pages", prefix_pages, i32, (None,)))
+    if workspace is not None:
+        named.append(("workspace", workspace, workspace.dtype, None))
+    if slopes is not None:
+        named.append(("slopes", slopes, torch.float32, (hq,)))
+    _check_operands(named, dev)
+    if prefix_len > 0 and prefix_pages.shape[0] * page_size < prefix_len:
+        raise ValueError(f"{prefix_pages.shape[0]} prefix pages of {page_size} hold no "
+                         f"{prefix_len} keys")
+    with _OnDevice(dev, stream) as s:
+        _check(lib().paged_attn_fwd(
+            _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(o), out, _ptr(lse), _ptr(kv_lens),
+            _ptr(cu_q), _ptr(block_table), b, block_table.shape[1],
+            _ptr(prefix_pages) if prefix_len > 0 else None, prefix_len, total, hq, hkv, d, pages,
+            page_size, float(softmax_scale), 0.0 if softcap is None else float(softcap),
+            _ptr(slopes), _ptr(workspace), _nbytes(workspace), s))
+
+
+class PagedPlan:
+    """The workspace of attention over a paged cache for calls of so many
+    requests and query rows.  Lengths, tables and the prefix's length may
+    change from call to call; calls that may overlap need plans of their own,
+    and a captured call needs its plan as long as its graph."""
+
+    def __init__(self, batch, total_tokens, hq, hkv, head_dim, prefix=False, ragged=False,
+                 device="cuda"):
+        """prefix: whether calls have a shared prefix; ragged: whether they
+        give cu_q (otherwise every request has one row)."""
+        import torch
+        nbytes = ta_paged_workspace_bytes(batch, total_tokens, ragged, prefix, hq, hkv, head_dim)
+        self.workspace = (torch.empty(nbytes, dtype=torch.uint8, device=device)
+                          if nbytes > 0 else None)
+
+    def run(self, q, k_cache, v_cache, o, kv_lens, block_table, cu_q=None, prefix_pages=None,
+            prefix_len=0, lse=None, softmax_scale=None, softcap=None, slopes=None, stream=None):
+        if softmax_scale is None:
+            softmax_scale = 1.0 / float(q.shape[-1]) ** 0.5
+        paged_attn_fwd(q, k_cache, v_cache, o, lse, kv_lens, cu_q, block_table, prefix_pages,
+                       prefix_len, softmax_scale, softcap, slopes, self.workspace, stream)
+        return o
+
+
 def ta_probe_workspace_bytes(info: ScheduleInfo, hq: int) -> int:
     return int(lib().ta_probe_workspace_bytes(ctypes.byref(info), hq))
 
@@ -506,10 +748,16 @@ class Plan:
         self.workspace = (torch.empty(nbytes, dtype=torch.uint8, device=device)
                           if nbytes > 0 else None)
 
-    def run(self, q, k, v, o, lse=None, softmax_scale=None, stream=None):
+    def run(self, q, k, v, o, lse=None, softmax_scale=None, stream=None, softcap=None,
+            slopes=None):
+        """softcap, slopes: modified scores (scored_attn_fwd); plain where
+        neither is given."""
         if softmax_scale is None:
             softmax_scale = 1.0 / float(q.shape[-1]) ** 0.5
-        if self.kind == TRIANGLE:
+        if softcap is not None or slopes is not None:
+            scored_attn_fwd(q, k, v, o, lse, self.sched, self.info, softmax_scale, softcap,
+                            slopes, self.workspace, stream)
+        elif self.kind == TRIANGLE:
             triangle_attn_fwd(q, k, v, o, lse, self.sched, self.info,
                               softmax_scale, self.workspace, stream)
         elif self.kind == BLOCKSPARSE:
@@ -522,7 +770,8 @@ class Plan:
 
 
 def attention(kind, q, k, v, cu_seqlens, sink=0, window=1, last=0, tile=128,
-              splits=0, softmax_scale=None, out_dtype=None, return_lse=False):
+              splits=0, softmax_scale=None, out_dtype=None, return_lse=False, softcap=None,
+              slopes=None):
     """Allocate outputs with torch and run one pass (convenience wrapper)."""
     import torch
     out_dtype = out_dtype or torch.bfloat16
@@ -531,5 +780,5 @@ def attention(kind, q, k, v, cu_seqlens, sink=0, window=1, last=0, tile=128,
     o = torch.empty(q.shape, dtype=out_dtype, device=q.device)
     lse = (torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32,
                        device=q.device) if return_lse else None)
-    plan.run(q, k, v, o, lse, softmax_scale)
+    plan.run(q, k, v, o, lse, softmax_scale, softcap=softcap, slopes=slopes)
     return (o, lse) if return_lse else o

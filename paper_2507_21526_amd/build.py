@@ -15,7 +15,10 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libtriattn.so")
 SOURCES = [os.path.join(CSRC, "triattn_schedule.cpp"),
            os.path.join(CSRC, "triattn_fwd.hip"),
-           os.path.join(CSRC, "triattn_probe.hip")]
+           os.path.join(CSRC, "triattn_probe.hip"),
+           os.path.join(CSRC, "triattn_scored.hip"),
+           os.path.join(CSRC, "triattn_cache.hip"),
+           os.path.join(CSRC, "triattn_paged.hip")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 

@@ -1,0 +1,953 @@
+// Attention over the paged K/V cache of libtriattn.so: single tokens, drafted
+// tokens and pieces of prompts, with a prefix that the whole batch shares.
+//
+// Work.  The query rows of one kv head's group, (token, head of the group) in
+// token-major order, are cut per request into row tiles of ROWS rows; the keys
+// of a row tile into steps.  Laid end to end, the steps of all row tiles of a
+// kv head are cut into equal shares, one a workgroup, so that the load is even
+// whatever the lengths: a few long requests spread over the chip, many short
+// ones share a workgroup.  Lengths are read on the device (a captured call
+// follows them), each workgroup scanning the requests for itself.  A row tile
+// whose steps fall into several shares leaves normalised fp32 partials and
+// their log-sum-exp, joined in key order by a second kernel: results depend on
+// the shape alone, not on timing.
+//
+// The shared prefix is one more such pass, in which the rows of all requests
+// together attend to the prefix's keys: each K/V tile is read once for up to
+// 128 rows instead of once a request; the join adds its partials to those of a
+// row's own keys.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "triattn_device.h"
+#include "triattn_internal.h"
+#include "triattn_rows.h"
+#include "triattn_spans.h"
+
+namespace triattn {
+
+int page_log2(int32_t page_size);  // triattn_cache.hip
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMaxTiles = 2048;    // row tiles of a kv head
+constexpr int kPageEntries = 512;  // page ids held in LDS at a time
+constexpr int kCus = 256;
+
+// Words of the record that the own-keys pass leaves for the join: a header,
+// then one entry a row tile.
+constexpr int kMetaWords = 8;
+enum MetaHeader { MH_BAD = 0, MH_TILES, MH_SHARE };
+enum MetaField { MF_Q0 = 0, MF_RHO0, MF_ROWS, MF_POS0, MF_BEGIN, MF_END, MF_BAD };
+
+struct PagedArgs {
+    const uint16_t *q, *kc, *vc;
+    void *o;
+    float *lse;
+    const int32_t *kv_lens, *cu_q, *table, *prefix_pages;
+    float *slot_o, *slot_lse;  // pieces of row tiles: [2 slots, hkv, ROWS (, D)]
+    float *row_o, *row_lse;    // whole row tiles that the join still needs: [T, hq (, D)]
+    int32_t *meta;
+    ScoreArgs score;
+    int32_t total_tokens, batch, width, hq, hkv, group;
+    uint32_t group_inv;  // 65536 / group + 1: x * group_inv >> 16 = x / group, x < 2^13
+    int32_t page_log2, num_pages, prefix_len;
+    int32_t slots;      // shares a kv head
+    int32_t max_tiles;  // row tiles that the record has room for
+    int32_t o_f32;
+};
+
+// Shapes of the two forms of the pass.
+//   RB = 1: up to 32 rows.  Each wave takes every fourth 32-key tile of a
+//     step into its own LDS stages and keeps its own softmax; nothing waits on
+//     another wave until the four are joined at the end of a piece.
+//   RB = 4: four waves of 32 rows each over the same 64-key tiles.
+template <int D, int RB>
+struct PagedShape {
+    static constexpr int NKB = RB == 4 ? 2 : 1;
+    static constexpr int TK = 32 * NKB;      // keys of a tile
+    static constexpr int KS = 4 / RB;        // key splits of a workgroup
+    static constexpr int STEP = TK * KS;     // keys of a step
+    static constexpr int ROWS = 32 * RB;
+    static constexpr int TILE_BYTES = TK * 2 * D;
+    static constexpr int STAGE_BYTES = 2 * TILE_BYTES;  // K tile, then V tile
+    static constexpr int LDS_BYTES = KS * 2 * STAGE_BYTES;
+    static constexpr int WGS_PER_CU = LDS_BYTES > 65536 ? 1 : 2;
+};
+
+// Exclusive scan of val(i), i < n, into out[0 .. n] (out[n]: the total) by
+// the workgroup, n <= 8 kThreads.
+template <typename F>
+__device__ __forceinline__ void block_scan(int n, int32_t *out, int32_t *wave_sum, F &&val)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int per = (n + kThreads - 1) / kThreads;
+    int32_t sum = 0;
+    for (int i = tid * per; i < min(n, (tid + 1) * per); ++i) {
+        out[i] = sum;
+        sum += val(i);
+    }
+    int32_t inc = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int32_t y = __shfl_up(inc, o);
+        inc += lane >= o ? y : 0;
+    }
+    if (lane == 63)
+        wave_sum[wave] = inc;
+    __syncthreads();
+    int32_t base = inc - sum, total = 0;
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) {
+        base += w < wave ? wave_sum[w] : 0;
+        total += wave_sum[w];
+    }
+    for (int i = tid * per; i < min(n, (tid + 1) * per); ++i)
+        out[i] += base;
+    if (tid == 0)
+        out[n] = total;
+    __syncthreads();
+}
+
+// The last i with start[i] <= x < start[i + 1], start ascending with
+// start[0] <= x < start[n].
+__device__ __forceinline__ int find_start(const int32_t *start, int n, int32_t x)
+{
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (start[mid] <= x)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    return lo;
+}
+
+struct RowTile {
+    int32_t q0;     // first token of the request
+    int32_t rho0;   // first row of the tile in the request
+    int32_t rows;   // rows of the tile
+    int32_t pos0;   // position of the request's first query token
+    int32_t limit;  // keys that some row of the tile keeps
+    int32_t req;
+    int32_t bad;    // a length past the block table
+};
+
+template <int D, int RB, int SCORE, bool PREFIX>
+__global__ __launch_bounds__(kThreads, (PagedShape<D, RB>::WGS_PER_CU)) void paged_attn_kernel(PagedArgs a)
+{
+    using S = PagedShape<D, RB>;
+    constexpr int ROW_BYTES = 2 * D;
+    constexpr int CHUNKS = D / 8;
+    constexpr int COPY_ROWS = 1024 / ROW_BYTES;          // keys of a 1 KB copy
+    constexpr int TILE_COPIES = S::TILE_BYTES / 1024;    // copies of a K (or V) tile
+    constexpr int COPY_WAVES = RB;                       // waves that share a tile's copies
+    constexpr int COPIES = TILE_COPIES / COPY_WAVES;     // of a wave, for K and again for V
+    constexpr int D_BLOCKS = D / 32;
+
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[S::LDS_BYTES];
+    __shared__ int32_t s_req[PREFIX ? 1 : TA_MAX_BATCH + 1];  // first row tile of a request
+    __shared__ int32_t s_step[PREFIX ? 1 : kMaxTiles + 1];    // first step of a row tile
+    __shared__ int32_t s_page[kPageEntries];
+    __shared__ int32_t s_wave[kThreads / 64];
+    __shared__ float s_ml[RB == 1 ? 4 : 1][32][2];
+    __shared__ int32_t s_bad;
+
+    const int tid = threadIdx.x;
+    const int lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int g = blockIdx.x % a.hkv;
+    const int slot = blockIdx.x / a.hkv;
+    // a value that is the same on every lane, in a scalar register
+    auto uni = [](int x) TA_INLINE -> int { return __builtin_amdgcn_readfirstlane(x); };
+    auto div_group = [&](int x) TA_INLINE -> int {
+        // row numbers pass 2^13 in prompts: a division there
+        return x < 8192 ? (int)((uint32_t)x * a.group_inv >> 16) : x / a.group;
+    };
+
+    // The row tiles and where each one's steps begin.
+    int n_tiles, total;
+    const int32_t prefix_steps = PREFIX ? (a.prefix_len + S::STEP - 1) / S::STEP : 0;
+    auto tile_of = [&](int t) TA_INLINE -> RowTile {
+        RowTile r;
+        r.bad = 0;
+        if constexpr (PREFIX) {
+            r.q0 = 0;
+            r.rho0 = t * S::ROWS;
+            r.rows = min(S::ROWS, a.total_tokens * a.group - r.rho0);
+            r.pos0 = 0;
+            r.limit = a.prefix_len;
+            r.req = 0;
+        } else {
+            int nq = 1;
+            r.req = t;
+            r.q0 = t;
+            r.rho0 = 0;
+            if (a.cu_q) {
+                r.req = find_start(s_req, a.batch, t);
+                r.q0 = a.cu_q[r.req];
+                nq = a.cu_q[r.req + 1] - r.q0;
+                r.rho0 = (t - s_req[r.req]) * S::ROWS;
+            }
+            int32_t kv = a.kv_lens[r.req];
+            r.bad = kv > (a.width << a.page_log2);
+            kv = r.bad ? 0 : max(kv, 0);
+            r.rows = min(S::ROWS, nq * a.group - r.rho0);
+            r.pos0 = kv - nq;
+            r.limit = max(0, r.pos0 + div_group(r.rho0 + r.rows - 1) + 1);
+        }
+        return r;
+    };
+    if constexpr (PREFIX) {
+        n_tiles = (a.total_tokens * a.group + S::ROWS - 1) / S::ROWS;
+        total = n_tiles * prefix_steps;
+    } else {
+        n_tiles = a.batch;
+        if (a.cu_q) {
+            if (tid == 0)
+                s_bad = 0;
+            __syncthreads();
+            bool bad = tid == 0 && (a.cu_q[0] != 0);
+            block_scan(a.batch, s_req, s_wave, [&](int b) TA_INLINE -> int32_t {
+                const int32_t b0 = a.cu_q[b], b1 = a.cu_q[b + 1];
+                if (b0 < 0 || b1 < b0 || b1 > a.total_tokens) {
+                    bad = true;
+                    return 0;
+                }
+                return ((b1 - b0) * a.group + S::ROWS - 1) / S::ROWS;
+            });
+            if (bad)
+                s_bad = 1;
+            __syncthreads();
+            n_tiles = uni(s_req[a.batch]);
+            // query offsets that are none: nothing is computed, NaN shows it
+            if (s_bad != 0 || n_tiles > a.max_tiles) {
+                if (blockIdx.x == 0 && tid == 0) {
+                    a.meta[MH_BAD] = 1;
+                    a.meta[MH_TILES] = 0;
+                }
+                rows_poison(a.o, a.o_f32, a.lse, (int64_t)a.total_tokens * a.hq, D);
+                return;
+            }
+        }
+        block_scan(n_tiles, s_step, s_wave, [&](int t) TA_INLINE -> int32_t {
+            return (tile_of(t).limit + S::STEP - 1) / S::STEP;
+        });
+        total = uni(s_step[n_tiles]);
+    }
+    const int share = max(1, (total + a.slots - 1) / a.slots);
+    if constexpr (!PREFIX) {
+        if (blockIdx.x == 0) {
+            if (tid == 0) {
+                a.meta[MH_BAD] = 0;
+                a.meta[MH_TILES] = n_tiles;
+                a.meta[MH_SHARE] = share;
+            }
+            for (int t = tid; t < n_tiles; t += kThreads) {
+                const RowTile r = tile_of(t);
+                int32_t *m = a.meta + kMetaWords * (t + 1);
+                m[MF_Q0] = r.q0;
+                m[MF_RHO0] = r.rho0;
+                m[MF_ROWS] = r.rows;
+                m[MF_POS0] = r.pos0;
+                m[MF_BEGIN] = s_step[t];
+                m[MF_END] = s_step[t + 1];
+                m[MF_BAD] = r.bad;
+            }
+        }
+    }
+    const int share0 = slot * share;
+    const int share1 = min(total, share0 + share);
+    if (slot > 0 && share0 >= total)
+        return;
+
+    const uint32_t smem_addr =
+        (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
+    // this wave's stages (RB = 1) or the workgroup's (RB = 4)
+    const int wave_lds = RB == 1 ? wave * 2 * S::STAGE_BYTES : 0;
+    const int copy_rank = RB == 1 ? 0 : wave;
+    const int dma_row = lane / CHUNKS, dma_chunk = lane % CHUNKS;
+    const int64_t page_stride = ((int64_t)a.hkv << a.page_log2) * ROW_BYTES;
+    const int64_t head_off = ((int64_t)g << a.page_log2) * ROW_BYTES;
+    const unsigned char *kc = reinterpret_cast<const unsigned char *>(a.kc) + head_off;
+    const unsigned char *vc = reinterpret_cast<const unsigned char *>(a.vc) + head_off;
+    const int page_mask = (1 << a.page_log2) - 1;
+
+    RowBlock<D, S::NKB, SCORE> rb;
+    rb.init(lane);
+
+    for (int at = share0, t = -1; at < share1;) {
+        // the row tile of step `at`
+        int t_begin, t_end;
+        if constexpr (PREFIX) {
+            t = at / prefix_steps;
+            t_begin = t * prefix_steps;
+            t_end = t_begin + prefix_steps;
+        } else {
+            if (t < 0)
+                t = find_start(s_step, n_tiles, at);
+            else
+                do
+                    ++t;
+                while (s_step[t + 1] <= at);
+            t = uni(t);
+            t_begin = uni(s_step[t]);
+            t_end = uni(s_step[t + 1]);
+        }
+        RowTile rt = tile_of(t);
+        rt.q0 = uni(rt.q0);
+        rt.rho0 = uni(rt.rho0);
+        rt.rows = uni(rt.rows);
+        rt.pos0 = uni(rt.pos0);
+        rt.limit = uni(rt.limit);
+        rt.req = uni(rt.req);
+        const int step0 = at - t_begin;
+        const int step1 = min(share1, t_end) - t_begin;
+        const bool whole = step0 == 0 && step1 == t_end - t_begin;
+        const int piece = 2 * slot + (t_begin > share0 ? 1 : 0);
+        at = t_begin + step1;
+
+        // this lane's query row (rows past the tile repeat its last one)
+        const int block0 = RB == 1 ? 0 : 32 * wave;  // the wave's first row in the tile
+        const int row = min(block0 + rb.col, rt.rows - 1);
+        const int rho = rt.rho0 + row;
+        const int tq = div_group(rho);
+        const int head = g * a.group + rho - tq * a.group;
+        const int tok = rt.q0 + tq;
+        rb.load_q(a.q + ((int64_t)tok * a.hq + head) * D);
+        rb.reset();
+        float slope = 0.f;
+        if constexpr ((SCORE & kScoreSlope) != 0)
+            slope = a.score.slopes[head] * kRowsLog2e;
+        // the last key that this row keeps, and the first row's: steps up to
+        // that one need no mask
+        const int last = PREFIX ? a.prefix_len - 1 : rt.pos0 + tq;
+        const int first_last =
+            PREFIX ? a.prefix_len - 1
+                   : rt.pos0 + div_group(rt.rho0 + min(block0, rt.rows - 1));
+        const int wave_last =
+            PREFIX ? a.prefix_len - 1
+                   : rt.pos0 + div_group(rt.rho0 + min(block0 + 31, rt.rows - 1));
+        // distances in the prefix pass are taken from the prefix's end: the
+        // join adds what each row is past it
+        const int dist_row = PREFIX ? a.prefix_len : last;
+        const int32_t *pages = PREFIX ? a.prefix_pages : a.table + (int64_t)rt.req * a.width;
+        bool fresh = true;
+        if (tid == 0)
+            s_bad = 0;
+
+        const int seg_steps = (((kPageEntries - 1) << a.page_log2) / S::STEP);
+        for (int seg0 = step0; seg0 < step1; seg0 += seg_steps) {
+            const int seg1 = min(step1, seg0 + seg_steps);
+            const int key_end = min(seg1 * S::STEP, rt.limit);
+            const int page0 = (seg0 * S::STEP) >> a.page_log2;
+            const int n_pages = ((key_end - 1) >> a.page_log2) + 1 - page0;
+            __syncthreads();  // the last segment's ids, and stages, are done with
+            for (int i = tid; i < n_pages; i += kThreads) {
+                int32_t id = pages[page0 + i];
+                if (id < 0 || id >= a.num_pages) {
+                    id = 0;
+                    s_bad = 1;
+                }
+                s_page[i] = id;
+            }
+            __syncthreads();
+
+            // Copies of one tile's K and V rows into a stage.  Keys from
+            // rt.limit on repeat the last one before it; they lie past every
+            // row's last key.
+            auto copy_tile = [&](int key0, int stage) TA_INLINE {
+                asm volatile("" ::: "memory");
+                const uint32_t lds =
+                    smem_addr + wave_lds + stage * S::STAGE_BYTES + copy_rank * COPIES * 1024;
+                // lane i of the first COPIES holds the page of this wave's copy i
+                const int mine = min(key0 + (copy_rank * COPIES + (lane & (COPIES - 1))) * COPY_ROWS,
+                                     rt.limit - 1);
+                const int ids = s_page[(mine >> a.page_log2) - page0];
+#pragma unroll
+                for (int i = 0; i < COPIES; ++i) {
+                    const int m = copy_rank * COPIES + i;
+                    int key = key0 + m * COPY_ROWS;
+                    const int over = rt.limit - 1 - key;  // keys after the first
+                    int lim = min(over, COPY_ROWS - 1);
+                    if (over < 0) {
+                        key = rt.limit - 1;
+                        lim = 0;
+                    }
+                    const int64_t id = __builtin_amdgcn_readlane(ids, i);
+                    const int64_t off =
+                        id * page_stride + (int64_t)((key & page_mask) * ROW_BYTES);
+                    const int r = m * COPY_ROWS + dma_row;
+                    const uint32_t row_off = (uint32_t)(min(dma_row, lim) * ROW_BYTES);
+                    copy_to_lds16(kc + off, row_off + ((dma_chunk ^ rows_kswz<D>(r)) << 4),
+                                  lds + i * 1024);
+                    copy_to_lds16(vc + off, row_off + ((dma_chunk ^ rows_vswz<D>(r)) << 4),
+                                  lds + S::TILE_BYTES + i * 1024);
+                }
+                asm volatile("" ::: "memory");
+            };
+            auto compute_tile = [&](int key0, int stage) TA_INLINE {
+                const unsigned char *kt = smem + wave_lds + stage * S::STAGE_BYTES;
+                f32x16 s[S::NKB];
+                bf16x8 p[S::NKB][2];
+                rb.products(kt, s);
+                rb.modify(s, a.score, slope, key0 - dist_row);
+                const bool masked = key0 + S::TK - 1 > first_last;
+                if (masked)
+                    rb.mask_above(s, last - key0);
+                rb.softmax(s, a.score, p, fresh);
+                fresh = false;
+                if (masked)
+                    rb.accumulate_masked(kt + S::TILE_BYTES, p, lane);
+                else
+                    rb.accumulate(kt + S::TILE_BYTES, p);
+            };
+            if constexpr (RB == 1) {
+                // tiles of this wave: key0 = step STEP + wave TK, two stages
+                const int base = seg0 * S::STEP + wave * S::TK;
+                const int n = base < key_end ? (key_end - base + S::STEP - 1) / S::STEP : 0;
+                if (n > 0)
+                    copy_tile(base, 0);
+                if (n > 1)
+                    copy_tile(base + S::STEP, 1);
+                for (int i = 0; i < n; ++i) {
+                    if (i + 1 < n)
+                        rows_wait_copies<2 * COPIES>();
+                    else
+                        rows_wait_copies<0>();
+                    __builtin_amdgcn_sched_barrier(0);
+                    compute_tile(base + i * S::STEP, i & 1);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (i + 2 < n) {
+                        // every read of the stage has returned before it is
+                        // written again
+                        __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+                        copy_tile(base + (i + 2) * S::STEP, i & 1);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+            } else {
+                const int n = (key_end - seg0 * S::STEP + S::STEP - 1) / S::STEP;
+                copy_tile(seg0 * S::STEP, 0);
+                for (int i = 0; i < n; ++i) {
+                    // this step's tile has landed for every wave, and every
+                    // wave is done with the other stage
+                    __builtin_amdgcn_sched_barrier(0);
+                    rows_wait_copies<0>();
+                    barrier_no_fence();
+                    __builtin_amdgcn_sched_barrier(0);
+                    const int key0 = (seg0 + i) * S::STEP;
+                    if (i + 1 < n)
+                        copy_tile(key0 + S::STEP, (i + 1) & 1);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (block0 < rt.rows && key0 <= wave_last)
+                        compute_tile(key0, i & 1);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
+
+        // Where the rows go.
+        const bool to_o = whole && !a.row_o;
+        auto store4 = [&](f32x4r x, int r, int d0) TA_INLINE {
+            const int rr = rt.rho0 + r, qt = div_group(rr);
+            const int64_t orow =
+                (int64_t)(rt.q0 + qt) * a.hq + g * a.group + rr - qt * a.group;
+            if (to_o && !a.o_f32)
+                *reinterpret_cast<bf16x4r *>(static_cast<__bf16 *>(a.o) + orow * D + d0) =
+                    __builtin_convertvector(x, bf16x4r);
+            else if (to_o)
+                *reinterpret_cast<f32x4r *>(static_cast<float *>(a.o) + orow * D + d0) = x;
+            else if (whole)
+                *reinterpret_cast<f32x4r *>(a.row_o + orow * D + d0) = x;
+            else
+                *reinterpret_cast<f32x4r *>(
+                    a.slot_o + (((int64_t)piece * a.hkv + g) * S::ROWS + r) * D + d0) = x;
+        };
+        auto store_lse = [&](float x, int r) TA_INLINE {
+            const int rr = rt.rho0 + r, qt = div_group(rr);
+            const int h = g * a.group + rr - qt * a.group;
+            if (to_o) {
+                if (a.lse)
+                    a.lse[(int64_t)h * a.total_tokens + rt.q0 + qt] = x;
+            } else if (whole) {
+                a.row_lse[(int64_t)(rt.q0 + qt) * a.hq + h] = x;
+            } else {
+                a.slot_lse[((int64_t)piece * a.hkv + g) * S::ROWS + r] = x;
+            }
+        };
+        __syncthreads();  // the stages are done with, and s_bad is final
+        const float nan_if_bad = s_bad != 0 ? __builtin_nanf("") : 0.f;
+        if constexpr (RB == 1) {
+            // join the four waves: each leaves its accumulators in its stages
+            constexpr int PITCH = 4 * D + 16;
+            static_assert(32 * PITCH <= 2 * S::STAGE_BYTES, "accumulators fit the wave's stages");
+            unsigned char *mine = smem + wave * 2 * S::STAGE_BYTES;
+            const float l = rows_pair_sum(rb.l_run);
+            if (rb.col < rt.rows) {
+                if (rb.half == 0) {
+                    s_ml[wave][rb.col][0] = rb.m_ref;
+                    s_ml[wave][rb.col][1] = l;
+                }
+#pragma unroll
+                for (int b = 0; b < D_BLOCKS; ++b)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        f32x4r x;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            x[e] = rb.oacc[b][4 * c + e];
+                        *reinterpret_cast<f32x4r *>(mine + rb.col * PITCH +
+                                                    (32 * b + 8 * c + 4 * rb.half) * 4) = x;
+                    }
+            }
+            __syncthreads();
+            for (int i = tid; i < rt.rows * (D / 4); i += kThreads) {
+                const int r = i / (D / 4), d0 = 4 * (i % (D / 4));
+                float m = -INFINITY;
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    m = fmaxf(m, s_ml[w][r][0]);
+                const float m_use = m == -INFINITY ? 0.f : m;
+                float den = 0.f;
+                f32x4r x{};
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const float f = __builtin_amdgcn_exp2f(s_ml[w][r][0] - m_use);
+                    den += f * s_ml[w][r][1];
+                    const f32x4r y = *reinterpret_cast<const f32x4r *>(
+                        smem + w * 2 * S::STAGE_BYTES + r * PITCH + d0 * 4);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        x[e] += f * y[e];
+                }
+                const float inv = (den == 0.f ? 0.f : 1.f / den) + nan_if_bad;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    x[e] *= inv;
+                store4(x, r, d0);
+                if (d0 == 0)
+                    store_lse((den == 0.f ? -INFINITY : (m + __log2f(den)) * kRowsLn2) +
+                                  nan_if_bad, r);
+            }
+        } else if (block0 + rb.col < rt.rows) {
+            float inv, lse;
+            rb.finish(inv, lse);
+            inv += nan_if_bad;
+            lse += nan_if_bad;
+#pragma unroll
+            for (int b = 0; b < D_BLOCKS; ++b)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    f32x4r x;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        x[e] = rb.oacc[b][4 * c + e] * inv;
+                    store4(x, block0 + rb.col, 32 * b + 8 * c + 4 * rb.half);
+                }
+            if (rb.half == 0)
+                store_lse(lse, block0 + rb.col);
+        }
+        __syncthreads();  // s_bad and the accumulators are read
+    }
+}
+
+struct JoinArgs {
+    void *o;
+    float *lse;
+    const int32_t *meta;
+    const float *slot_o, *slot_lse;
+    int32_t tile_rows;
+    // the prefix pass (prefix_len 0: none)
+    const float *row_o, *row_lse;
+    const float *pre_slot_o, *pre_slot_lse, *pre_row_o, *pre_row_lse;
+    int32_t prefix_len, pre_rows, pre_step, pre_slots;
+    const float *slopes;
+    int32_t total_tokens, hq, hkv, group, o_f32;
+};
+
+// Joins the partials of a row: O = sum_c w_c O_c / sum_c w_c with w_c =
+// exp(LSE_c - max_c LSE_c), the prefix's before the row's own, in key order.
+// A workgroup takes one row tile of one kv head, a wave one row at a time.
+// Row tiles that one share finished need nothing here, unless no share had
+// anything to do for them (rows without keys) or a prefix comes before.
+template <int D>
+__global__ __launch_bounds__(kThreads) void paged_join_kernel(JoinArgs a)
+{
+    constexpr int PER = D / 64;
+    if (a.meta[MH_BAD]) {
+        rows_poison(a.o, a.o_f32, a.lse, (int64_t)a.total_tokens * a.hq, D);
+        return;
+    }
+    const int t = blockIdx.x / a.hkv, g = blockIdx.x % a.hkv;
+    if (t >= a.meta[MH_TILES])
+        return;
+    const int32_t *m = a.meta + kMetaWords * (t + 1);
+    const int32_t share = a.meta[MH_SHARE];
+    const int32_t q0 = m[MF_Q0], rho0 = m[MF_RHO0], rows = m[MF_ROWS], pos0 = m[MF_POS0];
+    const int32_t begin = m[MF_BEGIN], end = m[MF_END], bad = m[MF_BAD];
+    const int w0 = begin / share;
+    const int n_own = end > begin ? (end - 1) / share - w0 + 1 : 0;
+    if (n_own == 1 && a.prefix_len == 0)
+        return;
+    const int lane = threadIdx.x & 63;
+    const int pre_steps = a.prefix_len > 0 ? (a.prefix_len + a.pre_step - 1) / a.pre_step : 0;
+    for (int r = threadIdx.x >> 6; r < rows; r += kThreads / 64) {
+        const int rho = rho0 + r, qt = rho / a.group, h = g * a.group + rho - qt * a.group;
+        const int64_t orow = (int64_t)(q0 + qt) * a.hq + h;
+        // the prefix pass's pieces of this row: its rows are those of all
+        // requests, in the same order
+        int n_pre = 0, pw0 = 0, prow = 0, pshare = 1, pbegin = 0;
+        float shift = 0.f;
+        if (a.prefix_len > 0 && pos0 + qt >= 0) {
+            const int prho = (q0 + qt) * a.group + rho - qt * a.group;
+            const int n_tiles = (a.total_tokens * a.group + a.pre_rows - 1) / a.pre_rows;
+            pshare = max(1, (n_tiles * pre_steps + a.pre_slots - 1) / a.pre_slots);
+            pbegin = prho / a.pre_rows * pre_steps;
+            prow = prho % a.pre_rows;
+            pw0 = pbegin / pshare;
+            n_pre = (pbegin + pre_steps - 1) / pshare - pw0 + 1;
+            if (a.slopes)
+                shift = -a.slopes[h] * (float)(pos0 + qt);
+        }
+        const int n = n_pre + n_own;
+        auto part = [&](int c, const float *&o) TA_INLINE -> float {
+            if (c < n_pre) {
+                if (n_pre == 1) {
+                    o = a.pre_row_o + orow * D;
+                    return a.pre_row_lse[orow] + shift;
+                }
+                const int w = pw0 + c;
+                const int64_t at = (((int64_t)2 * w + (pbegin > w * pshare ? 1 : 0)) * a.hkv + g) *
+                                       a.pre_rows + prow;
+                o = a.pre_slot_o + at * D;
+                return a.pre_slot_lse[at] + shift;
+            }
+            if (n_own == 1) {
+                o = a.row_o + orow * D;
+                return a.row_lse[orow];
+            }
+            const int w = w0 + c - n_pre;
+            const int64_t at =
+                (((int64_t)2 * w + (begin > w * share ? 1 : 0)) * a.hkv + g) * a.tile_rows + r;
+            o = a.slot_o + at * D;
+            return a.slot_lse[at];
+        };
+        float mx = -INFINITY, nan = 0.f;
+        for (int c = lane; c < n; c += 64) {
+            const float *po;
+            const float l = part(c, po);
+            mx = fmaxf(mx, l);
+            nan += l != l ? l : 0.f;
+        }
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) {
+            mx = fmaxf(mx, __shfl_xor(mx, o));
+            nan += __shfl_xor(nan, o);
+        }
+        const float m_use = mx == -INFINITY ? 0.f : mx;
+        float acc[PER] = {}, den = nan + (bad ? __builtin_nanf("") : 0.f);
+        constexpr int UNROLL = 8;
+        for (int c = 0; c < n; c += UNROLL) {
+            float x[UNROLL][PER], l[UNROLL];
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) {
+                const float *po;
+                l[u] = part(min(c + u, n - 1), po);
+#pragma unroll
+                for (int e = 0; e < PER; ++e)
+                    x[u][e] = po[PER * lane + e];
+            }
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u)
+                if (c + u < n) {
+                    const float f = __expf(l[u] - m_use);
+                    den += f;
+#pragma unroll
+                    for (int e = 0; e < PER; ++e)
+                        acc[e] += f * x[u][e];
+                }
+        }
+        const float inv = den == 0.f ? 0.f : 1.f / den;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            const int64_t at = orow * D + PER * lane + e;
+            if (a.o_f32)
+                static_cast<float *>(a.o)[at] = acc[e] * inv;
+            else
+                static_cast<__bf16 *>(a.o)[at] = (__bf16)(acc[e] * inv);
+        }
+        if (a.lse && lane == 0)
+            a.lse[(int64_t)h * a.total_tokens + q0 + qt] =
+                den == 0.f ? -INFINITY : m_use + __logf(den);
+    }
+}
+
+// How a call is laid out: forms, shares and the parts of the workspace.
+struct PagedLayout {
+    int own_rb, pre_rb;        // row blocks of the two passes
+    int own_slots, pre_slots;  // shares a kv head
+    int max_tiles;
+    size_t meta, own_slot_o, own_slot_lse, own_row_o, own_row_lse, pre_slot_o, pre_slot_lse,
+        pre_row_o, pre_row_lse, bytes;
+};
+
+int wgs_per_cu(int rb, int d)
+{
+    if (d == 128)
+        return rb == 4 ? PagedShape<128, 4>::WGS_PER_CU : PagedShape<128, 1>::WGS_PER_CU;
+    return rb == 4 ? PagedShape<64, 4>::WGS_PER_CU : PagedShape<64, 1>::WGS_PER_CU;
+}
+
+PagedLayout paged_layout(int32_t batch, int64_t total_tokens, bool ragged, bool prefix, int32_t hq,
+                         int32_t hkv, int32_t d)
+{
+    PagedLayout p{};
+    const int64_t group = hq / hkv;
+    // Up to 32 rows a request on average: tiles of 32 rows, which a step's
+    // four waves share out by keys.
+    p.own_rb = !ragged || total_tokens * group <= (int64_t)batch * 32 ? 1 : 4;
+    p.pre_rb = total_tokens * group <= 32 ? 1 : 4;
+    p.own_slots = std::max(1, kCus * wgs_per_cu(p.own_rb, d) / hkv);
+    p.pre_slots = std::max(1, kCus * wgs_per_cu(p.pre_rb, d) / hkv);
+    const int64_t rows = 32 * p.own_rb;
+    p.max_tiles = (int)std::min<int64_t>(
+        kMaxTiles + 1, ragged ? total_tokens * group / rows + batch : (int64_t)batch);
+    size_t at = 0;
+    auto take = [&](size_t n) {
+        const size_t here = at;
+        at += (n + 255) / 256 * 256;
+        return here;
+    };
+    p.meta = take((size_t)(p.max_tiles + 1) * kMetaWords * 4);
+    const size_t own = (size_t)2 * p.own_slots * hkv * rows;
+    p.own_slot_o = take(own * d * 4);
+    p.own_slot_lse = take(own * 4);
+    if (prefix) {
+        const size_t all = (size_t)total_tokens * hq;
+        const size_t pre = (size_t)2 * p.pre_slots * hkv * 32 * p.pre_rb;
+        p.own_row_o = take(all * d * 4);
+        p.own_row_lse = take(all * 4);
+        p.pre_slot_o = take(pre * d * 4);
+        p.pre_slot_lse = take(pre * 4);
+        p.pre_row_o = take(all * d * 4);
+        p.pre_row_lse = take(all * 4);
+    }
+    p.bytes = at;
+    return p;
+}
+
+template <int D, int RB, bool PREFIX>
+void launch_scores(int score, dim3 grid, hipStream_t s, const PagedArgs &a)
+{
+    switch (score) {
+    case 0: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 0, PREFIX>), grid, dim3(kThreads), 0, s, a); break;
+    case 1: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 1, PREFIX>), grid, dim3(kThreads), 0, s, a); break;
+    case 2: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 2, PREFIX>), grid, dim3(kThreads), 0, s, a); break;
+    default: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 3, PREFIX>), grid, dim3(kThreads), 0, s, a); break;
+    }
+}
+
+template <bool PREFIX>
+hipError_t launch_pass(int d, int rb, int score, hipStream_t s, const PagedArgs &a)
+{
+    const dim3 grid((uint32_t)(a.slots * a.hkv));
+    if (d == 128 && rb == 1)
+        launch_scores<128, 1, PREFIX>(score, grid, s, a);
+    else if (d == 128)
+        launch_scores<128, 4, PREFIX>(score, grid, s, a);
+    else if (rb == 1)
+        launch_scores<64, 1, PREFIX>(score, grid, s, a);
+    else
+        launch_scores<64, 4, PREFIX>(score, grid, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace triattn
+
+using namespace triattn;
+
+extern "C" size_t ta_paged_workspace_bytes(int32_t batch, int64_t total_tokens, int32_t ragged,
+                                           int32_t prefix, int32_t hq, int32_t hkv,
+                                           int32_t head_dim)
+{
+    if (batch < 0 || total_tokens < 0 || total_tokens > INT32_MAX || hq <= 0 || hkv <= 0 ||
+        hq % hkv != 0 || hq / hkv > 8 || (head_dim != 64 && head_dim != 128))
+        return 0;
+    return paged_layout(batch, total_tokens, ragged != 0, prefix != 0, hq, hkv, head_dim).bytes;
+}
+
+extern "C" ta_status paged_attn_fwd(const void *q, const void *k_cache, const void *v_cache,
+                                    void *o, int32_t o_dtype, float *lse, const int32_t *kv_lens,
+                                    const int32_t *cu_q, const int32_t *block_table, int32_t batch,
+                                    int32_t table_width, const int32_t *prefix_pages,
+                                    int32_t prefix_len, int64_t total_tokens, int32_t hq,
+                                    int32_t hkv, int32_t head_dim, int64_t num_pages,
+                                    int32_t page_size, float softmax_scale, float softcap,
+                                    const float *slopes, void *workspace, size_t workspace_bytes,
+                                    void *stream)
+{
+    clear_error();
+    const char *fn = "paged_attn_fwd";
+    if (batch < 0 || total_tokens < 0 || table_width < 0 || prefix_len < 0 || num_pages < 0)
+        return fail(TA_ERR_INVALID_ARG, "%s: negative size", fn);
+    if (hq <= 0 || hkv <= 0)
+        return fail(TA_ERR_INVALID_ARG, "%s: hq and hkv must be positive", fn);
+    if (hq % hkv != 0)
+        return fail(TA_ERR_INVALID_ARG, "%s: hq %d not a multiple of hkv %d", fn, hq, hkv);
+    if (hq / hkv > 8)
+        return fail(TA_ERR_UNSUPPORTED, "%s: GQA group %d > 8", fn, hq / hkv);
+    if (head_dim != 64 && head_dim != 128)
+        return fail(TA_ERR_UNSUPPORTED, "%s: head_dim %d not in {64, 128}", fn, head_dim);
+    const int lp = page_log2(page_size);
+    if (lp < 0)
+        return fail(TA_ERR_UNSUPPORTED, "%s: page_size %d not in {16, 32, 64, 128, 256}", fn,
+                    page_size);
+    if (o_dtype != TA_OUT_BF16 && o_dtype != TA_OUT_F32)
+        return fail(TA_ERR_INVALID_ARG, "%s: bad o_dtype %d", fn, o_dtype);
+    if (!std::isfinite(softmax_scale) || !(softmax_scale > 0.f))
+        return fail(TA_ERR_INVALID_ARG, "%s: softmax_scale must be finite and > 0", fn);
+    if (!std::isfinite(softcap) || softcap < 0.f)
+        return fail(TA_ERR_INVALID_ARG, "%s: softcap must be finite and >= 0", fn);
+    if (softcap > kRowsMaxCap)
+        return fail(TA_ERR_UNSUPPORTED, "%s: softcap %g > %g", fn, softcap, kRowsMaxCap);
+    ScoreArgs score_args;
+    if (!rows_score_args(score_args, softmax_scale, softcap, slopes))
+        return fail(TA_ERR_INVALID_ARG, "%s: softcap too small for the scale", fn);
+    if (!cu_q && total_tokens != batch)
+        return fail(TA_ERR_INVALID_ARG, "%s: %lld tokens for %d requests of one each", fn,
+                    (long long)total_tokens, batch);
+    if (batch > TA_MAX_BATCH)
+        return fail(TA_ERR_UNSUPPORTED, "%s: batch %d > %d", fn, batch, TA_MAX_BATCH);
+    if (num_pages > INT32_MAX / page_size || (int64_t)table_width * page_size > INT32_MAX ||
+        prefix_len > INT32_MAX - 256 || (int64_t)total_tokens * hq > INT32_MAX)
+        return fail(TA_ERR_UNSUPPORTED, "%s: positions, slots or rows past 32 bits", fn);
+    const PagedLayout p =
+        paged_layout(batch, total_tokens, cu_q != nullptr, prefix_len > 0, hq, hkv, head_dim);
+    const int64_t group = hq / hkv;
+    if (p.max_tiles > kMaxTiles)
+        return fail(TA_ERR_UNSUPPORTED, "%s: more than %d row tiles a kv head (pass fewer query "
+                    "tokens at a time)", fn, kMaxTiles);
+    // steps are counted in 32 bits
+    const int64_t steps = (int64_t)p.max_tiles * ((int64_t)table_width * page_size / 64 + 1);
+    const int64_t pre_tiles = (total_tokens * group + 32 * p.pre_rb - 1) / (32 * p.pre_rb);
+    if (steps > INT32_MAX || pre_tiles * (prefix_len / 64 + 1) > INT32_MAX)
+        return fail(TA_ERR_UNSUPPORTED, "%s: too many steps", fn);
+    if (total_tokens == 0 || batch == 0)
+        return TA_OK;
+    if (!q || !o || !kv_lens || (num_pages > 0 && (!k_cache || !v_cache)) ||
+        (table_width > 0 && !block_table) || (prefix_len > 0 && !prefix_pages))
+        return fail(TA_ERR_INVALID_ARG, "%s: NULL argument", fn);
+    if (num_pages == 0)
+        return fail(TA_ERR_INVALID_ARG, "%s: a cache without pages", fn);
+    if (((uintptr_t)q | (uintptr_t)k_cache | (uintptr_t)v_cache | (uintptr_t)o) & 15)
+        return fail(TA_ERR_INVALID_ARG, "%s: q, o and the caches must be 16-byte aligned", fn);
+    if (!workspace || workspace_bytes < p.bytes)
+        return fail(TA_ERR_WORKSPACE, "%s: workspace of %zu bytes, need %zu", fn,
+                    workspace ? workspace_bytes : (size_t)0, p.bytes);
+    if ((uintptr_t)workspace & 15)
+        return fail(TA_ERR_WORKSPACE, "%s: workspace must be 16-byte aligned", fn);
+    {
+        const int64_t rows = total_tokens * hq, cache = ((num_pages * hkv) << lp) * head_dim * 2;
+        const Span spans[] = {{o, rows * head_dim * (o_dtype == TA_OUT_F32 ? 4 : 2)},
+                              {lse, 4 * rows},
+                              {workspace, (int64_t)p.bytes},
+                              {q, rows * head_dim * 2},
+                              {k_cache, cache},
+                              {v_cache, cache},
+                              {kv_lens, 4LL * batch},
+                              {cu_q, 4LL * batch + 4},
+                              {block_table, 4LL * batch * table_width},
+                              {prefix_len > 0 ? prefix_pages : nullptr,
+                               4 * (((int64_t)prefix_len + page_size - 1) >> lp)},
+                              {slopes, 4LL * hq}};
+        if (spans_overlap(spans, 3, 11))
+            return fail(TA_ERR_INVALID_ARG, "%s: an output overlaps another argument", fn);
+    }
+    unsigned char *ws = static_cast<unsigned char *>(workspace);
+    auto part = [&](size_t off) { return reinterpret_cast<float *>(ws + off); };
+    PagedArgs a{};
+    a.q = static_cast<const uint16_t *>(q);
+    a.kc = static_cast<const uint16_t *>(k_cache);
+    a.vc = static_cast<const uint16_t *>(v_cache);
+    a.o = o;
+    a.lse = lse;
+    a.kv_lens = kv_lens;
+    a.cu_q = cu_q;
+    a.table = block_table;
+    a.prefix_pages = prefix_pages;
+    a.slot_o = part(p.own_slot_o);
+    a.slot_lse = part(p.own_slot_lse);
+    const bool prefix = prefix_len > 0;
+    a.row_o = prefix ? part(p.own_row_o) : nullptr;
+    a.row_lse = prefix ? part(p.own_row_lse) : nullptr;
+    a.meta = reinterpret_cast<int32_t *>(ws + p.meta);
+    a.score = score_args;
+    a.total_tokens = (int32_t)total_tokens;
+    a.batch = batch;
+    a.width = table_width;
+    a.hq = hq;
+    a.hkv = hkv;
+    a.group = (int32_t)group;
+    a.group_inv = 65536u / (uint32_t)group + 1;
+    a.page_log2 = lp;
+    a.num_pages = (int32_t)num_pages;
+    a.prefix_len = prefix_len;
+    a.slots = p.own_slots;
+    a.max_tiles = p.max_tiles;
+    a.o_f32 = o_dtype == TA_OUT_F32;
+    const int score = (softcap > 0.f ? kScoreCap : 0) | (slopes ? kScoreSlope : 0);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t err = hipSuccess;
+    if (prefix) {
+        PagedArgs b = a;
+        b.slot_o = part(p.pre_slot_o);
+        b.slot_lse = part(p.pre_slot_lse);
+        b.row_o = part(p.pre_row_o);
+        b.row_lse = part(p.pre_row_lse);
+        b.slots = p.pre_slots;
+        err = launch_pass<true>(head_dim, p.pre_rb, score, s, b);
+    }
+    if (err == hipSuccess)
+        err = launch_pass<false>(head_dim, p.own_rb, score, s, a);
+    if (err == hipSuccess) {
+        JoinArgs j{};
+        j.o = o;
+        j.lse = lse;
+        j.meta = a.meta;
+        j.slot_o = a.slot_o;
+        j.slot_lse = a.slot_lse;
+        j.tile_rows = 32 * p.own_rb;
+        j.row_o = a.row_o;
+        j.row_lse = a.row_lse;
+        j.pre_slot_o = part(p.pre_slot_o);
+        j.pre_slot_lse = part(p.pre_slot_lse);
+        j.pre_row_o = part(p.pre_row_o);
+        j.pre_row_lse = part(p.pre_row_lse);
+        j.prefix_len = prefix_len;
+        j.pre_rows = 32 * p.pre_rb;
+        j.pre_step = p.pre_rb == 4 ? PagedShape<128, 4>::STEP : PagedShape<128, 1>::STEP;
+        j.pre_slots = p.pre_slots;
+        j.slopes = slopes;
+        j.total_tokens = (int32_t)total_tokens;
+        j.hq = hq;
+        j.hkv = hkv;
+        j.group = (int32_t)group;
+        j.o_f32 = a.o_f32;
+        const dim3 grid((uint32_t)(p.max_tiles * hkv));
+        if (head_dim == 128)
+            hipLaunchKernelGGL(paged_join_kernel<128>, grid, dim3(kThreads), 0, s, j);
+        else
+            hipLaunchKernelGGL(paged_join_kernel<64>, grid, dim3(kThreads), 0, s, j);
+        err = hipGetLastError();
+    }
+    if (err != hipSuccess)
+        return fail(TA_ERR_HIP, "%s: %s", fn, hipGetErrorString(err));
+    return TA_OK;
+}

@@ -1,0 +1,518 @@
+// Prefill attention with modified scores (capped by a tanh, falling with the
+// distance) over the schedules of the forward passes: Triangle, dense causal
+// and block-sparse.
+//
+// A workgroup of four waves takes four row blocks (32 rows of one head) of a
+// schedule item, dealt out head first, over K/V tiles of 64 keys in LDS, two
+// workgroups to a CU.  The two waves of a SIMD then belong to different
+// workgroups, so that one's matrix instructions run beside the other's score
+// arithmetic without a barrier between them.  That arithmetic bounds the pass:
+// a capped score takes two exp2, a reciprocal and about seven plain operations,
+// some twenty issue slots of a lane, where the two products take eight.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "triattn_device.h"
+#include "triattn_internal.h"
+#include "triattn_rows.h"
+
+namespace triattn {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = 4;
+constexpr int kKeys = 64;           // keys of a step
+constexpr int kListSteps = 2048;    // steps of a list item held in LDS
+
+struct ScoredArgs {
+    const uint16_t *q, *k, *v;
+    void *o;
+    float *lse;
+    const int32_t *sched;
+    float *part_o, *part_lse;  // [partial rows, hq (, D)]
+    ScoreArgs score;
+    int64_t total_tokens, list_base, list_words;
+    int32_t kind, tile, hq, hkv, group, sink, window;
+    int32_t n_items, n_merges, n_partial_rows;
+    int32_t subtiles;  // workgroups per item and kv head
+    int32_t o_f32;
+};
+
+// The steps that one workgroup's rows can reach: two runs of 64-key steps, a
+// then b, or a list.
+struct Runs {
+    int a_lo, a_hi, b_lo, b_hi;
+};
+
+// Drops the steps in which none of the rows wr0 .. wr1 keeps a key: past the
+// last row, and for streaming rows between the sink and the first row's window.
+__device__ __forceinline__ Runs reach(Runs r, bool stream, int sink, int window, int wr0, int wr1)
+{
+    if (stream) {
+        const int band = max(wr0 - window + 1, 0) / kKeys;
+        const int sinks = (sink + kKeys - 1) / kKeys;
+        if (r.b_hi > r.b_lo) {
+            r.a_hi = max(min(r.a_hi, sinks), r.a_lo);
+            r.b_lo = min(max(r.b_lo, band), r.b_hi);
+        } else if (band > sinks || sink == 0) {
+            r.b_hi = r.a_hi;
+            r.b_lo = min(max(r.a_lo, band), r.a_hi);
+            r.a_hi = max(min(r.a_hi, sink == 0 ? r.a_lo : sinks), r.a_lo);
+        }
+    }
+    const int end = wr1 / kKeys + 1;
+    r.a_hi = max(min(r.a_hi, end), r.a_lo);
+    r.b_hi = max(min(r.b_hi, end), r.b_lo);
+    return r;
+}
+
+template <int D, int SCORE, bool LIST>
+__global__ __launch_bounds__(kThreads, 2) void scored_attn_kernel(ScoredArgs a)
+{
+    constexpr int ROW_BYTES = 2 * D;
+    constexpr int CHUNKS = D / 8;
+    constexpr int TILE_BYTES = kKeys * ROW_BYTES;
+    constexpr int STAGE_BYTES = 2 * TILE_BYTES;  // K tile, then V tile
+    constexpr int COPY_ROWS = 1024 / ROW_BYTES;  // keys of a 1 KB copy
+    constexpr int COPIES = TILE_BYTES / 1024 / kWaves;  // of a wave, for K and again for V
+    constexpr int D_BLOCKS = D / 32;
+
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE_BYTES];
+    __shared__ int32_t s_key[LIST ? kListSteps : 1];
+
+    const int32_t *sched = a.sched;
+    int bid = blockIdx.x;
+    const int g = bid % a.hkv;
+    bid /= a.hkv;
+    const int sub = bid % a.subtiles;
+    // a causal schedule lists the short rows first: the long ones start first
+    const int item = a.kind == TA_KIND_CAUSAL ? a.n_items - 1 - bid / a.subtiles
+                                              : bid / a.subtiles;
+    const int32_t *it = sched + kHdrWords + (int64_t)item * kItemWords;
+    const int64_t seq_off = it[I_SEQ_OFF];
+    const int32_t seq_len = it[I_SEQ_LEN];
+    const int32_t r0 = it[I_R0], r1 = it[I_R1];
+    const int32_t ka0 = it[I_KA0], ka1 = it[I_KA1], kb0 = it[I_KB0], kb1 = it[I_KB1];
+    const int32_t mode = it[I_MODE], part_base = it[I_PART_BASE];
+    const bool list = LIST && mode == kModeCausalList;
+    const int64_t sched_total =
+        (int64_t)(uint32_t)sched[H_TOTAL_LO] | ((int64_t)sched[H_TOTAL_HI] << 32);
+    const bool bad =
+        (sched[H_MAGIC] != TA_SCHEDULE_MAGIC) | (sched[H_VERSION] != TA_SCHEDULE_VERSION) |
+        (sched[H_KIND] != a.kind) | (sched_total != a.total_tokens) |
+        (sched[H_ITEMS] != a.n_items) | (sched[H_TILE] != a.tile) |
+        (LIST & (sched[H_WINDOW] != a.list_words)) | (seq_off < 0) | (seq_len < 0) |
+        (seq_off + seq_len > a.total_tokens) | (r0 < 0) | (r1 > seq_len) | (r0 >= r1) |
+        (r1 - r0 > a.tile) | (ka0 < 0) | (kb0 < 0) | (kb1 < kb0) |
+        (mode != kModeStreaming && mode != kModeCausal && !list) |
+        (list ? (ka1 < 0) | (kb1 != kb0) | ((int64_t)ka0 + ka1 > a.list_words) : ka1 < ka0) |
+        (part_base >= 0 && (int64_t)part_base + (r1 - r0) > a.n_partial_rows);
+    if (bad) {
+        rows_poison(a.o, a.o_f32, a.lse, a.total_tokens * a.hq, D);
+        // the item's own rows, as far as its words say where they are, are
+        // written by no other workgroup of this pass
+        const int64_t lo = min(max(seq_off + r0, (int64_t)0), a.total_tokens);
+        const int64_t hi = min(lo + a.tile, a.total_tokens);
+        for (int64_t i = lo * a.hq * D + threadIdx.x; i < hi * a.hq * D; i += kThreads) {
+            if (a.o_f32)
+                static_cast<float *>(a.o)[i] = __builtin_nanf("");
+            else
+                static_cast<uint16_t *>(a.o)[i] = 0x7fc0;
+        }
+        if (part_base >= 0 && part_base < a.n_partial_rows)
+            for (int64_t i = threadIdx.x;
+                 i < (int64_t)min(a.tile, a.n_partial_rows - part_base) * a.hq; i += kThreads)
+                a.part_lse[(int64_t)part_base * a.hq + i] = __builtin_nanf("");
+        return;
+    }
+    const int max_ktile = (seq_len - 1) / a.tile;
+    const bool stream = mode == kModeStreaming;
+
+    const int tid = threadIdx.x;
+    const int lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // row block b: head b % group, rows 32 (b / group) on
+    const int b0 = kWaves * sub;
+    const int wr0 = r0 + 32 * (b0 / a.group);
+    if (wr0 >= r1)
+        return;  // ragged q-tile: nothing for this workgroup
+    const int wr1 = min(r0 + 32 * ((b0 + kWaves - 1) / a.group + 1), r1) - 1;
+    const int head = g * a.group + (b0 + wave) % a.group;
+    const int row_base = r0 + 32 * ((b0 + wave) / a.group);
+    const bool active = row_base < r1;
+    const int row_hi = min(row_base + 31, r1 - 1);
+
+    RowBlock<D, 2, SCORE> rb;
+    rb.init(lane);
+    const int row = min(row_base + rb.col, r1 - 1);
+    rb.load_q(a.q + ((seq_off + row) * a.hq + head) * (int64_t)D);
+    rb.reset();
+    float slope = 0.f;
+    if constexpr ((SCORE & kScoreSlope) != 0)
+        slope = a.score.slopes[head] * kRowsLog2e;
+
+    // steps
+    const int tps = a.tile / kKeys;
+    Runs runs{ka0 * tps, ka1 * tps, kb0 * tps, kb1 * tps};
+    int n;
+    const int32_t *tiles = sched + a.list_base + (list ? ka0 : 0);
+    auto listed = [&](int s) TA_INLINE -> int {
+        return min(max(tiles[s / tps], 0), max_ktile) * a.tile + (s % tps) * kKeys;
+    };
+    if (list) {
+        n = ka1 * tps;
+        for (int s = tid; s < min(n, kListSteps); s += kThreads)
+            s_key[s] = listed(s);
+        __syncthreads();
+    } else {
+        runs = reach(runs, stream, a.sink, a.window, wr0, wr1);
+        n = runs.a_hi - runs.a_lo + runs.b_hi - runs.b_lo;
+    }
+    auto step_key = [&](int s) TA_INLINE -> int {
+        if (list)
+            return __builtin_amdgcn_readfirstlane(s < kListSteps ? s_key[s] : listed(s));
+        const int na = runs.a_hi - runs.a_lo;
+        return (s < na ? runs.a_lo + s : runs.b_lo + s - na) * kKeys;
+    };
+    if (list)  // listed tiles increase: only the last may pass the rows
+        while (n > 0 && step_key(n - 1) > wr1)
+            --n;
+
+    // copies: wave w takes 1 KB blocks w COPIES .. of the K and the V tile
+    const uint32_t smem_addr =
+        (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
+    const int dma_row = lane / CHUNKS, dma_chunk = lane % CHUNKS;
+    const uint32_t pitch = (uint32_t)(a.hkv * ROW_BYTES);
+    const uint16_t *kbase = a.k + (seq_off * a.hkv + g) * (int64_t)D;
+    const uint16_t *vbase = a.v + (seq_off * a.hkv + g) * (int64_t)D;
+    uint32_t koff[COPIES], voff[COPIES];
+#pragma unroll
+    for (int i = 0; i < COPIES; ++i) {
+        const int r = (wave * COPIES + i) * COPY_ROWS + dma_row;
+        koff[i] = (uint32_t)((dma_chunk ^ rows_kswz<D>(r)) << 4);
+        voff[i] = (uint32_t)((dma_chunk ^ rows_vswz<D>(r)) << 4);
+    }
+    auto copy_step = [&](int key0, int stage) TA_INLINE {
+        asm volatile("" ::: "memory");
+        // rows past the sequence repeat its last one; no row keeps them
+        const int first = min(key0, seq_len - 1);
+        const int lim = min(seq_len - 1 - first, kKeys - 1);
+        const uint16_t *kt = kbase + (int64_t)first * a.hkv * D;
+        const uint16_t *vt = vbase + (int64_t)first * a.hkv * D;
+        const uint32_t lds = smem_addr + stage * STAGE_BYTES + wave * COPIES * 1024;
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) {
+            const int r = min((wave * COPIES + i) * COPY_ROWS + dma_row, lim);
+            const uint32_t off = __umul24((uint32_t)r, pitch);
+            copy_to_lds16(kt, off + koff[i], lds + i * 1024);
+            copy_to_lds16(vt, off + voff[i], lds + TILE_BYTES + i * 1024);
+        }
+        asm volatile("" ::: "memory");
+    };
+
+    bool fresh = true;
+    if (n > 0)
+        copy_step(step_key(0), 0);
+    for (int i = 0; i < n; ++i) {
+        // this step's tile has landed for every wave, and every wave is done
+        // with the other stage
+        __builtin_amdgcn_sched_barrier(0);
+        rows_wait_copies<0>();
+        barrier_no_fence();
+        __builtin_amdgcn_sched_barrier(0);
+        const int key0 = step_key(i);
+        if (i + 1 < n)
+            copy_step(step_key(i + 1), (i + 1) & 1);
+        __builtin_amdgcn_sched_barrier(0);
+        // the wave's rows may keep nothing of a step that others need
+        const bool none = !active | (key0 > row_hi) |
+                          (stream & (key0 >= a.sink) &
+                           (row_base - (key0 + kKeys - 1) >= a.window));
+        if (!none) {
+            const unsigned char *kt = smem + (i & 1) * STAGE_BYTES;
+            f32x16 s[2];
+            bf16x8 p[2][2];
+            rb.products(kt, s);
+            rb.modify(s, a.score, slope, key0 - row);
+            const bool diagonal = key0 + kKeys - 1 > row_base;
+            const bool edge = stream && key0 + kKeys - 1 >= a.sink && row_hi - key0 >= a.window;
+            if (edge) {
+                const int lim = row - key0 - 8 * rb.half;
+                const int far = lim - a.window;             // kept: offset > far
+                const int sinks = a.sink - key0 - 8 * rb.half;  // or offset < sinks
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const int off = kb * 32 + rows_key_of_reg(v, 0);
+                        s[kb][v] = (off <= lim) & ((off > far) | (off < sinks)) ? s[kb][v]
+                                                                              : -INFINITY;
+                    }
+            } else if (diagonal) {
+                rb.mask_above(s, row - key0);
+            }
+            rb.softmax(s, a.score, p, fresh);
+            fresh = false;
+            if (diagonal | edge)
+                rb.accumulate_masked(kt + TILE_BYTES, p, lane);
+            else
+                rb.accumulate(kt + TILE_BYTES, p);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+
+    if (!active || row_base + rb.col >= r1)
+        return;
+    float inv, lse;
+    rb.finish(inv, lse);
+    const int64_t tok = seq_off + row;
+    const int64_t prow = (int64_t)part_base + (row - r0);
+#pragma unroll
+    for (int b = 0; b < D_BLOCKS; ++b)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            f32x4r x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                x[e] = rb.oacc[b][4 * c + e] * inv;
+            const int d = 32 * b + 8 * c + 4 * rb.half;
+            if (part_base >= 0)
+                *reinterpret_cast<f32x4r *>(a.part_o + (prow * a.hq + head) * D + d) = x;
+            else if (a.o_f32)
+                *reinterpret_cast<f32x4r *>(static_cast<float *>(a.o) +
+                                            (tok * a.hq + head) * D + d) = x;
+            else
+                *reinterpret_cast<bf16x4r *>(static_cast<__bf16 *>(a.o) +
+                                             (tok * a.hq + head) * D + d) =
+                    __builtin_convertvector(x, bf16x4r);
+        }
+    if (rb.half == 0) {
+        if (part_base >= 0)
+            a.part_lse[prow * a.hq + head] = lse;
+        else if (a.lse)
+            a.lse[(int64_t)head * a.total_tokens + tok] = lse;
+    }
+}
+
+// Joins the partials of the schedule's split q-tiles, a wave to a (row, head):
+// O = sum_c w_c O_c / sum_c w_c with w_c = exp(LSE_c - max_c LSE_c).
+template <int D>
+__global__ __launch_bounds__(kThreads) void scored_join_kernel(ScoredArgs a)
+{
+    constexpr int PER = D / 64;
+    const int32_t *sched = a.sched;
+    const int blocks = (a.tile * a.hq + kWaves - 1) / kWaves;  // workgroups of a merge item
+    const int m = blockIdx.x / blocks;
+    const int32_t *x = sched + kHdrWords + (int64_t)a.n_items * kItemWords +
+                       (int64_t)m * kMergeWords;
+    const int64_t seq_off = x[M_SEQ_OFF];
+    const int32_t r0 = x[M_R0], r1 = x[M_R1], ns = x[M_SPLITS], pb = x[M_PART_BASE];
+    const int rows = r1 - r0;
+    const int64_t sched_total =
+        (int64_t)(uint32_t)sched[H_TOTAL_LO] | ((int64_t)sched[H_TOTAL_HI] << 32);
+    if ((sched[H_MAGIC] != TA_SCHEDULE_MAGIC) | (sched[H_VERSION] != TA_SCHEDULE_VERSION) |
+        (sched[H_KIND] != a.kind) | (sched_total != a.total_tokens) |
+        (sched[H_ITEMS] != a.n_items) | (sched[H_TILE] != a.tile) | (rows < 1) |
+        (rows > a.tile) | (ns < 1) | (pb < 0) |
+        ((int64_t)pb + (int64_t)ns * rows > a.n_partial_rows) | (seq_off < 0) | (r0 < 0) |
+        (seq_off + r1 > a.total_tokens)) {
+        rows_poison(a.o, a.o_f32, a.lse, a.total_tokens * a.hq, D);
+        return;
+    }
+    const int lane = threadIdx.x & 63;
+    const int w = (int)(blockIdx.x % blocks) * kWaves + (threadIdx.x >> 6);
+    const int head = w % a.hq, r = w / a.hq;
+    if (r >= rows)
+        return;
+    auto at = [&](int c) TA_INLINE -> int64_t {
+        return ((int64_t)pb + (int64_t)c * rows + r) * a.hq + head;
+    };
+    float mx = -INFINITY;
+    for (int c = lane; c < ns; c += 64)
+        mx = fmaxf(mx, a.part_lse[at(c)]);
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1)
+        mx = fmaxf(mx, __shfl_xor(mx, o));
+    const float m_use = mx == -INFINITY ? 0.f : mx;
+    float acc[PER] = {}, den = 0.f;
+    constexpr int UNROLL = 8;
+    for (int c = 0; c < ns; c += UNROLL) {
+        float y[UNROLL][PER], l[UNROLL];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int64_t p = at(min(c + u, ns - 1));
+            l[u] = a.part_lse[p];
+#pragma unroll
+            for (int e = 0; e < PER; ++e)
+                y[u][e] = a.part_o[p * D + PER * lane + e];
+        }
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u)
+            if (c + u < ns) {
+                const float f = __expf(l[u] - m_use);
+                den += f;
+#pragma unroll
+                for (int e = 0; e < PER; ++e)
+                    acc[e] += f * y[u][e];
+            }
+    }
+    const float inv = den == 0.f ? 0.f : 1.f / den;
+    const int64_t tok = seq_off + r0 + r;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        const int64_t i = (tok * a.hq + head) * D + PER * lane + e;
+        if (a.o_f32)
+            static_cast<float *>(a.o)[i] = acc[e] * inv;
+        else
+            static_cast<__bf16 *>(a.o)[i] = (__bf16)(acc[e] * inv);
+    }
+    if (a.lse && lane == 0)
+        a.lse[(int64_t)head * a.total_tokens + tok] =
+            den == 0.f ? -INFINITY : m_use + __logf(den);
+}
+
+template <int D, bool LIST>
+void launch_scored(int score, dim3 grid, hipStream_t s, const ScoredArgs &a)
+{
+    switch (score) {
+    case 1: hipLaunchKernelGGL((scored_attn_kernel<D, 1, LIST>), grid, dim3(kThreads), 0, s, a); break;
+    case 2: hipLaunchKernelGGL((scored_attn_kernel<D, 2, LIST>), grid, dim3(kThreads), 0, s, a); break;
+    default: hipLaunchKernelGGL((scored_attn_kernel<D, 3, LIST>), grid, dim3(kThreads), 0, s, a); break;
+    }
+}
+
+}  // namespace
+}  // namespace triattn
+
+using namespace triattn;
+
+extern "C" ta_status scored_attn_fwd(const void *q, const void *k, const void *v, void *o,
+                                     int32_t o_dtype, float *lse, const int32_t *sched_dev,
+                                     const ta_schedule_info *info, int64_t total_tokens,
+                                     int32_t hq, int32_t hkv, int32_t head_dim,
+                                     float softmax_scale, float softcap, const float *slopes,
+                                     void *workspace, size_t workspace_bytes, void *stream)
+{
+    clear_error();
+    const char *fn = "scored_attn_fwd";
+    if (!info)
+        return fail(TA_ERR_INVALID_ARG, "%s: info is NULL", fn);
+    if (info->version != TA_SCHEDULE_VERSION)
+        return fail(TA_ERR_SCHEDULE_MISMATCH, "%s: schedule version %d != %d", fn, info->version,
+                    TA_SCHEDULE_VERSION);
+    if (info->kind != TA_KIND_TRIANGLE && info->kind != TA_KIND_CAUSAL &&
+        info->kind != TA_KIND_BLOCKSPARSE)
+        return fail(TA_ERR_SCHEDULE_MISMATCH, "%s: schedule kind %d", fn, info->kind);
+    if (total_tokens < 0)
+        return fail(TA_ERR_INVALID_ARG, "%s: total_tokens < 0", fn);
+    if (info->total_tokens != total_tokens)
+        return fail(TA_ERR_SCHEDULE_MISMATCH, "%s: schedule built for %lld tokens, call has %lld",
+                    fn, (long long)info->total_tokens, (long long)total_tokens);
+    if (hq <= 0 || hkv <= 0)
+        return fail(TA_ERR_INVALID_ARG, "%s: hq and hkv must be positive", fn);
+    if (hq % hkv != 0)
+        return fail(TA_ERR_INVALID_ARG, "%s: hq %d not a multiple of hkv %d", fn, hq, hkv);
+    if (hq / hkv > 8)
+        return fail(TA_ERR_UNSUPPORTED, "%s: GQA group %d > 8", fn, hq / hkv);
+    if (head_dim != 64 && head_dim != 128)
+        return fail(TA_ERR_UNSUPPORTED, "%s: head_dim %d not in {64, 128}", fn, head_dim);
+    if (info->tile != 64 && info->tile != 128)
+        return fail(TA_ERR_UNSUPPORTED, "%s: tile %d not in {64, 128}", fn, info->tile);
+    if (o_dtype != TA_OUT_BF16 && o_dtype != TA_OUT_F32)
+        return fail(TA_ERR_INVALID_ARG, "%s: bad o_dtype %d", fn, o_dtype);
+    if (!std::isfinite(softmax_scale) || !(softmax_scale > 0.f))
+        return fail(TA_ERR_INVALID_ARG, "%s: softmax_scale must be finite and > 0", fn);
+    if (!std::isfinite(softcap) || softcap < 0.f)
+        return fail(TA_ERR_INVALID_ARG, "%s: softcap must be finite and >= 0", fn);
+    if (softcap > kRowsMaxCap)
+        return fail(TA_ERR_UNSUPPORTED, "%s: softcap %g > %g", fn, softcap, kRowsMaxCap);
+    if (softcap == 0.f && !slopes)
+        return fail(TA_ERR_INVALID_ARG, "%s: neither a softcap nor slopes (plain scores are the "
+                    "other passes')", fn);
+    ScoredArgs a{};
+    if (!rows_score_args(a.score, softmax_scale, softcap, slopes))
+        return fail(TA_ERR_INVALID_ARG, "%s: softcap too small for the scale", fn);
+    const int64_t base = kHdrWords + (int64_t)info->n_items * kItemWords +
+                         (int64_t)info->n_merge_items * kMergeWords;
+    const int64_t lists = info->kind == TA_KIND_BLOCKSPARSE ? info->window : 0;
+    if (info->n_items < 0 || info->n_merge_items < 0 || info->n_partial_rows < 0 || lists < 0 ||
+        info->words != base + lists)
+        return fail(TA_ERR_SCHEDULE_MISMATCH, "%s: corrupt schedule info", fn);
+    if (2LL * hq * head_dim >= (1LL << 24))
+        return fail(TA_ERR_UNSUPPORTED, "%s: hq * head_dim too large", fn);
+    const int64_t group = hq / hkv;
+    const int64_t subtiles = (group * (info->tile / 32) + kWaves - 1) / kWaves;
+    const int64_t wgs = info->n_items * subtiles * hkv;
+    const int64_t join_wgs =
+        info->n_merge_items * (((int64_t)info->tile * hq + kWaves - 1) / kWaves);
+    if (wgs > INT32_MAX || join_wgs > INT32_MAX)
+        return fail(TA_ERR_UNSUPPORTED, "%s: grid too large", fn);
+    if (info->n_items == 0)
+        return TA_OK;
+    if (!q || !k || !v || !o || !sched_dev)
+        return fail(TA_ERR_INVALID_ARG, "%s: NULL q, k, v, o or schedule", fn);
+    if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)o) & 15)
+        return fail(TA_ERR_INVALID_ARG, "%s: q, k, v and o must be 16-byte aligned", fn);
+    const size_t need = ta_workspace_bytes(info, hq, head_dim);
+    if (need > 0 && (!workspace || workspace_bytes < need))
+        return fail(TA_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, got %zu", fn, need,
+                    workspace ? workspace_bytes : (size_t)0);
+    if ((uintptr_t)workspace & 15)
+        return fail(TA_ERR_INVALID_ARG, "%s: workspace must be 16-byte aligned", fn);
+    a.q = static_cast<const uint16_t *>(q);
+    a.k = static_cast<const uint16_t *>(k);
+    a.v = static_cast<const uint16_t *>(v);
+    a.o = o;
+    a.lse = lse;
+    a.sched = sched_dev;
+    if (need > 0) {
+        const size_t rows = (size_t)info->n_partial_rows * (size_t)hq;
+        a.part_o = static_cast<float *>(workspace);
+        a.part_lse = reinterpret_cast<float *>(
+            static_cast<char *>(workspace) +
+            ((rows * (size_t)head_dim * 4 + 255) & ~(size_t)255));
+    }
+    a.total_tokens = total_tokens;
+    a.list_base = base;
+    a.list_words = lists;
+    a.kind = info->kind;
+    a.tile = info->tile;
+    a.hq = hq;
+    a.hkv = hkv;
+    a.group = (int32_t)group;
+    a.sink = info->sink;
+    a.window = info->window;
+    a.n_items = info->n_items;
+    a.n_merges = info->n_merge_items;
+    a.n_partial_rows = need > 0 ? info->n_partial_rows : 0;
+    a.subtiles = (int32_t)subtiles;
+    a.o_f32 = o_dtype == TA_OUT_F32;
+    const int score = (softcap > 0.f ? kScoreCap : 0) | (slopes ? kScoreSlope : 0);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const dim3 grid((uint32_t)wgs);
+    const bool list = info->kind == TA_KIND_BLOCKSPARSE;
+    if (head_dim == 128 && list)
+        launch_scored<128, true>(score, grid, s, a);
+    else if (head_dim == 128)
+        launch_scored<128, false>(score, grid, s, a);
+    else if (list)
+        launch_scored<64, true>(score, grid, s, a);
+    else
+        launch_scored<64, false>(score, grid, s, a);
+    hipError_t err = hipGetLastError();
+    if (err == hipSuccess && join_wgs > 0) {
+        if (head_dim == 128)
+            hipLaunchKernelGGL(scored_join_kernel<128>, dim3((uint32_t)join_wgs), dim3(kThreads),
+                               0, s, a);
+        else
+            hipLaunchKernelGGL(scored_join_kernel<64>, dim3((uint32_t)join_wgs), dim3(kThreads), 0,
+                               s, a);
+        err = hipGetLastError();
+    }
+    if (err != hipSuccess)
+        return fail(TA_ERR_HIP, "%s: %s", fn, hipGetErrorString(err));
+    return TA_OK;
+}

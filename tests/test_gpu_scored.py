@@ -1,0 +1,205 @@
+"""GPU tests of prefill attention with modified scores, against 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2507_21526_amd import binding as B
+from paper_2507_21526_amd.inputs import draw_qkv
+from tests.serving_ref import attend, check, geometric_slopes, scored_keep
+
+pytestmark = pytest.mark.gpu
+
+
+def _lists(cu, tile, seed):
+    """Per-q-tile lists of every sequence, some of them empty."""
+    rng = np.random.default_rng(seed)
+    ptr, idx, per = [0], [], []
+    for a, b in zip(cu, cu[1:]):
+        mine = []
+        for t in range(-(-(b - a) // tile)):
+            tiles = [] if t % 5 == 3 else sorted(
+                set(np.flatnonzero(rng.random(t + 1) < 0.5).tolist()) | ({t} if t % 2 else set()))
+            mine.append(tiles)
+            idx.extend(tiles)
+            ptr.append(len(idx))
+        per.append(mine)
+    return (ptr, idx), per
+
+
+def _run(kind, cu, hq, hkv, d, tile, S, W, L, cap, slopes, dtype, splits=0, seed=1, blocks=None,
+         qkv=None):
+    q, k, v = qkv or (t.cuda() for t in draw_qkv(cu, hq, hkv, d, seed, key0_boost=8.0))
+    plan = B.Plan(kind, cu, S, W, L, tile, hq, d, splits, blocks=blocks)
+    if plan.workspace is not None:
+        plan.workspace.fill_(0xff)
+    o = torch.full(q.shape, math.nan, dtype=dtype, device="cuda")
+    lse = torch.full((hq, cu[-1]), math.nan, device="cuda")
+    plan.run(q, k, v, o, lse, softcap=cap, slopes=slopes)
+    torch.cuda.synchronize()
+    return q, k, v, o, lse, plan
+
+
+def _verify(kind, cu, q, k, v, o, lse, tile, S, W, L, cap, slopes, label, lists=None, rows=None):
+    for i, (a, b) in enumerate(zip(cu, cu[1:])):
+        n = b - a
+        if n == 0:
+            continue
+        keep = torch.from_numpy(scored_keep(kind, n, S, W, L, tile,
+                                            lists[i] if lists else None)).cuda()
+        pick = torch.arange(n, device="cuda") if rows is None else rows(n)
+        dist = pick[:, None] - torch.arange(n, device="cuda")
+        ref = attend(q[a:b][pick], k[a:b], v[a:b], keep[pick], dist, q.shape[2] ** -0.5, cap,
+                     slopes)
+        check(o[a:b][pick], lse[:, a:b].t()[pick], ref, o.dtype, f"{label} sequence {i}")
+
+
+CASES = [
+    # kind, cu, hq, hkv, d, tile, S, W, L, splits
+    ("causal", [0, 1], 1, 1, 64, 64, 0, 1, 0, 0),
+    ("causal", [0, 63, 64, 64, 193, 450], 4, 1, 128, 128, 0, 1, 0, 0),
+    ("causal", [0, 333], 7, 1, 64, 64, 0, 1, 0, 0),
+    ("causal", [0, 700], 10, 2, 128, 64, 0, 1, 0, 0),
+    ("triangle", [0, 300], 4, 1, 64, 64, 8, 64, 20, 0),
+    ("triangle", [0, 900, 901, 1000], 8, 1, 128, 128, 8, 200, 40, 0),
+    ("triangle", [0, 1300], 6, 2, 128, 128, 128, 256, 128, 7),
+    ("triangle", [0, 800], 3, 1, 64, 128, 0, 130, 0, 0),       # no sink, no Last rows
+    ("triangle", [0, 777], 5, 1, 128, 64, 70, 1, 3, 0),        # a window of one key
+    ("triangle", [0, 640], 16, 2, 64, 64, 100, 90, 640, 5),    # every row is a Last row
+    ("blocksparse", [0, 700, 1100], 4, 2, 128, 64, 0, 1, 0, 2),
+    ("blocksparse", [0, 900], 8, 1, 64, 128, 0, 1, 0, 0),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: f"{c[0]}-{c[1][-1]}-{c[2]}-{c[3]}-{c[4]}-"
+                         f"{c[5]}-{c[6]}-{c[7]}-{c[8]}")
+@pytest.mark.parametrize("score", ["cap", "slopes", "both"])
+def test_parity(case, score):
+    kind, cu, hq, hkv, d, tile, S, W, L, splits = case
+    cap = 11.0 if score != "slopes" else None
+    sl = geometric_slopes(hq) if score != "cap" else None
+    dtype = torch.float32 if score == "slopes" else torch.bfloat16
+    blocks, per = _lists(cu, tile, 3) if kind == "blocksparse" else (None, None)
+    q, k, v, o, lse, plan = _run(kind, cu, hq, hkv, d, tile, S, W, L, cap, sl, dtype, splits,
+                                 blocks=blocks)
+    _verify(kind, cu, q, k, v, o, lse, tile, S, W, L, cap, sl, f"{case} {score}", per)
+
+
+def test_long_triangle_and_causal_rows():
+    """Sampled rows of long sequences: split Last rows, far distances."""
+    def rows(n):
+        g = torch.Generator().manual_seed(n)
+        r = torch.cat([torch.randint(0, n, (40,), generator=g), torch.tensor(
+            [0, 127, 128, n - 129, n - 128, n - 1])])
+        return r.unique().cuda()
+
+    for kind, n, cap, slopes in (("triangle", 9000, None, geometric_slopes(8) / 16),
+                                 ("causal", 5000, 30.0, None)):
+        cu = [0, n]
+        out = _run(kind, cu, 8, 2, 128, 128, 128, 1024, 128, cap, slopes, torch.float32)
+        _verify(kind, cu, *out[:5], 128, 128, 1024, 128, cap, slopes, f"long {kind}", rows=rows)
+
+
+def test_a_wide_cap_and_no_slope_are_the_plain_pass():
+    """Slopes of zero change nothing but the order of roundings."""
+    cu = [0, 500, 800]
+    q, k, v, o, lse, plan = _run("triangle", cu, 8, 2, 128, 128, 8, 100, 30, None,
+                                 torch.zeros(8, device="cuda"), torch.float32)
+    po, pl = torch.empty_like(o), torch.empty_like(lse)
+    plan.run(q, k, v, po, pl)
+    torch.cuda.synchronize()
+    assert float((o - po).norm() / po.norm()) < 2 * 2.0 ** -8  # each rounds P to bf16
+    assert float((lse - pl).abs().max()) < 2 * 2.0 ** -13
+
+
+@pytest.mark.parametrize("cap", [0.5, 50.0, 1000.0])
+def test_cap_holds_far_scores(cap):
+    """Scores far past the cap, both signs: keys of 100 times the norm."""
+    cu = [0, 200]
+    q, k, v = (t.cuda() for t in draw_qkv(cu, 4, 1, 64, 9))
+    k[::3] *= 100
+    q, k, v, o, lse, _ = _run("causal", cu, 4, 1, 64, 64, 0, 1, 0, cap, None, torch.float32,
+                              qkv=(q, k, v))
+    dist = torch.arange(200, device="cuda")[:, None] - torch.arange(200, device="cuda")
+    ro, rl, absw = attend(q, k, v, dist >= 0, dist, 0.125, cap)
+    # products of up to 100 * 30: an error e of a product is damped by the
+    # tanh's slope, at most e; 3000 * 2^-24 * 16 = 2.9e-3, and 2^-22 cap
+    e = 2.9e-3 + 2.0 ** -22 * cap
+    assert bool(((o.double() - ro).abs() <= (2.0 ** -8 + 2 * e) * absw + 1e-5).all())
+    assert bool(((lse.t().double() - rl).abs() <= e + 2.0 ** -22 * rl.abs()).all())
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("kind,d,W", [("causal", 128, 1), ("triangle", 64, 70)])
+def test_values_of_masked_keys(bad, kind, d, W):
+    """An infinite or NaN value reaches the rows that keep its key only, also
+    within a step of keys."""
+    cu = [0, 300]
+    q, k, v = (t.cuda() for t in draw_qkv(cu, 4, 1, d, 10))
+    for j in (100, 150, 299):
+        v[j, 0, 5] = bad
+    out = _run(kind, cu, 4, 1, d, 64, 0, W, 0, 20.0, None, torch.float32, qkv=(q, k, v))
+    _verify(kind, cu, *out[:5], 64, 0, W, 0, 20.0, None, f"{kind} {bad}")
+
+
+def test_infinite_keys_at_masked_places():
+    """A NaN key that a row does not keep changes nothing for it."""
+    cu = [0, 200]
+    q, k, v = (t.cuda() for t in draw_qkv(cu, 4, 1, 128, 12))
+    sl = geometric_slopes(4)
+    want = _run("causal", cu, 4, 1, 128, 64, 0, 1, 0, 15.0, sl, torch.float32, qkv=(q, k, v))[3]
+    k2 = k.clone()
+    k2[150:] = math.nan
+    got = _run("causal", cu, 4, 1, 128, 64, 0, 1, 0, 15.0, sl, torch.float32, qkv=(q, k2, v))[3]
+    assert torch.equal(got[:150], want[:150])
+    assert bool(torch.isnan(got[150:]).all())
+
+
+@pytest.mark.parametrize("kind", ["triangle", "causal", "blocksparse"])
+def test_a_schedule_that_does_not_fit_shows(kind):
+    cu = [0, 600]
+    blocks, _ = _lists(cu, 64, 3)
+    q, k, v = (t.cuda() for t in draw_qkv(cu, 4, 1, 64, 2))
+    plan = B.Plan(kind, cu, 8, 100, 64, 64, 4, 64, 2, blocks=blocks)
+    o = torch.zeros(q.shape, device="cuda")
+    lse = torch.zeros(4, 600, device="cuda")
+    for word, value in ((0, 1), (2, 7), (3, 128), (11, 5)):  # magic, kind, tile, items
+        keep = int(plan.sched[word])
+        plan.sched[word] = value
+        plan.run(q, k, v, o.zero_(), lse.zero_(), softcap=5.0)
+        assert bool(torch.isnan(o).all()) and bool(torch.isnan(lse).all()), word
+        plan.sched[word] = keep
+    item = 16 + 12 * (plan.info.n_items - 1)  # the last item: its rows are its own
+    r0, r1 = int(plan.sched[item + 2]), int(plan.sched[item + 3])
+    part = int(plan.sched[item + 9])
+    plan.sched[item + 8] = 9  # no such mode
+    plan.run(q, k, v, o.zero_(), lse.zero_(), softcap=5.0)
+    assert part >= 0 or bool(torch.isnan(o[r0:r1]).all())
+
+
+def test_empty_batches_and_streams():
+    for cu in ([0], [0, 0, 0]):
+        q = torch.zeros(0, 4, 64, dtype=torch.bfloat16, device="cuda")
+        k = torch.zeros(0, 1, 64, dtype=torch.bfloat16, device="cuda")
+        B.Plan("causal", cu, 0, 1, 0, 64, 4, 64).run(q, k, k.clone(), torch.empty_like(q),
+                                                     softcap=5.0)
+    cu = [0, 700]
+    sl = geometric_slopes(4)
+    q, k, v, o, lse, plan = _run("triangle", cu, 4, 1, 64, 64, 8, 100, 64, 9.0, sl,
+                                 torch.bfloat16, 3)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    o2 = torch.zeros_like(o)
+    plan.run(q, k, v, o2, stream=side, softcap=9.0, slopes=sl)
+    side.synchronize()
+    assert torch.equal(o, o2)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        plan.run(q, k, v, o2, softcap=9.0, slopes=sl)
+    for _ in range(3):
+        o2.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, o2)
+        plan.run(q, k, v, torch.empty_like(o), softcap=9.0)
