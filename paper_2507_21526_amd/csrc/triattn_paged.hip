@@ -320,7 +320,6 @@ __global__ __launch_bounds__(kThreads, (PagedShape<D, RB>::WGS_PER_CU)) void pag
         const int head = g * a.group + rho - tq * a.group;
         const int tok = rt.q0 + tq;
         rb.load_q(a.q + ((int64_t)tok * a.hq + head) * D);
-        rb.reset();
         float slope = 0.f;
         if constexpr ((SCORE & kScoreSlope) != 0)
             slope = a.score.slopes[head] * kRowsLog2e;
@@ -330,17 +329,19 @@ __global__ __launch_bounds__(kThreads, (PagedShape<D, RB>::WGS_PER_CU)) void pag
         const int first_last =
             PREFIX ? a.prefix_len - 1
                    : rt.pos0 + div_group(rt.rho0 + min(block0, rt.rows - 1));
-        const int wave_last =
-            PREFIX ? a.prefix_len - 1
-                   : rt.pos0 + div_group(rt.rho0 + min(block0 + 31, rt.rows - 1));
         // distances in the prefix pass are taken from the prefix's end: the
         // join adds what each row is past it
         const int dist_row = PREFIX ? a.prefix_len : last;
         const int32_t *pages = PREFIX ? a.prefix_pages : a.table + (int64_t)rt.req * a.width;
-        bool fresh = true;
         if (tid == 0)
             s_bad = 0;
-
+        // One pass over the piece's steps; with `careful`, infinite or NaN
+        // values in masked steps are kept from the rows that do not keep their
+        // keys.  Returns whether a masked step holds any.
+        auto pass = [&](auto careful) TA_INLINE -> bool {
+        constexpr bool CAREFUL = decltype(careful)::value;
+        bool fresh = true, odd = false;
+        rb.reset();
         const int seg_steps = (((kPageEntries - 1) << a.page_log2) / S::STEP);
         for (int seg0 = step0; seg0 < step1; seg0 += seg_steps) {
             const int seg1 = min(step1, seg0 + seg_steps);
@@ -391,22 +392,28 @@ __global__ __launch_bounds__(kThreads, (PagedShape<D, RB>::WGS_PER_CU)) void pag
                 }
                 asm volatile("" ::: "memory");
             };
-            auto compute_tile = [&](int key0, int stage) TA_INLINE {
-                const unsigned char *kt = smem + wave_lds + stage * S::STAGE_BYTES;
+            auto compute_tile = [&](int key0, auto stage) TA_INLINE {
+                const unsigned char *kt =
+                    smem + wave_lds + decltype(stage)::value * S::STAGE_BYTES;
                 f32x16 s[S::NKB];
                 bf16x8 p[S::NKB][2];
                 rb.products(kt, s);
-                rb.modify(s, a.score, slope, key0 - dist_row);
+                rb.modify(s, a.score);
                 const bool masked = key0 + S::TK - 1 > first_last;
-                if (masked)
+                if (__builtin_expect(masked, 0)) {
+                    asm volatile("");  // a branch: most steps have no mask
+                    odd |= rb.odd_values(kt + S::TILE_BYTES, lane);
                     rb.mask_above(s, last - key0);
-                rb.softmax(s, a.score, p, fresh);
+                }
+                rb.softmax(s, a.score, slope, key0 - dist_row, p, fresh);
                 fresh = false;
-                if (masked)
-                    rb.accumulate_masked(kt + S::TILE_BYTES, p, lane);
+                if (CAREFUL && masked)
+                    rb.accumulate_by_key(kt + S::TILE_BYTES, p);
                 else
                     rb.accumulate(kt + S::TILE_BYTES, p);
             };
+            using Stage0 = std::integral_constant<int, 0>;
+            using Stage1 = std::integral_constant<int, 1>;
             if constexpr (RB == 1) {
                 // tiles of this wave: key0 = step STEP + wave TK, two stages
                 const int base = seg0 * S::STEP + wave * S::TK;
@@ -415,26 +422,33 @@ __global__ __launch_bounds__(kThreads, (PagedShape<D, RB>::WGS_PER_CU)) void pag
                     copy_tile(base, 0);
                 if (n > 1)
                     copy_tile(base + S::STEP, 1);
-                for (int i = 0; i < n; ++i) {
+                auto step = [&](int i, auto stage) TA_INLINE {
                     if (i + 1 < n)
                         rows_wait_copies<2 * COPIES>();
                     else
                         rows_wait_copies<0>();
                     __builtin_amdgcn_sched_barrier(0);
-                    compute_tile(base + i * S::STEP, i & 1);
+                    compute_tile(base + i * S::STEP, stage);
                     __builtin_amdgcn_sched_barrier(0);
                     if (i + 2 < n) {
                         // every read of the stage has returned before it is
                         // written again
                         __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
-                        copy_tile(base + (i + 2) * S::STEP, i & 1);
+                        copy_tile(base + (i + 2) * S::STEP, stage);
                         __builtin_amdgcn_sched_barrier(0);
                     }
+                };
+                int i = 0;
+                for (; i + 1 < n; i += 2) {
+                    step(i, Stage0{});
+                    step(i + 1, Stage1{});
                 }
+                if (i < n)
+                    step(i, Stage0{});
             } else {
                 const int n = (key_end - seg0 * S::STEP + S::STEP - 1) / S::STEP;
                 copy_tile(seg0 * S::STEP, 0);
-                for (int i = 0; i < n; ++i) {
+                auto step = [&](int i, auto stage) TA_INLINE {
                     // this step's tile has landed for every wave, and every
                     // wave is done with the other stage
                     __builtin_amdgcn_sched_barrier(0);
@@ -443,14 +457,24 @@ __global__ __launch_bounds__(kThreads, (PagedShape<D, RB>::WGS_PER_CU)) void pag
                     __builtin_amdgcn_sched_barrier(0);
                     const int key0 = (seg0 + i) * S::STEP;
                     if (i + 1 < n)
-                        copy_tile(key0 + S::STEP, (i + 1) & 1);
+                        copy_tile(key0 + S::STEP, 1 - decltype(stage)::value);
                     __builtin_amdgcn_sched_barrier(0);
-                    if (block0 < rt.rows && key0 <= wave_last)
-                        compute_tile(key0, i & 1);
+                    compute_tile(key0, stage);
                     __builtin_amdgcn_sched_barrier(0);
+                };
+                int i = 0;
+                for (; i + 1 < n; i += 2) {
+                    step(i, Stage0{});
+                    step(i + 1, Stage1{});
                 }
+                if (i < n)
+                    step(i, Stage0{});
             }
         }
+        return odd;
+        };
+        if (__builtin_expect(__syncthreads_or(pass(std::false_type{})), 0))
+            pass(std::true_type{});
 
         // Where the rows go.
         const bool to_o = whole && !a.row_o;

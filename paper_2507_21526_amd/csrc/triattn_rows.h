@@ -31,7 +31,6 @@
 
 namespace triattn {
 
-typedef float f32x8r __attribute__((ext_vector_type(8)));
 typedef float f32x4r __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x4r __attribute__((ext_vector_type(4)));
 typedef short s16x4r __attribute__((ext_vector_type(4)));
@@ -201,35 +200,26 @@ struct RowBlock {
             }
     }
 
-    // Products to scores in the log2 domain (left as products where the score
-    // is plain: the scale then enters the exponent).  dist0 = first key of
-    // the tile - this lane's row.
-    __device__ __forceinline__ void modify(f32x16 (&s)[NKB], const ScoreArgs &a, float slope_log2,
-                                           int dist0) const
+    // Scores are held as values x of which the log2-domain score is
+    // x factor + offset + slope (key - row): the products themselves, or for a
+    // capped score -1 / (1 + e^(2 x / cap)), the factor then 2 cap and the offset
+    // cap.  Factor, offset, bias and reference enter the exponent in one fused
+    // multiply-add (two where there are slopes), and a key that drops out is
+    // -inf either way.
+    __device__ __forceinline__ void modify(f32x16 (&s)[NKB], const ScoreArgs &a) const
     {
-        if constexpr (SCORE != 0) {
-            const float d0 = (float)(dist0 + 8 * half);
+        if constexpr ((SCORE & kScoreCap) != 0) {
 #pragma unroll
             for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    float x = s[kb][v];
-                    if constexpr ((SCORE & kScoreCap) != 0) {
-                        const float e = __builtin_amdgcn_exp2f(x * a.cap_in);
-                        x = __builtin_fmaf(-2.f * a.cap_out, __builtin_amdgcn_rcpf(e + 1.f),
-                                           a.cap_out);
-                    }
-                    if constexpr ((SCORE & kScoreSlope) != 0) {
-                        // distances below 2^24 are exact in fp32
-                        const float dist = d0 + (float)(kb * 32 + rows_key_of_reg(v, 0));
-                        if constexpr ((SCORE & kScoreCap) != 0)
-                            x = __builtin_fmaf(slope_log2, dist, x);
-                        else
-                            x = __builtin_fmaf(x, a.scale_log2, slope_log2 * dist);
-                    }
-                    s[kb][v] = x;
-                }
+                for (int v = 0; v < 16; ++v)
+                    s[kb][v] = __builtin_amdgcn_rcpf(
+                        -1.f - __builtin_amdgcn_exp2f(s[kb][v] * a.cap_in));
         }
+    }
+    __device__ __forceinline__ static float factor(const ScoreArgs &a)
+    {
+        return (SCORE & kScoreCap) != 0 ? 2.f * a.cap_out : a.scale_log2;
     }
 
     // Keys whose offset in the tile is above lim (this lane's row) drop out.
@@ -248,41 +238,57 @@ struct RowBlock {
     // is >= 0, so where their sum is at most kRowsRebase none exceeds it.
     // Otherwise (also when no reference is set yet: the sum is then infinite
     // or NaN) the row maxima are taken and the accumulators rescaled.
-    // fresh: the first step, which has no reference on any lane.
-    __device__ __forceinline__ void softmax(f32x16 (&s)[NKB], const ScoreArgs &a,
-                                            bf16x8 (&pf)[NKB][2], bool fresh)
+    // dist0 = first key of the tile - this lane's row; fresh: the first step,
+    // which has no reference on any lane.
+    __device__ __forceinline__ void softmax(const f32x16 (&s)[NKB], const ScoreArgs &a,
+                                            float slope_log2, int dist0, bf16x8 (&pf)[NKB][2],
+                                            bool fresh)
     {
+        const float f = factor(a);
+        // distances below 2^24 are exact in fp32
+        float base = (SCORE & kScoreCap) != 0 ? a.cap_out : 0.f;
+        if constexpr ((SCORE & kScoreSlope) != 0)
+            base = __builtin_fmaf(slope_log2, (float)(dist0 + 8 * half), base);
+        auto score = [&](int kb, int v, float b) TA_INLINE -> float {
+            if constexpr ((SCORE & kScoreSlope) != 0)
+                b = __builtin_fmaf(slope_log2, (float)(kb * 32 + rows_key_of_reg(v, 0)), b);
+            return __builtin_fmaf(s[kb][v], f, b);
+        };
         auto exps = [&](float m) TA_INLINE -> float {
+            const float b = base - m;
             float sum = 0.f;
 #pragma unroll
             for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
                 for (int s2 = 0; s2 < 2; ++s2) {
-                    f32x8r t;
+                    u32x4 packed;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float x = s[kb][8 * s2 + e];
-                        t[e] = __builtin_amdgcn_exp2f(
-                            SCORE == 0 ? __builtin_fmaf(x, a.scale_log2, -m) : x - m);
-                        sum = (kb | s2 | e) ? sum + t[e] : t[e];
+                    for (int e = 0; e < 8; e += 2) {
+                        typedef float f32x2r __attribute__((ext_vector_type(2)));
+                        typedef __bf16 bf16x2r __attribute__((ext_vector_type(2)));
+                        f32x2r t;
+                        t[0] = __builtin_amdgcn_exp2f(score(kb, 8 * s2 + e, b));
+                        t[1] = __builtin_amdgcn_exp2f(score(kb, 8 * s2 + e + 1, b));
+                        sum = (kb | s2 | e) ? sum + t[0] : t[0];
+                        sum += t[1];
+                        packed[e / 2] = __builtin_bit_cast(
+                            uint32_t, __builtin_convertvector(t, bf16x2r));
                     }
-                    pf[kb][s2] = __builtin_convertvector(t, bf16x8);
+                    pf[kb][s2] = __builtin_bit_cast(bf16x8, packed);
                 }
             return sum;
         };
         float sum = INFINITY;
         if (!fresh)
             sum = exps(m_ref);
-        if (__builtin_amdgcn_ballot_w64(!(sum <= kRowsRebase)) != 0) {
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum <= kRowsRebase)) != 0, 0)) {
             float mx = -INFINITY;
 #pragma unroll
             for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
                 for (int v = 0; v < 16; ++v)
-                    mx = fmaxf(mx, s[kb][v]);
+                    mx = fmaxf(mx, score(kb, v, base));
             mx = rows_pair_max(mx);
-            if (SCORE == 0)
-                mx *= a.scale_log2;
             // only the rows that need it: a row's bits follow from its own
             // scores, not from the rows that share its wave
             const bool mine = rows_pair_max(sum <= kRowsRebase ? 0.f : 1.f) != 0.f;
@@ -326,12 +332,11 @@ struct RowBlock {
                         v_fragment(vt, kb, s2, b), pf[kb][s2], oacc[b], 0, 0, 0);
     }
 
-    // The same for a masked step, where rows give keys probability zero that
-    // other rows keep: zero times an infinite or NaN value must not reach
-    // them.  A tile that holds one is added key by key, each only to the rows
-    // whose probability of it is not zero.
-    __device__ __forceinline__ void accumulate_masked(const unsigned char *vt,
-                                                      const bf16x8 (&pf)[NKB][2], int lane)
+    // Whether a tile holds an infinite or NaN value.  In a masked step rows
+    // give keys probability zero that other rows keep, and zero times such a
+    // value must not reach them: accumulate_by_key then takes the place of
+    // accumulate.
+    __device__ __forceinline__ static bool odd_values(const unsigned char *vt, int lane)
     {
         bool odd = false;
 #pragma unroll
@@ -341,10 +346,14 @@ struct RowBlock {
             for (int e = 0; e < 4; ++e)
                 odd |= ((w[e] & 0x7f80u) == 0x7f80u) | ((w[e] & 0x7f800000u) == 0x7f800000u);
         }
-        if (__builtin_amdgcn_ballot_w64(odd) == 0) {
-            accumulate(vt, pf);
-            return;
-        }
+        return __builtin_amdgcn_ballot_w64(odd) != 0;
+    }
+
+    // accumulate() key by key, each only to the rows whose probability of it
+    // is not zero.
+    __device__ __forceinline__ void accumulate_by_key(const unsigned char *vt,
+                                                      const bf16x8 (&pf)[NKB][2])
+    {
         typedef uint16_t u16x8r __attribute__((ext_vector_type(8)));
         typedef uint16_t u16x4r __attribute__((ext_vector_type(4)));
 #pragma unroll 1

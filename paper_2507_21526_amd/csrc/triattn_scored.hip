@@ -149,7 +149,6 @@ __global__ __launch_bounds__(kThreads, 2) void scored_attn_kernel(ScoredArgs a)
     rb.init(lane);
     const int row = min(row_base + rb.col, r1 - 1);
     rb.load_q(a.q + ((seq_off + row) * a.hq + head) * (int64_t)D);
-    rb.reset();
     float slope = 0.f;
     if constexpr ((SCORE & kScoreSlope) != 0)
         slope = a.score.slopes[head] * kRowsLog2e;
@@ -213,56 +212,71 @@ __global__ __launch_bounds__(kThreads, 2) void scored_attn_kernel(ScoredArgs a)
         asm volatile("" ::: "memory");
     };
 
-    bool fresh = true;
-    if (n > 0)
+    // One pass over the steps; with `careful`, infinite or NaN values in
+    // masked steps are kept from the rows that do not keep their keys.
+    // Returns whether a masked step holds any.
+    auto pass = [&](auto careful) TA_INLINE -> bool {
+        constexpr bool CAREFUL = decltype(careful)::value;
+        bool fresh = true, odd = false;
+        rb.reset();
         copy_step(step_key(0), 0);
-    for (int i = 0; i < n; ++i) {
-        // this step's tile has landed for every wave, and every wave is done
-        // with the other stage
-        __builtin_amdgcn_sched_barrier(0);
-        rows_wait_copies<0>();
-        barrier_no_fence();
-        __builtin_amdgcn_sched_barrier(0);
-        const int key0 = step_key(i);
-        if (i + 1 < n)
-            copy_step(step_key(i + 1), (i + 1) & 1);
-        __builtin_amdgcn_sched_barrier(0);
-        // the wave's rows may keep nothing of a step that others need
-        const bool none = !active | (key0 > row_hi) |
-                          (stream & (key0 >= a.sink) &
-                           (row_base - (key0 + kKeys - 1) >= a.window));
-        if (!none) {
-            const unsigned char *kt = smem + (i & 1) * STAGE_BYTES;
+        auto step = [&](int i, auto stage) TA_INLINE {
+            constexpr int ST = decltype(stage)::value;
+            // this step's tile has landed for every wave, and every wave is
+            // done with the other stage
+            __builtin_amdgcn_sched_barrier(0);
+            rows_wait_copies<0>();
+            barrier_no_fence();
+            __builtin_amdgcn_sched_barrier(0);
+            const int key0 = step_key(i);
+            if (i + 1 < n)
+                copy_step(step_key(i + 1), 1 - ST);
+            __builtin_amdgcn_sched_barrier(0);
+            const unsigned char *kt = smem + ST * STAGE_BYTES;
             f32x16 s[2];
             bf16x8 p[2][2];
             rb.products(kt, s);
-            rb.modify(s, a.score, slope, key0 - row);
-            const bool diagonal = key0 + kKeys - 1 > row_base;
-            const bool edge = stream && key0 + kKeys - 1 >= a.sink && row_hi - key0 >= a.window;
-            if (edge) {
-                const int lim = row - key0 - 8 * rb.half;
-                const int far = lim - a.window;             // kept: offset > far
-                const int sinks = a.sink - key0 - 8 * rb.half;  // or offset < sinks
+            rb.modify(s, a.score);
+            const bool edge = stream & (key0 + kKeys - 1 >= a.sink) & (row_hi - key0 >= a.window);
+            const bool masked = (key0 + kKeys - 1 > row_base) | edge;
+            if (__builtin_expect(masked, 0)) {
+                asm volatile("");  // a branch: most steps have no mask
+                odd |= rb.odd_values(kt + TILE_BYTES, lane);
+                if (edge) {
+                    const int lim = row - key0 - 8 * rb.half;
+                    const int far = lim - a.window;                 // kept: offset > far
+                    const int sinks = a.sink - key0 - 8 * rb.half;  // or offset < sinks
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
+                    for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const int off = kb * 32 + rows_key_of_reg(v, 0);
-                        s[kb][v] = (off <= lim) & ((off > far) | (off < sinks)) ? s[kb][v]
-                                                                              : -INFINITY;
-                    }
-            } else if (diagonal) {
-                rb.mask_above(s, row - key0);
+                        for (int v = 0; v < 16; ++v) {
+                            const int off = kb * 32 + rows_key_of_reg(v, 0);
+                            s[kb][v] = (off <= lim) & ((off > far) | (off < sinks)) ? s[kb][v]
+                                                                                  : -INFINITY;
+                        }
+                } else {
+                    rb.mask_above(s, row - key0);
+                }
             }
-            rb.softmax(s, a.score, p, fresh);
+            rb.softmax(s, a.score, slope, key0 - row, p, fresh);
             fresh = false;
-            if (diagonal | edge)
-                rb.accumulate_masked(kt + TILE_BYTES, p, lane);
+            if (CAREFUL && masked)
+                rb.accumulate_by_key(kt + TILE_BYTES, p);
             else
                 rb.accumulate(kt + TILE_BYTES, p);
+        };
+        int i = 0;
+        for (; i + 1 < n; i += 2) {
+            step(i, std::integral_constant<int, 0>{});
+            step(i + 1, std::integral_constant<int, 1>{});
         }
-        __builtin_amdgcn_sched_barrier(0);
-    }
+        if (i < n)
+            step(i, std::integral_constant<int, 0>{});
+        return odd;
+    };
+    rb.reset();
+    if (n > 0 && __builtin_expect(__syncthreads_or(pass(std::false_type{})), 0))
+        pass(std::true_type{});
 
     if (!active || row_base + rb.col >= r1)
         return;
