@@ -402,7 +402,7 @@ __global__ __launch_bounds__(kThreads, (PagedShape<D, RB>::WGS_PER_CU)) void pag
                 const bool masked = key0 + S::TK - 1 > first_last;
                 if (__builtin_expect(masked, 0)) {
                     asm volatile("");  // a branch: most steps have no mask
-                    odd |= rb.odd_values(kt + S::TILE_BYTES, lane);
+                    odd |= rb.odd_values(kt + S::TILE_BYTES, lane, 0, 1);
                     rb.mask_above(s, last - key0);
                 }
                 rb.softmax(s, a.score, slope, key0 - dist_row, p, fresh);

@@ -332,21 +332,22 @@ struct RowBlock {
                         v_fragment(vt, kb, s2, b), pf[kb][s2], oacc[b], 0, 0, 0);
     }
 
-    // Whether a tile holds an infinite or NaN value.  In a masked step rows
-    // give keys probability zero that other rows keep, and zero times such a
-    // value must not reach them: accumulate_by_key then takes the place of
-    // accumulate.
-    __device__ __forceinline__ static bool odd_values(const unsigned char *vt, int lane)
+    // Whether a tile holds an infinite or NaN value (this wave looks at part
+    // `part` of `parts`).  In a masked step rows give keys probability zero that
+    // other rows keep, and zero times such a value must not reach them:
+    // accumulate_by_key then takes the place of accumulate.
+    __device__ __forceinline__ static bool odd_values(const unsigned char *vt, int lane, int part,
+                                                      int parts)
     {
-        bool odd = false;
-#pragma unroll
-        for (int i = 0; i < NKB * 32 * ROW_BYTES / 1024; ++i) {
+        constexpr int BYTES = NKB * 32 * ROW_BYTES;
+        uint32_t carry = 0;
+        for (int i = part; i < BYTES / 1024; i += parts) {
             const u32x4 w = *reinterpret_cast<const u32x4 *>(vt + i * 1024 + lane * 16);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                odd |= ((w[e] & 0x7f80u) == 0x7f80u) | ((w[e] & 0x7f800000u) == 0x7f800000u);
+            for (int e = 0; e < 4; ++e)  // an exponent of all ones carries into the sign bit
+                carry |= (w[e] & 0x7f807f80u) + 0x00800080u;
         }
-        return __builtin_amdgcn_ballot_w64(odd) != 0;
+        return __builtin_amdgcn_ballot_w64((carry & 0x80008000u) != 0) != 0;
     }
 
     // accumulate() key by key, each only to the rows whose probability of it
@@ -384,6 +385,32 @@ struct RowBlock {
                         oacc[b][4 * c + e] +=
                             keeps ? p * __uint_as_float((uint32_t)v[e] << 16) : 0.f;
                 }
+        }
+    }
+
+    // Order of the LDS reads and MFMAs issued since the last scheduling region
+    // began: products() when QK, then accumulate() when PV.  MFMA i of products
+    // needs one read (a K fragment), one of accumulate two; the reads of MFMA i +
+    // AHEAD go out just before MFMA i, so that their latency (over a hundred
+    // cycles under load, four MFMAs) is covered.
+    template <bool QK, bool PV>
+    __device__ __forceinline__ static void schedule()
+    {
+        constexpr int NQ = QK ? NKB * QK_STEPS : 0, N = NQ + (PV ? NKB * 2 * D_BLOCKS : 0);
+        constexpr int AHEAD = 6;
+        static_assert(N >= AHEAD, "more MFMAs than reads ahead");
+        constexpr int first = AHEAD <= NQ ? AHEAD : NQ + 2 * (AHEAD - NQ);
+        __builtin_amdgcn_sched_group_barrier(kSchedDsRead, first, 0);
+        schedule_from<NQ, N, AHEAD, 0>();
+    }
+    template <int NQ, int N, int AHEAD, int I>
+    __device__ __forceinline__ static void schedule_from()
+    {
+        if constexpr (I < N) {
+            __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
+            if constexpr (I + AHEAD < N)
+                __builtin_amdgcn_sched_group_barrier(kSchedDsRead, I + AHEAD < NQ ? 1 : 2, 0);
+            schedule_from<NQ, N, AHEAD, I + 1>();
         }
     }
 

@@ -22,8 +22,7 @@
 namespace triattn {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWaves = 4;
+constexpr int kJoinThreads = 256;
 constexpr int kKeys = 64;           // keys of a step
 constexpr int kListSteps = 2048;    // steps of a list item held in LDS
 
@@ -69,15 +68,16 @@ __device__ __forceinline__ Runs reach(Runs r, bool stream, int sink, int window,
     return r;
 }
 
-template <int D, int SCORE, bool LIST>
-__global__ __launch_bounds__(kThreads, 2) void scored_attn_kernel(ScoredArgs a)
+template <int D, int SCORE, bool LIST, int NW>
+__global__ __launch_bounds__(NW * 64, 8 / NW) void scored_attn_kernel(ScoredArgs a)
 {
+    constexpr int kThreads = NW * 64;
     constexpr int ROW_BYTES = 2 * D;
     constexpr int CHUNKS = D / 8;
     constexpr int TILE_BYTES = kKeys * ROW_BYTES;
     constexpr int STAGE_BYTES = 2 * TILE_BYTES;  // K tile, then V tile
     constexpr int COPY_ROWS = 1024 / ROW_BYTES;  // keys of a 1 KB copy
-    constexpr int COPIES = TILE_BYTES / 1024 / kWaves;  // of a wave, for K and again for V
+    constexpr int COPIES = TILE_BYTES / 1024 / NW;  // of a wave, for K and again for V
     constexpr int D_BLOCKS = D / 32;
 
     __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE_BYTES];
@@ -135,11 +135,11 @@ __global__ __launch_bounds__(kThreads, 2) void scored_attn_kernel(ScoredArgs a)
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     // row block b: head b % group, rows 32 (b / group) on
-    const int b0 = kWaves * sub;
+    const int b0 = NW * sub;
     const int wr0 = r0 + 32 * (b0 / a.group);
     if (wr0 >= r1)
         return;  // ragged q-tile: nothing for this workgroup
-    const int wr1 = min(r0 + 32 * ((b0 + kWaves - 1) / a.group + 1), r1) - 1;
+    const int wr1 = min(r0 + 32 * ((b0 + NW - 1) / a.group + 1), r1) - 1;
     const int head = g * a.group + (b0 + wave) % a.group;
     const int row_base = r0 + 32 * ((b0 + wave) / a.group);
     const bool active = row_base < r1;
@@ -170,114 +170,257 @@ __global__ __launch_bounds__(kThreads, 2) void scored_attn_kernel(ScoredArgs a)
         runs = reach(runs, stream, a.sink, a.window, wr0, wr1);
         n = runs.a_hi - runs.a_lo + runs.b_hi - runs.b_lo;
     }
-    auto step_key = [&](int s) TA_INLINE -> int {
+    // Step i of the pass.  Where scores fall with the distance the steps run
+    // from the last key to the first: a row's largest scores come first, and
+    // its reference stands (in the other order each step's outgrow it, and
+    // nearly every step of a steep head rescales the accumulators).
+    auto step_key = [&](int i) TA_INLINE -> int {
+        const int s = (SCORE & kScoreSlope) != 0 ? n - 1 - i : i;
         if (list)
             return __builtin_amdgcn_readfirstlane(s < kListSteps ? s_key[s] : listed(s));
         const int na = runs.a_hi - runs.a_lo;
         return (s < na ? runs.a_lo + s : runs.b_lo + s - na) * kKeys;
     };
     if (list)  // listed tiles increase: only the last may pass the rows
-        while (n > 0 && step_key(n - 1) > wr1)
+        while (n > 0 && listed(n - 1) > wr1)
             --n;
 
-    // copies: wave w takes 1 KB blocks w COPIES .. of the K and the V tile
+    // copies: wave w takes 1 KB blocks w COPIES .. of a tile.  The swizzle of
+    // block i's rows is that of block 0's with the bits of i COPY_ROWS flipped (K;
+    // V's does not depend on them).
     const uint32_t smem_addr =
         (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
-    const int dma_row = lane / CHUNKS, dma_chunk = lane % CHUNKS;
     const uint32_t pitch = (uint32_t)(a.hkv * ROW_BYTES);
     const uint16_t *kbase = a.k + (seq_off * a.hkv + g) * (int64_t)D;
     const uint16_t *vbase = a.v + (seq_off * a.hkv + g) * (int64_t)D;
-    uint32_t koff[COPIES], voff[COPIES];
-#pragma unroll
-    for (int i = 0; i < COPIES; ++i) {
-        const int r = (wave * COPIES + i) * COPY_ROWS + dma_row;
-        koff[i] = (uint32_t)((dma_chunk ^ rows_kswz<D>(r)) << 4);
-        voff[i] = (uint32_t)((dma_chunk ^ rows_vswz<D>(r)) << 4);
-    }
-    auto copy_step = [&](int key0, int stage) TA_INLINE {
+    const int dma_row = wave * COPIES * COPY_ROWS + lane / CHUNKS;
+    const uint32_t dma_off = __umul24((uint32_t)dma_row, pitch);
+    const uint32_t kswz = (uint32_t)(((lane % CHUNKS) ^ rows_kswz<D>(dma_row)) << 4);
+    const uint32_t vswz = (uint32_t)(((lane % CHUNKS) ^ rows_vswz<D>(dma_row)) << 4);
+    static_assert((COPIES & (COPIES - 1)) == 0 && COPIES <= 4, "blocks of a wave differ in bits");
+    auto copy_tile = [&](const uint16_t *base, int key0, uint32_t lds, auto is_v) TA_INLINE {
         asm volatile("" ::: "memory");
         // rows past the sequence repeat its last one; no row keeps them
         const int first = min(key0, seq_len - 1);
-        const int lim = min(seq_len - 1 - first, kKeys - 1);
-        const uint16_t *kt = kbase + (int64_t)first * a.hkv * D;
-        const uint16_t *vt = vbase + (int64_t)first * a.hkv * D;
-        const uint32_t lds = smem_addr + stage * STAGE_BYTES + wave * COPIES * 1024;
+        const uint32_t lim = (uint32_t)min(seq_len - 1 - first, kKeys - 1) * pitch;
+        const uint16_t *from = base + (int64_t)first * a.hkv * D;
 #pragma unroll
         for (int i = 0; i < COPIES; ++i) {
-            const int r = min((wave * COPIES + i) * COPY_ROWS + dma_row, lim);
-            const uint32_t off = __umul24((uint32_t)r, pitch);
-            copy_to_lds16(kt, off + koff[i], lds + i * 1024);
-            copy_to_lds16(vt, off + voff[i], lds + TILE_BYTES + i * 1024);
+            const uint32_t swz =
+                decltype(is_v)::value ? vswz : kswz ^ (uint32_t)(rows_kswz<D>(i * COPY_ROWS) << 4);
+            copy_to_lds16(from, min(dma_off + (uint32_t)(i * COPY_ROWS) * pitch, lim) + swz,
+                          lds + (wave * COPIES + i) * 1024);
         }
         asm volatile("" ::: "memory");
     };
+    auto copy_k = [&](int key0, int stage) TA_INLINE {
+        copy_tile(kbase, key0, smem_addr + stage * STAGE_BYTES, std::false_type{});
+    };
+    auto copy_v = [&](int key0, int stage) TA_INLINE {
+        copy_tile(vbase, key0, smem_addr + stage * STAGE_BYTES + TILE_BYTES, std::true_type{});
+    };
+    auto end_phase = [&](bool copies) TA_INLINE {
+        __builtin_amdgcn_sched_barrier(0);
+        if (copies)
+            rows_wait_copies<0>();
+        barrier_no_fence();
+        __builtin_amdgcn_sched_barrier(0);
+    };
 
-    // One pass over the steps; with `careful`, infinite or NaN values in
-    // masked steps are kept from the rows that do not keep their keys.
-    // Returns whether a masked step holds any.
-    auto pass = [&](auto careful) TA_INLINE -> bool {
+    f32x16 s[2];
+    bf16x8 p[2][2];
+    bool fresh, odd;
+    // Whether some row of the workgroup drops keys of a step.
+    auto any_mask = [&](int key0) TA_INLINE -> bool {
+        return (key0 + kKeys - 1 > wr0) |
+               (stream & (key0 + kKeys - 1 >= a.sink) & (wr1 - key0 >= a.window));
+    };
+    // Keys that this wave's rows drop (three comparisons a score only where a
+    // step holds more than one of the edges).
+    auto mask = [&](int key0) TA_INLINE {
+        const bool diagonal = key0 + kKeys - 1 > row_base;
+        const bool edge = stream & (key0 + kKeys - 1 >= a.sink) & (row_hi - key0 >= a.window);
+        if (!edge) {
+            if (diagonal)
+                rb.mask_above(s, row - key0);
+            return;
+        }
+        const int lim = row - key0 - 8 * rb.half;
+        const int far = lim - a.window;                 // in the window: offset > far
+        const int sinks = a.sink - key0 - 8 * rb.half;  // in the sink: offset < sinks
+        auto keep = [&](auto &&test) TA_INLINE {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    s[kb][v] = test(kb * 32 + rows_key_of_reg(v, 0)) ? s[kb][v] : -INFINITY;
+        };
+        if (!diagonal && key0 >= a.sink)
+            keep([&](int off) TA_INLINE { return off > far; });
+        else if (key0 + kKeys - 1 <= row_base - a.window)
+            keep([&](int off) TA_INLINE { return off < sinks; });
+        else
+            keep([&](int off) TA_INLINE { return (off <= lim) & ((off > far) | (off < sinks)); });
+    };
+    // X(j): the scores of step j to probabilities
+    auto softmax = [&](int key0) TA_INLINE {
+        rb.modify(s, a.score);
+        if (__builtin_expect(any_mask(key0), 0)) {
+            asm volatile("");  // a branch: most steps have no mask
+            mask(key0);
+        }
+        rb.softmax(s, a.score, slope, key0 - row, p, fresh);
+        fresh = false;
+    };
+    // The values of a masked step, each wave its part of the tile (apart from
+    // the common path).
+    auto look = [&](int key0, const unsigned char *vt) TA_INLINE {
+        if (__builtin_expect(any_mask(key0), 0)) {
+            asm volatile("");
+            odd |= rb.odd_values(vt, lane, wave, NW);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // O += V P of the step whose probabilities p holds
+    auto values = [&](int key0, const unsigned char *vt) TA_INLINE {
+        look(key0, vt);
+        rb.accumulate(vt, p);
+        rb.template schedule<false, true>();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto products = [&](const unsigned char *kt) TA_INLINE {
+        __builtin_amdgcn_sched_barrier(0);
+        rb.products(kt, s);
+        rb.template schedule<true, false>();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    using Stage0 = std::integral_constant<int, 0>;
+    using Stage1 = std::integral_constant<int, 1>;
+
+    // One pass over the steps, every wave in the same one.  With `careful`,
+    // infinite or NaN values in masked steps are kept from the rows that do not
+    // keep their keys; otherwise `odd` tells whether a masked step holds any.
+    auto together = [&](auto careful) TA_INLINE {
         constexpr bool CAREFUL = decltype(careful)::value;
-        bool fresh = true, odd = false;
-        rb.reset();
-        copy_step(step_key(0), 0);
+        auto copies = [&](int i, int stage) TA_INLINE {
+            copy_k(step_key(i), stage);
+            copy_v(step_key(i), stage);
+        };
+        copies(0, 0);
         auto step = [&](int i, auto stage) TA_INLINE {
             constexpr int ST = decltype(stage)::value;
             // this step's tile has landed for every wave, and every wave is
             // done with the other stage
-            __builtin_amdgcn_sched_barrier(0);
-            rows_wait_copies<0>();
-            barrier_no_fence();
-            __builtin_amdgcn_sched_barrier(0);
-            const int key0 = step_key(i);
+            end_phase(true);
             if (i + 1 < n)
-                copy_step(step_key(i + 1), 1 - ST);
+                copies(i + 1, 1 - ST);
             __builtin_amdgcn_sched_barrier(0);
             const unsigned char *kt = smem + ST * STAGE_BYTES;
-            f32x16 s[2];
-            bf16x8 p[2][2];
-            rb.products(kt, s);
-            rb.modify(s, a.score);
-            const bool edge = stream & (key0 + kKeys - 1 >= a.sink) & (row_hi - key0 >= a.window);
-            const bool masked = (key0 + kKeys - 1 > row_base) | edge;
-            if (__builtin_expect(masked, 0)) {
-                asm volatile("");  // a branch: most steps have no mask
-                odd |= rb.odd_values(kt + TILE_BYTES, lane);
-                if (edge) {
-                    const int lim = row - key0 - 8 * rb.half;
-                    const int far = lim - a.window;                 // kept: offset > far
-                    const int sinks = a.sink - key0 - 8 * rb.half;  // or offset < sinks
-#pragma unroll
-                    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                        for (int v = 0; v < 16; ++v) {
-                            const int off = kb * 32 + rows_key_of_reg(v, 0);
-                            s[kb][v] = (off <= lim) & ((off > far) | (off < sinks)) ? s[kb][v]
-                                                                                  : -INFINITY;
-                        }
-                } else {
-                    rb.mask_above(s, row - key0);
-                }
-            }
-            rb.softmax(s, a.score, slope, key0 - row, p, fresh);
-            fresh = false;
-            if (CAREFUL && masked)
+            products(kt);
+            softmax(step_key(i));
+            if (!CAREFUL)
+                values(step_key(i), kt + TILE_BYTES);
+            else if (any_mask(step_key(i)))
                 rb.accumulate_by_key(kt + TILE_BYTES, p);
             else
                 rb.accumulate(kt + TILE_BYTES, p);
         };
         int i = 0;
         for (; i + 1 < n; i += 2) {
-            step(i, std::integral_constant<int, 0>{});
-            step(i + 1, std::integral_constant<int, 1>{});
+            step(i, Stage0{});
+            step(i + 1, Stage1{});
         }
         if (i < n)
-            step(i, std::integral_constant<int, 0>{});
-        return odd;
+            step(i, Stage0{});
     };
-    rb.reset();
-    if (n > 0 && __builtin_expect(__syncthreads_or(pass(std::false_type{})), 0))
-        pass(std::true_type{});
-
+    // The same in two groups of four waves, one wave of each on a SIMD, in
+    // turns: M(j) = {S(j) = K(j) Q^T, O += V(j - 1) P(j - 1)} on the matrix
+    // cores beside the other group's X(j) on the vector units.  Group 0 runs
+    // M(j) in phase 2 j and X(j) in phase 2 j + 1, group 1 X(j - 1) in phase 2 j
+    // and M(j) in phase 2 j + 1.  Stage j & 1 holds K(j) and V(j - 1) in these
+    // two phases; K(j + 1) and V(j) are copied into the other one, last read in
+    // phase 2 j - 1, from phase 2 j on.
+    auto in_turns = [&]() TA_INLINE {
+        auto matrix = [&](int j, auto stage) TA_INLINE {
+            const unsigned char *kt = smem + decltype(stage)::value * STAGE_BYTES;
+            look(step_key(j - 1), kt + TILE_BYTES);
+            __builtin_amdgcn_s_setprio(1);
+            __builtin_amdgcn_sched_barrier(0);
+            rb.products(kt, s);
+            rb.accumulate(kt + TILE_BYTES, p);
+            rb.template schedule<true, true>();
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(0);
+        };
+        auto copies = [&](int j, int stage) TA_INLINE {
+            copy_k(step_key(min(j + 1, n - 1)), 1 - stage);
+            copy_v(step_key(j), 1 - stage);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        copy_k(step_key(0), 0);
+        end_phase(true);
+        copies(0, 0);
+        int j = 1;
+        if (wave < 4) {
+            products(smem);
+            end_phase(false);
+            softmax(step_key(0));
+            end_phase(true);
+            auto step = [&](int j, auto stage) TA_INLINE {
+                copies(j, decltype(stage)::value);
+                matrix(j, stage);
+                end_phase(false);
+                softmax(step_key(j));
+                end_phase(true);
+            };
+            for (; j + 1 < n; j += 2) {
+                step(j, Stage1{});
+                step(j + 1, Stage0{});
+            }
+            if (j < n)
+                step(j, Stage1{});
+            values(step_key(n - 1), smem + (n & 1) * STAGE_BYTES + TILE_BYTES);
+            end_phase(false);
+            end_phase(false);
+        } else {
+            end_phase(false);
+            products(smem);
+            end_phase(true);
+            auto step = [&](int j, auto stage) TA_INLINE {
+                copies(j, decltype(stage)::value);
+                softmax(step_key(j - 1));
+                end_phase(false);
+                matrix(j, stage);
+                end_phase(true);
+            };
+            for (; j + 1 < n; j += 2) {
+                step(j, Stage1{});
+                step(j + 1, Stage0{});
+            }
+            if (j < n)
+                step(j, Stage1{});
+            softmax(step_key(n - 1));
+            end_phase(false);
+            values(step_key(n - 1), smem + (n & 1) * STAGE_BYTES + TILE_BYTES);
+            end_phase(false);
+        }
+    };
+    auto start = [&]() TA_INLINE {
+        fresh = true;
+        odd = false;
+        rb.reset();
+    };
+    start();
+    if (n > 0) {
+        if constexpr (NW == 8)
+            in_turns();
+        else
+            together(std::false_type{});
+        if (__builtin_expect(__syncthreads_or(odd), 0)) {
+            start();
+            together(std::true_type{});
+        }
+    }
     if (!active || row_base + rb.col >= r1)
         return;
     float inv, lse;
@@ -314,9 +457,9 @@ __global__ __launch_bounds__(kThreads, 2) void scored_attn_kernel(ScoredArgs a)
 // Joins the partials of the schedule's split q-tiles, a wave to a (row, head):
 // O = sum_c w_c O_c / sum_c w_c with w_c = exp(LSE_c - max_c LSE_c).
 template <int D>
-__global__ __launch_bounds__(kThreads) void scored_join_kernel(ScoredArgs a)
+__global__ __launch_bounds__(kJoinThreads) void scored_join_kernel(ScoredArgs a)
 {
-    constexpr int PER = D / 64;
+    constexpr int PER = D / 64, kWaves = kJoinThreads / 64;
     const int32_t *sched = a.sched;
     const int blocks = (a.tile * a.hq + kWaves - 1) / kWaves;  // workgroups of a merge item
     const int m = blockIdx.x / blocks;
@@ -388,14 +531,24 @@ __global__ __launch_bounds__(kThreads) void scored_join_kernel(ScoredArgs a)
             den == 0.f ? -INFINITY : m_use + __logf(den);
 }
 
-template <int D, bool LIST>
+template <int D, bool LIST, int NW>
 void launch_scored(int score, dim3 grid, hipStream_t s, const ScoredArgs &a)
 {
+    const dim3 threads(NW * 64);
     switch (score) {
-    case 1: hipLaunchKernelGGL((scored_attn_kernel<D, 1, LIST>), grid, dim3(kThreads), 0, s, a); break;
-    case 2: hipLaunchKernelGGL((scored_attn_kernel<D, 2, LIST>), grid, dim3(kThreads), 0, s, a); break;
-    default: hipLaunchKernelGGL((scored_attn_kernel<D, 3, LIST>), grid, dim3(kThreads), 0, s, a); break;
+    case 1: hipLaunchKernelGGL((scored_attn_kernel<D, 1, LIST, NW>), grid, threads, 0, s, a); break;
+    case 2: hipLaunchKernelGGL((scored_attn_kernel<D, 2, LIST, NW>), grid, threads, 0, s, a); break;
+    default: hipLaunchKernelGGL((scored_attn_kernel<D, 3, LIST, NW>), grid, threads, 0, s, a); break;
     }
+}
+
+template <int D, int NW>
+void launch_scored(bool list, int score, dim3 grid, hipStream_t s, const ScoredArgs &a)
+{
+    if (list)
+        launch_scored<D, true, NW>(score, grid, s, a);
+    else
+        launch_scored<D, false, NW>(score, grid, s, a);
 }
 
 }  // namespace
@@ -458,10 +611,12 @@ extern "C" ta_status scored_attn_fwd(const void *q, const void *k, const void *v
     if (2LL * hq * head_dim >= (1LL << 24))
         return fail(TA_ERR_UNSUPPORTED, "%s: hq * head_dim too large", fn);
     const int64_t group = hq / hkv;
-    const int64_t subtiles = (group * (info->tile / 32) + kWaves - 1) / kWaves;
+    const int64_t blocks = group * (info->tile / 32);
+    const int nw = blocks > 4 ? 8 : 4;
+    const int64_t subtiles = (blocks + nw - 1) / nw;
     const int64_t wgs = info->n_items * subtiles * hkv;
     const int64_t join_wgs =
-        info->n_merge_items * (((int64_t)info->tile * hq + kWaves - 1) / kWaves);
+        info->n_merge_items * (((int64_t)info->tile * hq + 3) / 4);
     if (wgs > INT32_MAX || join_wgs > INT32_MAX)
         return fail(TA_ERR_UNSUPPORTED, "%s: grid too large", fn);
     if (info->n_items == 0)
@@ -508,22 +663,22 @@ extern "C" ta_status scored_attn_fwd(const void *q, const void *k, const void *v
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const dim3 grid((uint32_t)wgs);
     const bool list = info->kind == TA_KIND_BLOCKSPARSE;
-    if (head_dim == 128 && list)
-        launch_scored<128, true>(score, grid, s, a);
+    if (head_dim == 128 && nw == 8)
+        launch_scored<128, 8>(list, score, grid, s, a);
     else if (head_dim == 128)
-        launch_scored<128, false>(score, grid, s, a);
-    else if (list)
-        launch_scored<64, true>(score, grid, s, a);
+        launch_scored<128, 4>(list, score, grid, s, a);
+    else if (nw == 8)
+        launch_scored<64, 8>(list, score, grid, s, a);
     else
-        launch_scored<64, false>(score, grid, s, a);
+        launch_scored<64, 4>(list, score, grid, s, a);
     hipError_t err = hipGetLastError();
     if (err == hipSuccess && join_wgs > 0) {
         if (head_dim == 128)
-            hipLaunchKernelGGL(scored_join_kernel<128>, dim3((uint32_t)join_wgs), dim3(kThreads),
-                               0, s, a);
+            hipLaunchKernelGGL(scored_join_kernel<128>, dim3((uint32_t)join_wgs),
+                               dim3(kJoinThreads), 0, s, a);
         else
-            hipLaunchKernelGGL(scored_join_kernel<64>, dim3((uint32_t)join_wgs), dim3(kThreads), 0,
-                               s, a);
+            hipLaunchKernelGGL(scored_join_kernel<64>, dim3((uint32_t)join_wgs),
+                               dim3(kJoinThreads), 0, s, a);
         err = hipGetLastError();
     }
     if (err != hipSuccess)
