@@ -184,8 +184,10 @@ struct RowBlock {
             qf[s] = *reinterpret_cast<const bf16x8 *>(row + 16 * s + 8 * half);
     }
 
-    // Raw products of one tile.
-    __device__ __forceinline__ void products(const unsigned char *kt, f32x16 (&s)[NKB]) const
+    // Raw products of one tile; hook(i) runs after MFMA i.
+    template <typename F>
+    __device__ __forceinline__ void products(const unsigned char *kt, f32x16 (&s)[NKB],
+                                             F &&hook) const
     {
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb)
@@ -197,7 +199,12 @@ struct RowBlock {
                 const bf16x8 a =
                     *reinterpret_cast<const bf16x8 *>(kt + koff[i] + kb * 32 * ROW_BYTES);
                 s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[i], s[kb], 0, 0, 0);
+                hook(i * NKB + kb);
             }
+    }
+    __device__ __forceinline__ void products(const unsigned char *kt, f32x16 (&s)[NKB]) const
+    {
+        products(kt, s, [](int) {});
     }
 
     // Scores are held as values x of which the log2-domain score is
@@ -319,17 +326,25 @@ struct RowBlock {
                                   __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
     }
 
-    // O^T += V^T P^T for one tile.
-    __device__ __forceinline__ void accumulate(const unsigned char *vt, const bf16x8 (&pf)[NKB][2])
+    // O^T += V^T P^T for one tile; hook(i) runs after MFMA i.
+    template <typename F>
+    __device__ __forceinline__ void accumulate(const unsigned char *vt, const bf16x8 (&pf)[NKB][2],
+                                               F &&hook)
     {
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
             for (int s2 = 0; s2 < 2; ++s2)
 #pragma unroll
-                for (int b = 0; b < D_BLOCKS; ++b)
+                for (int b = 0; b < D_BLOCKS; ++b) {
                     oacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
                         v_fragment(vt, kb, s2, b), pf[kb][s2], oacc[b], 0, 0, 0);
+                    hook((kb * 2 + s2) * D_BLOCKS + b);
+                }
+    }
+    __device__ __forceinline__ void accumulate(const unsigned char *vt, const bf16x8 (&pf)[NKB][2])
+    {
+        accumulate(vt, pf, [](int) {});
     }
 
     // Whether a tile holds an infinite or NaN value (this wave looks at part

@@ -77,7 +77,7 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void scored_attn_kernel(ScoredArgs
     constexpr int TILE_BYTES = kKeys * ROW_BYTES;
     constexpr int STAGE_BYTES = 2 * TILE_BYTES;  // K tile, then V tile
     constexpr int COPY_ROWS = 1024 / ROW_BYTES;  // keys of a 1 KB copy
-    constexpr int COPIES = TILE_BYTES / 1024 / NW;  // of a wave, for K and again for V
+    constexpr int COPIES = TILE_BYTES / 1024 / 4;  // of a copying wave, for K and again for V
     constexpr int D_BLOCKS = D / 32;
 
     __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * STAGE_BYTES];
@@ -185,9 +185,9 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void scored_attn_kernel(ScoredArgs
         while (n > 0 && listed(n - 1) > wr1)
             --n;
 
-    // copies: wave w takes 1 KB blocks w COPIES .. of a tile.  The swizzle of
-    // block i's rows is that of block 0's with the bits of i COPY_ROWS flipped (K;
-    // V's does not depend on them).
+    // copies: of the first four waves, wave w takes 1 KB blocks w COPIES .. of a
+    // tile.  The swizzle of block i's rows is that of block 0's with the bits of
+    // i COPY_ROWS flipped (K; V's does not depend on them).
     const uint32_t smem_addr =
         (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
     const uint32_t pitch = (uint32_t)(a.hkv * ROW_BYTES);
@@ -198,26 +198,42 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void scored_attn_kernel(ScoredArgs
     const uint32_t kswz = (uint32_t)(((lane % CHUNKS) ^ rows_kswz<D>(dma_row)) << 4);
     const uint32_t vswz = (uint32_t)(((lane % CHUNKS) ^ rows_vswz<D>(dma_row)) << 4);
     static_assert((COPIES & (COPIES - 1)) == 0 && COPIES <= 4, "blocks of a wave differ in bits");
-    auto copy_tile = [&](const uint16_t *base, int key0, uint32_t lds, auto is_v) TA_INLINE {
-        asm volatile("" ::: "memory");
-        // rows past the sequence repeat its last one; no row keeps them
-        const int first = min(key0, seq_len - 1);
-        const uint32_t lim = (uint32_t)min(seq_len - 1 - first, kKeys - 1) * pitch;
-        const uint16_t *from = base + (int64_t)first * a.hkv * D;
+    // Where a step's keys are.  Rows past the sequence repeat its last one; no
+    // row keeps them.
+    struct Place {
+        int key0;
+        bool masked;   // some row of the workgroup drops keys of it
+        uint32_t lim;  // byte offset of the tile's last row
+        int64_t off;   // elements to its first row
+    };
+    auto place = [&](int i) TA_INLINE -> Place {
+        Place x;
+        x.key0 = step_key(i);
+        x.masked = (x.key0 + kKeys - 1 > wr0) |
+                   (stream & (x.key0 + kKeys - 1 >= a.sink) & (wr1 - x.key0 >= a.window));
+        const int first = min(x.key0, seq_len - 1);
+        x.lim = (uint32_t)min(seq_len - 1 - first, kKeys - 1) * pitch;
+        x.off = (int64_t)first * a.hkv * D;
+        return x;
+    };
+    // block i of this wave, K or V
+    auto copy_block = [&](const Place &x, int i, int stage, auto is_v) TA_INLINE {
+        constexpr bool V = decltype(is_v)::value;
+        const uint32_t swz = V ? vswz : kswz ^ (uint32_t)(rows_kswz<D>(i * COPY_ROWS) << 4);
+        copy_to_lds16((V ? vbase : kbase) + x.off,
+                      min(dma_off + (uint32_t)(i * COPY_ROWS) * pitch, x.lim) + swz,
+                      smem_addr + stage * STAGE_BYTES + (V ? TILE_BYTES : 0) +
+                          (wave * COPIES + i) * 1024);
+    };
+    auto copy_k = [&](const Place &x, int stage) TA_INLINE {
 #pragma unroll
-        for (int i = 0; i < COPIES; ++i) {
-            const uint32_t swz =
-                decltype(is_v)::value ? vswz : kswz ^ (uint32_t)(rows_kswz<D>(i * COPY_ROWS) << 4);
-            copy_to_lds16(from, min(dma_off + (uint32_t)(i * COPY_ROWS) * pitch, lim) + swz,
-                          lds + (wave * COPIES + i) * 1024);
-        }
-        asm volatile("" ::: "memory");
+        for (int i = 0; i < COPIES; ++i)
+            copy_block(x, i, stage, std::false_type{});
     };
-    auto copy_k = [&](int key0, int stage) TA_INLINE {
-        copy_tile(kbase, key0, smem_addr + stage * STAGE_BYTES, std::false_type{});
-    };
-    auto copy_v = [&](int key0, int stage) TA_INLINE {
-        copy_tile(vbase, key0, smem_addr + stage * STAGE_BYTES + TILE_BYTES, std::true_type{});
+    auto copy_v = [&](const Place &x, int stage) TA_INLINE {
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i)
+            copy_block(x, i, stage, std::true_type{});
     };
     auto end_phase = [&](bool copies) TA_INLINE {
         __builtin_amdgcn_sched_barrier(0);
@@ -230,11 +246,6 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void scored_attn_kernel(ScoredArgs
     f32x16 s[2];
     bf16x8 p[2][2];
     bool fresh, odd;
-    // Whether some row of the workgroup drops keys of a step.
-    auto any_mask = [&](int key0) TA_INLINE -> bool {
-        return (key0 + kKeys - 1 > wr0) |
-               (stream & (key0 + kKeys - 1 >= a.sink) & (wr1 - key0 >= a.window));
-    };
     // Keys that this wave's rows drop (three comparisons a score only where a
     // step holds more than one of the edges).
     auto mask = [&](int key0) TA_INLINE {
@@ -263,27 +274,27 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void scored_attn_kernel(ScoredArgs
             keep([&](int off) TA_INLINE { return (off <= lim) & ((off > far) | (off < sinks)); });
     };
     // X(j): the scores of step j to probabilities
-    auto softmax = [&](int key0) TA_INLINE {
+    auto softmax = [&](const Place &x) TA_INLINE {
         rb.modify(s, a.score);
-        if (__builtin_expect(any_mask(key0), 0)) {
+        if (__builtin_expect(x.masked, 0)) {
             asm volatile("");  // a branch: most steps have no mask
-            mask(key0);
+            mask(x.key0);
         }
-        rb.softmax(s, a.score, slope, key0 - row, p, fresh);
+        rb.softmax(s, a.score, slope, x.key0 - row, p, fresh);
         fresh = false;
     };
     // The values of a masked step, each wave its part of the tile (apart from
     // the common path).
-    auto look = [&](int key0, const unsigned char *vt) TA_INLINE {
-        if (__builtin_expect(any_mask(key0), 0)) {
+    auto look = [&](const Place &x, const unsigned char *vt) TA_INLINE {
+        if (__builtin_expect(x.masked, 0)) {
             asm volatile("");
             odd |= rb.odd_values(vt, lane, wave, NW);
         }
         __builtin_amdgcn_sched_barrier(0);
     };
     // O += V P of the step whose probabilities p holds
-    auto values = [&](int key0, const unsigned char *vt) TA_INLINE {
-        look(key0, vt);
+    auto values = [&](const Place &x, const unsigned char *vt) TA_INLINE {
+        look(x, vt);
         rb.accumulate(vt, p);
         rb.template schedule<false, true>();
         __builtin_amdgcn_sched_barrier(0);
@@ -302,28 +313,32 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void scored_attn_kernel(ScoredArgs
     // keep their keys; otherwise `odd` tells whether a masked step holds any.
     auto together = [&](auto careful) TA_INLINE {
         constexpr bool CAREFUL = decltype(careful)::value;
-        auto copies = [&](int i, int stage) TA_INLINE {
-            copy_k(step_key(i), stage);
-            copy_v(step_key(i), stage);
+        Place now = place(0);
+        auto copies = [&](const Place &x, int stage) TA_INLINE {
+            if (NW == 4 || wave < 4) {
+                copy_k(x, stage);
+                copy_v(x, stage);
+            }
         };
-        copies(0, 0);
+        copies(now, 0);
         auto step = [&](int i, auto stage) TA_INLINE {
             constexpr int ST = decltype(stage)::value;
             // this step's tile has landed for every wave, and every wave is
             // done with the other stage
             end_phase(true);
+            const Place next = place(min(i + 1, n - 1));
             if (i + 1 < n)
-                copies(i + 1, 1 - ST);
-            __builtin_amdgcn_sched_barrier(0);
+                copies(next, 1 - ST);
             const unsigned char *kt = smem + ST * STAGE_BYTES;
             products(kt);
-            softmax(step_key(i));
+            softmax(now);
             if (!CAREFUL)
-                values(step_key(i), kt + TILE_BYTES);
-            else if (any_mask(step_key(i)))
+                values(now, kt + TILE_BYTES);
+            else if (now.masked)
                 rb.accumulate_by_key(kt + TILE_BYTES, p);
             else
                 rb.accumulate(kt + TILE_BYTES, p);
+            now = next;
         };
         int i = 0;
         for (; i + 1 < n; i += 2) {
@@ -338,39 +353,54 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void scored_attn_kernel(ScoredArgs
     // cores beside the other group's X(j) on the vector units.  Group 0 runs
     // M(j) in phase 2 j and X(j) in phase 2 j + 1, group 1 X(j - 1) in phase 2 j
     // and M(j) in phase 2 j + 1.  Stage j & 1 holds K(j) and V(j - 1) in these
-    // two phases; K(j + 1) and V(j) are copied into the other one, last read in
-    // phase 2 j - 1, from phase 2 j on.
+    // two phases; group 0 copies K(j + 1) and V(j) into the other one, last read
+    // in phase 2 j - 1, spread over the MFMAs of M(j): issue slots that are free
+    // there.
     auto in_turns = [&]() TA_INLINE {
-        auto matrix = [&](int j, auto stage) TA_INLINE {
+        constexpr int NQ = 2 * (D / 16);        // MFMAs of products()
+        constexpr int SLOTS = NQ + 4 * (D / 32);  // and of accumulate()
+        constexpr int STRIDE = SLOTS / (2 * COPIES);
+        Place prev, now = place(0), next = place(min(1, n - 1));
+        auto matrix = [&](auto stage, auto &&hook) TA_INLINE {
             const unsigned char *kt = smem + decltype(stage)::value * STAGE_BYTES;
-            look(step_key(j - 1), kt + TILE_BYTES);
+            look(prev, kt + TILE_BYTES);
             __builtin_amdgcn_s_setprio(1);
             __builtin_amdgcn_sched_barrier(0);
-            rb.products(kt, s);
-            rb.accumulate(kt + TILE_BYTES, p);
+            rb.products(kt, s, hook);
+            rb.accumulate(kt + TILE_BYTES, p, [&](int i) TA_INLINE { hook(NQ + i); });
             rb.template schedule<true, true>();
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(0);
         };
-        auto copies = [&](int j, int stage) TA_INLINE {
-            copy_k(step_key(min(j + 1, n - 1)), 1 - stage);
-            copy_v(step_key(j), 1 - stage);
-            __builtin_amdgcn_sched_barrier(0);
+        auto advance = [&](int j) TA_INLINE {  // to step j
+            prev = now;
+            now = next;
+            next = place(min(j + 1, n - 1));
         };
-        copy_k(step_key(0), 0);
-        end_phase(true);
-        copies(0, 0);
         int j = 1;
         if (wave < 4) {
+            copy_k(now, 0);
+            end_phase(true);
+            copy_k(next, 1);
+            copy_v(now, 1);
             products(smem);
             end_phase(false);
-            softmax(step_key(0));
+            softmax(now);
             end_phase(true);
             auto step = [&](int j, auto stage) TA_INLINE {
-                copies(j, decltype(stage)::value);
-                matrix(j, stage);
+                constexpr int OTHER = 1 - decltype(stage)::value;
+                advance(j);
+                matrix(stage, [&](int i) TA_INLINE {
+                    if (i % STRIDE == STRIDE - 1) {
+                        const int c = i / STRIDE;
+                        if (c < COPIES)
+                            copy_block(next, c, OTHER, std::false_type{});
+                        else if (c < 2 * COPIES)
+                            copy_block(now, c - COPIES, OTHER, std::true_type{});
+                    }
+                });
                 end_phase(false);
-                softmax(step_key(j));
+                softmax(now);
                 end_phase(true);
             };
             for (; j + 1 < n; j += 2) {
@@ -379,19 +409,20 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void scored_attn_kernel(ScoredArgs
             }
             if (j < n)
                 step(j, Stage1{});
-            values(step_key(n - 1), smem + (n & 1) * STAGE_BYTES + TILE_BYTES);
+            values(now, smem + (n & 1) * STAGE_BYTES + TILE_BYTES);
             end_phase(false);
             end_phase(false);
         } else {
             end_phase(false);
+            end_phase(false);
             products(smem);
-            end_phase(true);
+            end_phase(false);
             auto step = [&](int j, auto stage) TA_INLINE {
-                copies(j, decltype(stage)::value);
-                softmax(step_key(j - 1));
+                softmax(now);
                 end_phase(false);
-                matrix(j, stage);
-                end_phase(true);
+                advance(j);
+                matrix(stage, [](int) {});
+                end_phase(false);
             };
             for (; j + 1 < n; j += 2) {
                 step(j, Stage1{});
@@ -399,9 +430,9 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void scored_attn_kernel(ScoredArgs
             }
             if (j < n)
                 step(j, Stage1{});
-            softmax(step_key(n - 1));
+            softmax(now);
             end_phase(false);
-            values(step_key(n - 1), smem + (n & 1) * STAGE_BYTES + TILE_BYTES);
+            values(now, smem + (n & 1) * STAGE_BYTES + TILE_BYTES);
             end_phase(false);
         }
     };
