@@ -33,16 +33,17 @@ int page_log2(int32_t page_size);  // triattn_cache.hip
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kJoinThreads = 256;
 constexpr int kMaxTiles = 2048;    // row tiles of a kv head
 constexpr int kPageEntries = 512;  // page ids held in LDS at a time
 constexpr int kCus = 256;
 
-// Words of the record that the own-keys pass leaves for the join: a header,
-// then one entry a row tile.
+// Words of the record that the own-keys pass leaves for the join: a header, one
+// entry a row tile, and for each share the row tile that the share's start is
+// the first to cut (-1: none).
 constexpr int kMetaWords = 8;
-enum MetaHeader { MH_BAD = 0, MH_TILES, MH_SHARE };
-enum MetaField { MF_Q0 = 0, MF_RHO0, MF_ROWS, MF_POS0, MF_BEGIN, MF_END, MF_BAD };
+enum MetaHeader { MH_TILES = 0, MH_SHARE };
+enum MetaField { MF_Q0 = 0, MF_RHO0, MF_ROWS, MF_POS0, MF_BEGIN, MF_END };
 
 struct PagedArgs {
     const uint16_t *q, *kc, *vc;
@@ -61,27 +62,36 @@ struct PagedArgs {
     int32_t o_f32;
 };
 
+__device__ __forceinline__ int32_t *meta_cuts(int32_t *meta, int max_tiles)
+{
+    return meta + kMetaWords * (max_tiles + 1);
+}
+
 // Shapes of the two forms of the pass.
-//   RB = 1: up to 32 rows.  Each wave takes every fourth 32-key tile of a
-//     step into its own LDS stages and keeps its own softmax; nothing waits on
-//     another wave until the four are joined at the end of a piece.
-//   RB = 4: four waves of 32 rows each over the same 64-key tiles.
+//   RB = 1: up to 32 rows, bound by the bytes of K and V.  Two waves take 32-key
+//     tiles in turn, each into two stages of its own, and keep their own softmax:
+//     nothing waits on the other wave until they are joined at the end of a
+//     piece.  64 KB of stages at d = 128 let two workgroups share a CU, so that one
+//     loads while the other finds its next request or joins its waves.
+//   RB = 4: four waves of 32 rows each over the same 64-key tiles, in two stages.
 template <int D, int RB>
 struct PagedShape {
     static constexpr int NKB = RB == 4 ? 2 : 1;
     static constexpr int TK = 32 * NKB;      // keys of a tile
-    static constexpr int KS = 4 / RB;        // key splits of a workgroup
+    static constexpr int KS = RB == 4 ? 1 : 2;  // key splits of a workgroup
+    static constexpr int THREADS = 64 * RB * KS;
     static constexpr int STEP = TK * KS;     // keys of a step
     static constexpr int ROWS = 32 * RB;
     static constexpr int TILE_BYTES = TK * 2 * D;
     static constexpr int STAGE_BYTES = 2 * TILE_BYTES;  // K tile, then V tile
     static constexpr int LDS_BYTES = KS * 2 * STAGE_BYTES;
-    static constexpr int WGS_PER_CU = LDS_BYTES > 65536 ? 1 : 2;
+    static constexpr int WGS_PER_CU = RB == 1 && D == 64 ? 3 : 2;
+    static constexpr int WAVES_PER_SIMD = (WGS_PER_CU * THREADS / 64 + 3) / 4;
 };
 
 // Exclusive scan of val(i), i < n, into out[0 .. n] (out[n]: the total) by
-// the workgroup, n <= 8 kThreads.
-template <typename F>
+// the workgroup.
+template <int kThreads, typename F>
 __device__ __forceinline__ void block_scan(int n, int32_t *out, int32_t *wave_sum, F &&val)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -139,15 +149,17 @@ struct RowTile {
 };
 
 template <int D, int RB, int SCORE, bool PREFIX>
-__global__ __launch_bounds__(kThreads, (PagedShape<D, RB>::WGS_PER_CU)) void paged_attn_kernel(PagedArgs a)
+__global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
+                             (PagedShape<D, RB>::WAVES_PER_SIMD)) void paged_attn_kernel(PagedArgs a)
 {
     using S = PagedShape<D, RB>;
+    constexpr int kThreads = S::THREADS;
     constexpr int ROW_BYTES = 2 * D;
     constexpr int CHUNKS = D / 8;
     constexpr int COPY_ROWS = 1024 / ROW_BYTES;          // keys of a 1 KB copy
-    constexpr int TILE_COPIES = S::TILE_BYTES / 1024;    // copies of a K (or V) tile
-    constexpr int COPY_WAVES = RB;                       // waves that share a tile's copies
-    constexpr int COPIES = TILE_COPIES / COPY_WAVES;     // of a wave, for K and again for V
+    constexpr int GROUP = 16;  // keys that surely share a page
+    constexpr int COPIES = GROUP / COPY_ROWS;              // 1 KB copies of a group
+    constexpr int GROUPS = S::TK / GROUP / (RB == 4 ? 4 : 1);  // of a wave and tile
     constexpr int D_BLOCKS = D / 32;
 
     __shared__ __attribute__((aligned(1024))) unsigned char smem[S::LDS_BYTES];
@@ -155,7 +167,7 @@ __global__ __launch_bounds__(kThreads, (PagedShape<D, RB>::WGS_PER_CU)) void pag
     __shared__ int32_t s_step[PREFIX ? 1 : kMaxTiles + 1];    // first step of a row tile
     __shared__ int32_t s_page[kPageEntries];
     __shared__ int32_t s_wave[kThreads / 64];
-    __shared__ float s_ml[RB == 1 ? 4 : 1][32][2];
+    __shared__ float s_ml[S::KS][32][2];
     __shared__ int32_t s_bad;
 
     const int tid = threadIdx.x;
@@ -194,7 +206,7 @@ __global__ __launch_bounds__(kThreads, (PagedShape<D, RB>::WGS_PER_CU)) void pag
                 nq = a.cu_q[r.req + 1] - r.q0;
                 r.rho0 = (t - s_req[r.req]) * S::ROWS;
             }
-            int32_t kv = a.kv_lens[r.req];
+            int32_t kv = a.cu_q ? a.kv_lens[r.req] : s_req[t];
             r.bad = kv > (a.width << a.page_log2);
             kv = r.bad ? 0 : max(kv, 0);
             r.rows = min(S::ROWS, nq * a.group - r.rho0);
@@ -213,7 +225,7 @@ __global__ __launch_bounds__(kThreads, (PagedShape<D, RB>::WGS_PER_CU)) void pag
                 s_bad = 0;
             __syncthreads();
             bool bad = tid == 0 && (a.cu_q[0] != 0);
-            block_scan(a.batch, s_req, s_wave, [&](int b) TA_INLINE -> int32_t {
+            block_scan<kThreads>(a.batch, s_req, s_wave, [&](int b) TA_INLINE -> int32_t {
                 const int32_t b0 = a.cu_q[b], b1 = a.cu_q[b + 1];
                 if (b0 < 0 || b1 < b0 || b1 > a.total_tokens) {
                     bad = true;
@@ -227,24 +239,29 @@ __global__ __launch_bounds__(kThreads, (PagedShape<D, RB>::WGS_PER_CU)) void pag
             n_tiles = uni(s_req[a.batch]);
             // query offsets that are none: nothing is computed, NaN shows it
             if (s_bad != 0 || n_tiles > a.max_tiles) {
-                if (blockIdx.x == 0 && tid == 0) {
-                    a.meta[MH_BAD] = 1;
-                    a.meta[MH_TILES] = 0;
+                if (g == 0 && tid == 0) {
+                    meta_cuts(a.meta, a.max_tiles)[slot] = -1;
+                    if (slot == 0)
+                        a.meta[MH_TILES] = 0;
                 }
                 rows_poison(a.o, a.o_f32, a.lse, (int64_t)a.total_tokens * a.hq, D);
                 return;
             }
         }
-        block_scan(n_tiles, s_step, s_wave, [&](int t) TA_INLINE -> int32_t {
+        block_scan<kThreads>(n_tiles, s_step, s_wave, [&](int t) TA_INLINE -> int32_t {
+            if (!a.cu_q)
+                s_req[t] = a.kv_lens[t];  // (no row tiles to count: the lengths)
             return (tile_of(t).limit + S::STEP - 1) / S::STEP;
         });
         total = uni(s_step[n_tiles]);
     }
     const int share = max(1, (total + a.slots - 1) / a.slots);
+    const int share0 = slot * share;
+    const int share1 = min(total, share0 + share);
     if constexpr (!PREFIX) {
+        // the record for the join
         if (blockIdx.x == 0) {
             if (tid == 0) {
-                a.meta[MH_BAD] = 0;
                 a.meta[MH_TILES] = n_tiles;
                 a.meta[MH_SHARE] = share;
             }
@@ -257,21 +274,51 @@ __global__ __launch_bounds__(kThreads, (PagedShape<D, RB>::WGS_PER_CU)) void pag
                 m[MF_POS0] = r.pos0;
                 m[MF_BEGIN] = s_step[t];
                 m[MF_END] = s_step[t + 1];
-                m[MF_BAD] = r.bad;
+            }
+        }
+        if (g == 0 && tid == 0) {
+            int cut = -1;
+            if (share0 < total) {
+                const int t = find_start(s_step, n_tiles, share0);
+                if (s_step[t] < share0 && s_step[t] >= share0 - share)
+                    cut = t;
+            }
+            meta_cuts(a.meta, a.max_tiles)[slot] = cut;
+        }
+        // rows without keys, shared out over the slots
+        for (int t = slot; t < n_tiles; t += a.slots) {
+            if (s_step[t] != s_step[t + 1])
+                continue;
+            const RowTile r = tile_of(t);
+            const float o = r.bad ? __builtin_nanf("") : 0.f;
+            for (int i = tid; i < r.rows * D; i += kThreads) {
+                const int rho = r.rho0 + i / D, qt = div_group(rho);
+                const int h = g * a.group + rho - qt * a.group;
+                const int64_t at = ((int64_t)(r.q0 + qt) * a.hq + h) * D + i % D;
+                if (a.o_f32)
+                    static_cast<float *>(a.o)[at] = o;
+                else
+                    static_cast<__bf16 *>(a.o)[at] = (__bf16)o;
+                if (a.lse && i % D == 0)
+                    a.lse[(int64_t)h * a.total_tokens + r.q0 + qt] = r.bad ? o : -INFINITY;
             }
         }
     }
-    const int share0 = slot * share;
-    const int share1 = min(total, share0 + share);
-    if (slot > 0 && share0 >= total)
+    if (share0 >= total)
         return;
 
     const uint32_t smem_addr =
         (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
-    // this wave's stages (RB = 1) or the workgroup's (RB = 4)
+    // this wave's buffers (RB = 1) or the workgroup's stages (RB = 4)
     const int wave_lds = RB == 1 ? wave * 2 * S::STAGE_BYTES : 0;
-    const int copy_rank = RB == 1 ? 0 : wave;
-    const int dma_row = lane / CHUNKS, dma_chunk = lane % CHUNKS;
+    const int first_group = RB == 1 ? 0 : wave * GROUPS;
+    const int dma_row = lane / CHUNKS;
+    // a copying lane's place in a group's first block; block m flips the K
+    // swizzle's bits of m COPY_ROWS
+    const uint32_t dma_k =
+        (uint32_t)(dma_row * ROW_BYTES + (((lane % CHUNKS) ^ rows_kswz<D>(dma_row)) << 4));
+    const uint32_t dma_v =
+        (uint32_t)(dma_row * ROW_BYTES + (((lane % CHUNKS) ^ rows_vswz<D>(dma_row)) << 4));
     const int64_t page_stride = ((int64_t)a.hkv << a.page_log2) * ROW_BYTES;
     const int64_t head_off = ((int64_t)g << a.page_log2) * ROW_BYTES;
     const unsigned char *kc = reinterpret_cast<const unsigned char *>(a.kc) + head_off;
@@ -343,12 +390,17 @@ __global__ __launch_bounds__(kThreads, (PagedShape<D, RB>::WGS_PER_CU)) void pag
         bool fresh = true, odd = false;
         rb.reset();
         const int seg_steps = (((kPageEntries - 1) << a.page_log2) / S::STEP);
-        for (int seg0 = step0; seg0 < step1; seg0 += seg_steps) {
+        const int n_segs = (step1 - step0 + seg_steps - 1) / seg_steps;
+        // where scores fall with the distance, the last keys come first: their
+        // scores are the largest, and the rows' references stand
+        constexpr bool BACK = (SCORE & kScoreSlope) != 0;
+        for (int sg = 0; sg < n_segs; ++sg) {
+            const int seg0 = step0 + (BACK ? n_segs - 1 - sg : sg) * seg_steps;
             const int seg1 = min(step1, seg0 + seg_steps);
             const int key_end = min(seg1 * S::STEP, rt.limit);
             const int page0 = (seg0 * S::STEP) >> a.page_log2;
             const int n_pages = ((key_end - 1) >> a.page_log2) + 1 - page0;
-            __syncthreads();  // the last segment's ids, and stages, are done with
+            __syncthreads();  // the last segment's ids, and buffers, are done with
             for (int i = tid; i < n_pages; i += kThreads) {
                 int32_t id = pages[page0 + i];
                 if (id < 0 || id >= a.num_pages) {
@@ -359,116 +411,149 @@ __global__ __launch_bounds__(kThreads, (PagedShape<D, RB>::WGS_PER_CU)) void pag
             }
             __syncthreads();
 
-            // Copies of one tile's K and V rows into a stage.  Keys from
-            // rt.limit on repeat the last one before it; they lie past every
-            // row's last key.
-            auto copy_tile = [&](int key0, int stage) TA_INLINE {
+            // This wave's copies of a tile's K or V rows.  Keys from rt.limit on
+            // repeat the last one before it; they lie past every row's last
+            // key.
+            auto copy = [&](int key0, uint32_t lds, auto is_v) TA_INLINE {
+                constexpr bool V = decltype(is_v)::value;
                 asm volatile("" ::: "memory");
-                const uint32_t lds =
-                    smem_addr + wave_lds + stage * S::STAGE_BYTES + copy_rank * COPIES * 1024;
-                // lane i of the first COPIES holds the page of this wave's copy i
-                const int mine = min(key0 + (copy_rank * COPIES + (lane & (COPIES - 1))) * COPY_ROWS,
-                                     rt.limit - 1);
+                // lane i of the first GROUPS holds the page of this wave's group i
+                const int mine =
+                    min(key0 + (first_group + (lane & (GROUPS - 1))) * GROUP, rt.limit - 1);
                 const int ids = s_page[(mine >> a.page_log2) - page0];
+                const bool inside = key0 + S::TK <= rt.limit;
 #pragma unroll
-                for (int i = 0; i < COPIES; ++i) {
-                    const int m = copy_rank * COPIES + i;
-                    int key = key0 + m * COPY_ROWS;
-                    const int over = rt.limit - 1 - key;  // keys after the first
-                    int lim = min(over, COPY_ROWS - 1);
-                    if (over < 0) {
-                        key = rt.limit - 1;
-                        lim = 0;
+                for (int i = 0; i < GROUPS; ++i) {
+                    const int gr = first_group + i;
+                    const int key = key0 + gr * GROUP;
+                    const unsigned char *page =
+                        (V ? vc : kc) + (int64_t)__builtin_amdgcn_readlane(ids, i) * page_stride;
+                    const uint32_t to = smem_addr + lds + gr * GROUP * ROW_BYTES;
+                    uint32_t off[COPIES];
+#pragma unroll
+                    for (int m = 0; m < COPIES; ++m)
+                        off[m] = V ? dma_v : dma_k ^ (uint32_t)(rows_kswz<D>(m * COPY_ROWS) << 4);
+                    if (inside) {
+                        copy_burst_to_lds16<COPIES>(page + (key & page_mask) * ROW_BYTES, off, to);
+                    } else {
+#pragma unroll
+                        for (int m = 0; m < COPIES; ++m) {
+                            const int first = min(key + m * COPY_ROWS, rt.limit - 1);
+                            const int lim = rt.limit - 1 - first;  // rows after the first
+                            copy_to_lds16(page + (first & page_mask) * ROW_BYTES,
+                                          off[m] - (uint32_t)(max(dma_row - lim, 0) * ROW_BYTES),
+                                          to + m * 1024);
+                        }
                     }
-                    const int64_t id = __builtin_amdgcn_readlane(ids, i);
-                    const int64_t off =
-                        id * page_stride + (int64_t)((key & page_mask) * ROW_BYTES);
-                    const int r = m * COPY_ROWS + dma_row;
-                    const uint32_t row_off = (uint32_t)(min(dma_row, lim) * ROW_BYTES);
-                    copy_to_lds16(kc + off, row_off + ((dma_chunk ^ rows_kswz<D>(r)) << 4),
-                                  lds + i * 1024);
-                    copy_to_lds16(vc + off, row_off + ((dma_chunk ^ rows_vswz<D>(r)) << 4),
-                                  lds + S::TILE_BYTES + i * 1024);
                 }
                 asm volatile("" ::: "memory");
             };
-            auto compute_tile = [&](int key0, auto stage) TA_INLINE {
-                const unsigned char *kt =
-                    smem + wave_lds + decltype(stage)::value * S::STAGE_BYTES;
-                f32x16 s[S::NKB];
-                bf16x8 p[S::NKB][2];
-                rb.products(kt, s);
+            using K = std::false_type;
+            using V = std::true_type;
+            f32x16 s[S::NKB];
+            bf16x8 p[S::NKB][2];
+            auto softmax = [&](int key0) TA_INLINE {
                 rb.modify(s, a.score);
-                const bool masked = key0 + S::TK - 1 > first_last;
-                if (__builtin_expect(masked, 0)) {
+                if (__builtin_expect(key0 + S::TK - 1 > first_last, 0)) {
                     asm volatile("");  // a branch: most steps have no mask
-                    odd |= rb.odd_values(kt + S::TILE_BYTES, lane, 0, 1);
                     rb.mask_above(s, last - key0);
                 }
                 rb.softmax(s, a.score, slope, key0 - dist_row, p, fresh);
                 fresh = false;
-                if (CAREFUL && masked)
-                    rb.accumulate_by_key(kt + S::TILE_BYTES, p);
-                else
-                    rb.accumulate(kt + S::TILE_BYTES, p);
             };
-            using Stage0 = std::integral_constant<int, 0>;
-            using Stage1 = std::integral_constant<int, 1>;
+            auto values = [&](int key0, const unsigned char *vt) TA_INLINE {
+                const bool masked = key0 + S::TK - 1 > first_last;
+                if (__builtin_expect(masked, 0)) {
+                    asm volatile("");
+                    odd |= rb.odd_values(vt, lane, RB == 1 ? 0 : wave, RB);
+                }
+                if (CAREFUL && masked) {
+                    rb.accumulate_by_key(vt, p);
+                } else {
+                    __builtin_amdgcn_sched_barrier(0);
+                    rb.accumulate(vt, p);
+                    rb.template schedule<false, true>();
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            };
+            auto products = [&](const unsigned char *kt) TA_INLINE {
+                __builtin_amdgcn_sched_barrier(0);
+                rb.products(kt, s);
+                rb.template schedule<true, false>();
+                __builtin_amdgcn_sched_barrier(0);
+            };
             if constexpr (RB == 1) {
-                // tiles of this wave: key0 = step STEP + wave TK, two stages
+                // tiles of this wave: key0 = step STEP + wave TK
                 const int base = seg0 * S::STEP + wave * S::TK;
                 const int n = base < key_end ? (key_end - base + S::STEP - 1) / S::STEP : 0;
+                auto key_of = [&](int i) TA_INLINE -> int {
+                    return base + (BACK ? n - 1 - i : i) * S::STEP;
+                };
+                auto copies = [&](int key0, int stage) TA_INLINE {
+                    copy(key0, wave_lds + stage * S::STAGE_BYTES, K{});
+                    copy(key0, wave_lds + stage * S::STAGE_BYTES + S::TILE_BYTES, V{});
+                    __builtin_amdgcn_sched_barrier(0);
+                };
                 if (n > 0)
-                    copy_tile(base, 0);
+                    copies(key_of(0), 0);
                 if (n > 1)
-                    copy_tile(base + S::STEP, 1);
+                    copies(key_of(1), 1);
                 auto step = [&](int i, auto stage) TA_INLINE {
+                    constexpr int ST = decltype(stage)::value;
+                    const unsigned char *kt = smem + wave_lds + ST * S::STAGE_BYTES;
                     if (i + 1 < n)
-                        rows_wait_copies<2 * COPIES>();
+                        rows_wait_copies<2 * GROUPS * COPIES>();
                     else
                         rows_wait_copies<0>();
-                    __builtin_amdgcn_sched_barrier(0);
-                    compute_tile(base + i * S::STEP, stage);
-                    __builtin_amdgcn_sched_barrier(0);
+                    products(kt);
+                    softmax(key_of(i));
+                    values(key_of(i), kt + S::TILE_BYTES);
                     if (i + 2 < n) {
                         // every read of the stage has returned before it is
                         // written again
                         __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
-                        copy_tile(base + (i + 2) * S::STEP, stage);
-                        __builtin_amdgcn_sched_barrier(0);
+                        copies(key_of(i + 2), ST);
                     }
                 };
                 int i = 0;
                 for (; i + 1 < n; i += 2) {
-                    step(i, Stage0{});
-                    step(i + 1, Stage1{});
+                    step(i, std::integral_constant<int, 0>{});
+                    step(i + 1, std::integral_constant<int, 1>{});
                 }
                 if (i < n)
-                    step(i, Stage0{});
+                    step(i, std::integral_constant<int, 0>{});
             } else {
                 const int n = (key_end - seg0 * S::STEP + S::STEP - 1) / S::STEP;
-                copy_tile(seg0 * S::STEP, 0);
+                auto key_of = [&](int i) TA_INLINE -> int {
+                    return (seg0 + (BACK ? n - 1 - i : i)) * S::STEP;
+                };
+                auto copies = [&](int key0, int stage) TA_INLINE {
+                    copy(key0, stage * S::STAGE_BYTES, K{});
+                    copy(key0, stage * S::STAGE_BYTES + S::TILE_BYTES, V{});
+                };
+                copies(key_of(0), 0);
                 auto step = [&](int i, auto stage) TA_INLINE {
+                    constexpr int ST = decltype(stage)::value;
                     // this step's tile has landed for every wave, and every
                     // wave is done with the other stage
                     __builtin_amdgcn_sched_barrier(0);
                     rows_wait_copies<0>();
                     barrier_no_fence();
                     __builtin_amdgcn_sched_barrier(0);
-                    const int key0 = (seg0 + i) * S::STEP;
                     if (i + 1 < n)
-                        copy_tile(key0 + S::STEP, 1 - decltype(stage)::value);
-                    __builtin_amdgcn_sched_barrier(0);
-                    compute_tile(key0, stage);
-                    __builtin_amdgcn_sched_barrier(0);
+                        copies(key_of(i + 1), 1 - ST);
+                    const unsigned char *kt = smem + ST * S::STAGE_BYTES;
+                    products(kt);
+                    softmax(key_of(i));
+                    values(key_of(i), kt + S::TILE_BYTES);
                 };
                 int i = 0;
                 for (; i + 1 < n; i += 2) {
-                    step(i, Stage0{});
-                    step(i + 1, Stage1{});
+                    step(i, std::integral_constant<int, 0>{});
+                    step(i + 1, std::integral_constant<int, 1>{});
                 }
                 if (i < n)
-                    step(i, Stage0{});
+                    step(i, std::integral_constant<int, 0>{});
             }
         }
         return odd;
@@ -508,9 +593,13 @@ __global__ __launch_bounds__(kThreads, (PagedShape<D, RB>::WGS_PER_CU)) void pag
         __syncthreads();  // the stages are done with, and s_bad is final
         const float nan_if_bad = s_bad != 0 ? __builtin_nanf("") : 0.f;
         if constexpr (RB == 1) {
-            // join the four waves: each leaves its accumulators in its stages
-            constexpr int PITCH = 4 * D + 16;
+            // join the waves: each leaves its accumulators in its buffers,
+            // 16-byte chunks of row r permuted by r against bank conflicts
+            constexpr int PITCH = 4 * D;
             static_assert(32 * PITCH <= 2 * S::STAGE_BYTES, "accumulators fit the wave's stages");
+            auto place = [&](int r, int chunk) TA_INLINE -> int {
+                return r * PITCH + ((chunk ^ (r & (D / 4 - 1))) << 4);
+            };
             unsigned char *mine = smem + wave * 2 * S::STAGE_BYTES;
             const float l = rows_pair_sum(rb.l_run);
             if (rb.col < rt.rows) {
@@ -526,8 +615,8 @@ __global__ __launch_bounds__(kThreads, (PagedShape<D, RB>::WGS_PER_CU)) void pag
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             x[e] = rb.oacc[b][4 * c + e];
-                        *reinterpret_cast<f32x4r *>(mine + rb.col * PITCH +
-                                                    (32 * b + 8 * c + 4 * rb.half) * 4) = x;
+                        *reinterpret_cast<f32x4r *>(
+                            mine + place(rb.col, 8 * b + 2 * c + rb.half)) = x;
                     }
             }
             __syncthreads();
@@ -535,17 +624,17 @@ __global__ __launch_bounds__(kThreads, (PagedShape<D, RB>::WGS_PER_CU)) void pag
                 const int r = i / (D / 4), d0 = 4 * (i % (D / 4));
                 float m = -INFINITY;
 #pragma unroll
-                for (int w = 0; w < 4; ++w)
+                for (int w = 0; w < S::KS; ++w)
                     m = fmaxf(m, s_ml[w][r][0]);
                 const float m_use = m == -INFINITY ? 0.f : m;
                 float den = 0.f;
                 f32x4r x{};
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
+                for (int w = 0; w < S::KS; ++w) {
                     const float f = __builtin_amdgcn_exp2f(s_ml[w][r][0] - m_use);
                     den += f * s_ml[w][r][1];
                     const f32x4r y = *reinterpret_cast<const f32x4r *>(
-                        smem + w * 2 * S::STAGE_BYTES + r * PITCH + d0 * 4);
+                        smem + w * 2 * S::STAGE_BYTES + place(r, d0 / 4));
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         x[e] += f * y[e];
@@ -584,127 +673,124 @@ __global__ __launch_bounds__(kThreads, (PagedShape<D, RB>::WGS_PER_CU)) void pag
 struct JoinArgs {
     void *o;
     float *lse;
-    const int32_t *meta;
+    int32_t *meta;
     const float *slot_o, *slot_lse;
-    int32_t tile_rows;
+    int32_t tile_rows, max_tiles, slots;
+    int32_t chunks, chunk_rows;  // workgroups of a row tile, rows of each
     // the prefix pass (prefix_len 0: none)
     const float *row_o, *row_lse;
     const float *pre_slot_o, *pre_slot_lse, *pre_row_o, *pre_row_lse;
-    int32_t prefix_len, pre_rows, pre_step, pre_slots;
+    int32_t prefix_len, pre_rows, pre_steps, pre_share;
     const float *slopes;
     int32_t total_tokens, hq, hkv, group, o_f32;
 };
 
 // Joins the partials of a row: O = sum_c w_c O_c / sum_c w_c with w_c =
 // exp(LSE_c - max_c LSE_c), the prefix's before the row's own, in key order.
-// A workgroup takes one row tile of one kv head, a wave one row at a time.
-// Row tiles that one share finished need nothing here, unless no share had
-// anything to do for them (rows without keys) or a prefix comes before.
+// With a prefix every row has partials to join; without one only the row tiles
+// that a share's start cuts, which the shares name.  A wave takes a row at a
+// time, its lanes the log-sum-exps of up to 64 partials at once.
 template <int D>
-__global__ __launch_bounds__(kThreads) void paged_join_kernel(JoinArgs a)
+__global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(JoinArgs a)
 {
     constexpr int PER = D / 64;
-    if (a.meta[MH_BAD]) {
-        rows_poison(a.o, a.o_f32, a.lse, (int64_t)a.total_tokens * a.hq, D);
-        return;
-    }
-    const int t = blockIdx.x / a.hkv, g = blockIdx.x % a.hkv;
-    if (t >= a.meta[MH_TILES])
+    typedef float vec __attribute__((ext_vector_type(PER)));
+    const int g = blockIdx.x % a.hkv, at = blockIdx.x / a.hkv;
+    const int chunk = at % a.chunks;
+    int t = at / a.chunks;
+    const int32_t tiles = a.meta[MH_TILES], share = a.meta[MH_SHARE];
+    if (a.prefix_len == 0)
+        t = meta_cuts(a.meta, a.max_tiles)[t];
+    if (t < 0 || t >= tiles)
         return;
     const int32_t *m = a.meta + kMetaWords * (t + 1);
-    const int32_t share = a.meta[MH_SHARE];
     const int32_t q0 = m[MF_Q0], rho0 = m[MF_RHO0], rows = m[MF_ROWS], pos0 = m[MF_POS0];
-    const int32_t begin = m[MF_BEGIN], end = m[MF_END], bad = m[MF_BAD];
+    const int32_t begin = m[MF_BEGIN], end = m[MF_END];
+    if (begin == end)
+        return;  // rows without keys are written
     const int w0 = begin / share;
-    const int n_own = end > begin ? (end - 1) / share - w0 + 1 : 0;
-    if (n_own == 1 && a.prefix_len == 0)
-        return;
+    const int n_own = (end - 1) / share - w0 + 1;
     const int lane = threadIdx.x & 63;
-    const int pre_steps = a.prefix_len > 0 ? (a.prefix_len + a.pre_step - 1) / a.pre_step : 0;
-    for (int r = threadIdx.x >> 6; r < rows; r += kThreads / 64) {
+    const int r_end = min(rows, (chunk + 1) * a.chunk_rows);
+    for (int r = chunk * a.chunk_rows + (threadIdx.x >> 6); r < r_end; r += kJoinThreads / 64) {
         const int rho = rho0 + r, qt = rho / a.group, h = g * a.group + rho - qt * a.group;
         const int64_t orow = (int64_t)(q0 + qt) * a.hq + h;
         // the prefix pass's pieces of this row: its rows are those of all
         // requests, in the same order
-        int n_pre = 0, pw0 = 0, prow = 0, pshare = 1, pbegin = 0;
+        int n_pre = 0, pw0 = 0, prow = 0, pbegin = 0;
         float shift = 0.f;
         if (a.prefix_len > 0 && pos0 + qt >= 0) {
             const int prho = (q0 + qt) * a.group + rho - qt * a.group;
-            const int n_tiles = (a.total_tokens * a.group + a.pre_rows - 1) / a.pre_rows;
-            pshare = max(1, (n_tiles * pre_steps + a.pre_slots - 1) / a.pre_slots);
-            pbegin = prho / a.pre_rows * pre_steps;
+            pbegin = prho / a.pre_rows * a.pre_steps;
             prow = prho % a.pre_rows;
-            pw0 = pbegin / pshare;
-            n_pre = (pbegin + pre_steps - 1) / pshare - pw0 + 1;
-            if (a.slopes)
+            pw0 = pbegin / a.pre_share;
+            n_pre = (pbegin + a.pre_steps - 1) / a.pre_share - pw0 + 1;
+            if (a.slopes)  // its distances end at the prefix's end
                 shift = -a.slopes[h] * (float)(pos0 + qt);
         }
         const int n = n_pre + n_own;
-        auto part = [&](int c, const float *&o) TA_INLINE -> float {
+        // row of partial c: in the whole rows or the pieces of its pass
+        auto index = [&](int c) TA_INLINE -> int64_t {
             if (c < n_pre) {
-                if (n_pre == 1) {
-                    o = a.pre_row_o + orow * D;
-                    return a.pre_row_lse[orow] + shift;
-                }
                 const int w = pw0 + c;
-                const int64_t at = (((int64_t)2 * w + (pbegin > w * pshare ? 1 : 0)) * a.hkv + g) *
-                                       a.pre_rows + prow;
-                o = a.pre_slot_o + at * D;
-                return a.pre_slot_lse[at] + shift;
-            }
-            if (n_own == 1) {
-                o = a.row_o + orow * D;
-                return a.row_lse[orow];
+                return n_pre == 1 ? orow
+                                  : ((int64_t)(2 * w + (pbegin > w * a.pre_share)) * a.hkv + g) *
+                                            a.pre_rows + prow;
             }
             const int w = w0 + c - n_pre;
-            const int64_t at =
-                (((int64_t)2 * w + (begin > w * share ? 1 : 0)) * a.hkv + g) * a.tile_rows + r;
-            o = a.slot_o + at * D;
-            return a.slot_lse[at];
+            return n_own == 1 ? orow
+                              : ((int64_t)(2 * w + (begin > w * share)) * a.hkv + g) *
+                                        a.tile_rows + r;
         };
-        float mx = -INFINITY, nan = 0.f;
-        for (int c = lane; c < n; c += 64) {
-            const float *po;
-            const float l = part(c, po);
-            mx = fmaxf(mx, l);
-            nan += l != l ? l : 0.f;
-        }
+        auto lse_of = [&](int c) TA_INLINE -> float {
+            const float *from = c < n_pre ? (n_pre == 1 ? a.pre_row_lse : a.pre_slot_lse)
+                                          : (n_own == 1 ? a.row_lse : a.slot_lse);
+            return from[index(c)] + (c < n_pre ? shift : 0.f);
+        };
+        float mx = -INFINITY;
+        for (int c = lane; c < n; c += 64)
+            mx = fmaxf(mx, lse_of(c));
 #pragma unroll
-        for (int o = 32; o >= 1; o >>= 1) {
+        for (int o = 32; o >= 1; o >>= 1)
             mx = fmaxf(mx, __shfl_xor(mx, o));
-            nan += __shfl_xor(nan, o);
-        }
         const float m_use = mx == -INFINITY ? 0.f : mx;
-        float acc[PER] = {}, den = nan + (bad ? __builtin_nanf("") : 0.f);
-        constexpr int UNROLL = 8;
-        for (int c = 0; c < n; c += UNROLL) {
-            float x[UNROLL][PER], l[UNROLL];
+        vec acc{};
+        float den = 0.f;
+        for (int c0 = 0; c0 < n; c0 += 64) {
+            const float w = c0 + lane < n ? __expf(lse_of(c0 + lane) - m_use) : 0.f;
+            den += w;  // (NaN stays visible)
+            const int top = min(n - c0, 64);
+            constexpr int UNROLL = 8;
+            for (int c = 0; c < top; c += UNROLL) {
+                vec x[UNROLL];
 #pragma unroll
-            for (int u = 0; u < UNROLL; ++u) {
-                const float *po;
-                l[u] = part(min(c + u, n - 1), po);
-#pragma unroll
-                for (int e = 0; e < PER; ++e)
-                    x[u][e] = po[PER * lane + e];
-            }
-#pragma unroll
-            for (int u = 0; u < UNROLL; ++u)
-                if (c + u < n) {
-                    const float f = __expf(l[u] - m_use);
-                    den += f;
-#pragma unroll
-                    for (int e = 0; e < PER; ++e)
-                        acc[e] += f * x[u][e];
+                for (int u = 0; u < UNROLL; ++u) {
+                    const int cc = c0 + min(c + u, top - 1);
+                    const float *from = cc < n_pre ? (n_pre == 1 ? a.pre_row_o : a.pre_slot_o)
+                                                   : (n_own == 1 ? a.row_o : a.slot_o);
+                    x[u] = *reinterpret_cast<const vec *>(from + index(cc) * D + PER * lane);
                 }
+#pragma unroll
+                for (int u = 0; u < UNROLL; ++u) {
+                    const float f = __shfl(w, min(c + u, top - 1));
+                    if (c + u < top)
+#pragma unroll
+                        for (int e = 0; e < PER; ++e)
+                            acc[e] += f * x[u][e];
+                }
+            }
         }
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1)
+            den += __shfl_xor(den, o);
         const float inv = den == 0.f ? 0.f : 1.f / den;
 #pragma unroll
         for (int e = 0; e < PER; ++e) {
-            const int64_t at = orow * D + PER * lane + e;
+            const int64_t to = orow * D + PER * lane + e;
             if (a.o_f32)
-                static_cast<float *>(a.o)[at] = acc[e] * inv;
+                static_cast<float *>(a.o)[to] = acc[e] * inv;
             else
-                static_cast<__bf16 *>(a.o)[at] = (__bf16)(acc[e] * inv);
+                static_cast<__bf16 *>(a.o)[to] = (__bf16)(acc[e] * inv);
         }
         if (a.lse && lane == 0)
             a.lse[(int64_t)h * a.total_tokens + q0 + qt] =
@@ -748,7 +834,7 @@ PagedLayout paged_layout(int32_t batch, int64_t total_tokens, bool ragged, bool 
         at += (n + 255) / 256 * 256;
         return here;
     };
-    p.meta = take((size_t)(p.max_tiles + 1) * kMetaWords * 4);
+    p.meta = take(((size_t)(p.max_tiles + 1) * kMetaWords + p.own_slots) * 4);
     const size_t own = (size_t)2 * p.own_slots * hkv * rows;
     p.own_slot_o = take(own * d * 4);
     p.own_slot_lse = take(own * 4);
@@ -769,11 +855,12 @@ PagedLayout paged_layout(int32_t batch, int64_t total_tokens, bool ragged, bool 
 template <int D, int RB, bool PREFIX>
 void launch_scores(int score, dim3 grid, hipStream_t s, const PagedArgs &a)
 {
+    const dim3 threads(PagedShape<D, RB>::THREADS);
     switch (score) {
-    case 0: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 0, PREFIX>), grid, dim3(kThreads), 0, s, a); break;
-    case 1: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 1, PREFIX>), grid, dim3(kThreads), 0, s, a); break;
-    case 2: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 2, PREFIX>), grid, dim3(kThreads), 0, s, a); break;
-    default: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 3, PREFIX>), grid, dim3(kThreads), 0, s, a); break;
+    case 0: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 0, PREFIX>), grid, threads, 0, s, a); break;
+    case 1: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 1, PREFIX>), grid, threads, 0, s, a); break;
+    case 2: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 2, PREFIX>), grid, threads, 0, s, a); break;
+    default: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 3, PREFIX>), grid, threads, 0, s, a); break;
     }
 }
 
@@ -948,6 +1035,12 @@ extern "C" ta_status paged_attn_fwd(const void *q, const void *k_cache, const vo
         j.slot_o = a.slot_o;
         j.slot_lse = a.slot_lse;
         j.tile_rows = 32 * p.own_rb;
+        j.max_tiles = p.max_tiles;
+        j.slots = p.own_slots;
+        // a wave to a row, but four rows to a wave in tiles of 128
+        const int rows = cu_q ? j.tile_rows : (int)group;
+        j.chunk_rows = p.own_rb == 4 ? 16 : 4;
+        j.chunks = (rows + j.chunk_rows - 1) / j.chunk_rows;
         j.row_o = a.row_o;
         j.row_lse = a.row_lse;
         j.pre_slot_o = part(p.pre_slot_o);
@@ -956,19 +1049,21 @@ extern "C" ta_status paged_attn_fwd(const void *q, const void *k_cache, const vo
         j.pre_row_lse = part(p.pre_row_lse);
         j.prefix_len = prefix_len;
         j.pre_rows = 32 * p.pre_rb;
-        j.pre_step = p.pre_rb == 4 ? PagedShape<128, 4>::STEP : PagedShape<128, 1>::STEP;
-        j.pre_slots = p.pre_slots;
+        const int step = p.pre_rb == 4 ? PagedShape<128, 4>::STEP : PagedShape<128, 1>::STEP;
+        j.pre_steps = (prefix_len + step - 1) / step;
+        j.pre_share =
+            (int32_t)std::max<int64_t>(1, (pre_tiles * j.pre_steps + p.pre_slots - 1) / p.pre_slots);
         j.slopes = slopes;
         j.total_tokens = (int32_t)total_tokens;
         j.hq = hq;
         j.hkv = hkv;
         j.group = (int32_t)group;
         j.o_f32 = a.o_f32;
-        const dim3 grid((uint32_t)(p.max_tiles * hkv));
+        const dim3 grid((uint32_t)((prefix ? p.max_tiles : p.own_slots) * j.chunks * hkv));
         if (head_dim == 128)
-            hipLaunchKernelGGL(paged_join_kernel<128>, grid, dim3(kThreads), 0, s, j);
+            hipLaunchKernelGGL(paged_join_kernel<128>, grid, dim3(kJoinThreads), 0, s, j);
         else
-            hipLaunchKernelGGL(paged_join_kernel<64>, grid, dim3(kThreads), 0, s, j);
+            hipLaunchKernelGGL(paged_join_kernel<64>, grid, dim3(kJoinThreads), 0, s, j);
         err = hipGetLastError();
     }
     if (err != hipSuccess)

@@ -412,8 +412,7 @@ struct RowBlock {
     __device__ __forceinline__ static void schedule()
     {
         constexpr int NQ = QK ? NKB * QK_STEPS : 0, N = NQ + (PV ? NKB * 2 * D_BLOCKS : 0);
-        constexpr int AHEAD = 6;
-        static_assert(N >= AHEAD, "more MFMAs than reads ahead");
+        constexpr int AHEAD = N < 6 ? N : 6;
         constexpr int first = AHEAD <= NQ ? AHEAD : NQ + 2 * (AHEAD - NQ);
         __builtin_amdgcn_sched_group_barrier(kSchedDsRead, first, 0);
         schedule_from<NQ, N, AHEAD, 0>();
