@@ -382,9 +382,9 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
         const int32_t *pages = PREFIX ? a.prefix_pages : a.table + (int64_t)rt.req * a.width;
         if (tid == 0)
             s_bad = 0;
-        // One pass over the piece's steps; with `careful`, infinite or NaN
-        // values in masked steps are kept from the rows that do not keep their
-        // keys.  Returns whether a masked step holds any.
+        // One pass over the piece's steps.  Returns whether a masked step holds
+        // infinite or NaN values; the `careful` pass then keeps them from the
+        // rows that do not keep their keys.
         auto pass = [&](auto careful) TA_INLINE -> bool {
         constexpr bool CAREFUL = decltype(careful)::value;
         bool fresh = true, odd = false;
@@ -467,14 +467,10 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
                     asm volatile("");
                     odd |= rb.odd_values(vt, lane, RB == 1 ? 0 : wave, RB);
                 }
-                if (CAREFUL && masked) {
-                    rb.accumulate_by_key(vt, p);
-                } else {
-                    __builtin_amdgcn_sched_barrier(0);
-                    rb.accumulate(vt, p);
-                    rb.template schedule<false, true>();
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+                __builtin_amdgcn_sched_barrier(0);
+                rb.accumulate(vt, p);
+                rb.template schedule<false, true>();
+                __builtin_amdgcn_sched_barrier(0);
             };
             auto products = [&](const unsigned char *kt) TA_INLINE {
                 __builtin_amdgcn_sched_barrier(0);
@@ -482,7 +478,28 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
                 rb.template schedule<true, false>();
                 __builtin_amdgcn_sched_barrier(0);
             };
-            if constexpr (RB == 1) {
+            if constexpr (CAREFUL) {
+                // tile by tile, in this wave's first stage (RB = 1) or the
+                // workgroup's
+                const int n = (key_end - seg0 * S::STEP + S::STEP - 1) / S::STEP;
+                for (int i = 0; i < n; ++i) {
+                    const int key0 = (seg0 + (BACK ? n - 1 - i : i)) * S::STEP +
+                                     (RB == 1 ? wave * S::TK : 0);
+                    const bool on = key0 < key_end;
+                    if (on) {
+                        copy(key0, wave_lds, K{});
+                        copy(key0, wave_lds + S::TILE_BYTES, V{});
+                    }
+                    rows_wait_copies<0>();
+                    barrier_no_fence();
+                    if (on) {
+                        products(smem + wave_lds);
+                        softmax(key0);
+                        rb.accumulate_by_key(smem + wave_lds + S::TILE_BYTES, p);
+                    }
+                    barrier_no_fence();
+                }
+            } else if constexpr (RB == 1) {
                 // tiles of this wave: key0 = step STEP + wave TK
                 const int base = seg0 * S::STEP + wave * S::TK;
                 const int n = base < key_end ? (key_end - base + S::STEP - 1) / S::STEP : 0;
@@ -688,13 +705,16 @@ struct JoinArgs {
 // Joins the partials of a row: O = sum_c w_c O_c / sum_c w_c with w_c =
 // exp(LSE_c - max_c LSE_c), the prefix's before the row's own, in key order.
 // With a prefix every row has partials to join; without one only the row tiles
-// that a share's start cuts, which the shares name.  A wave takes a row at a
-// time, its lanes the log-sum-exps of up to 64 partials at once.
+// that a share's start cuts, which the shares name.  Sixteen lanes take a row:
+// what bounds this is the chain of loads (cut, record, log-sum-exps, partials), so
+// many rows at once matter more than wide ones (prompt pieces: JOIN16 us, with a
+// wave to a row 50).
 template <int D>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(JoinArgs a)
 {
-    constexpr int PER = D / 64;
-    typedef float vec __attribute__((ext_vector_type(PER)));
+    constexpr int LANES = 16;        // of a row
+    constexpr int PER = D / LANES;   // values of a lane, in runs of four
+    constexpr int RUNS = PER / 4;
     const int g = blockIdx.x % a.hkv, at = blockIdx.x / a.hkv;
     const int chunk = at % a.chunks;
     int t = at / a.chunks;
@@ -710,9 +730,11 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(JoinArgs a)
         return;  // rows without keys are written
     const int w0 = begin / share;
     const int n_own = (end - 1) / share - w0 + 1;
-    const int lane = threadIdx.x & 63;
-    const int r_end = min(rows, (chunk + 1) * a.chunk_rows);
-    for (int r = chunk * a.chunk_rows + (threadIdx.x >> 6); r < r_end; r += kJoinThreads / 64) {
+    const int lane = threadIdx.x % LANES;
+    {
+        const int r = chunk * a.chunk_rows + threadIdx.x / LANES;
+        if (threadIdx.x / LANES >= a.chunk_rows || r >= rows)
+            return;
         const int rho = rho0 + r, qt = rho / a.group, h = g * a.group + rho - qt * a.group;
         const int64_t orow = (int64_t)(q0 + qt) * a.hq + h;
         // the prefix pass's pieces of this row: its rows are those of all
@@ -748,49 +770,56 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(JoinArgs a)
             return from[index(c)] + (c < n_pre ? shift : 0.f);
         };
         float mx = -INFINITY;
-        for (int c = lane; c < n; c += 64)
+        for (int c = lane; c < n; c += LANES)
             mx = fmaxf(mx, lse_of(c));
 #pragma unroll
-        for (int o = 32; o >= 1; o >>= 1)
+        for (int o = LANES / 2; o >= 1; o >>= 1)
             mx = fmaxf(mx, __shfl_xor(mx, o));
         const float m_use = mx == -INFINITY ? 0.f : mx;
-        vec acc{};
+        f32x4r acc[RUNS] = {};
         float den = 0.f;
-        for (int c0 = 0; c0 < n; c0 += 64) {
+        for (int c0 = 0; c0 < n; c0 += LANES) {
             const float w = c0 + lane < n ? __expf(lse_of(c0 + lane) - m_use) : 0.f;
             den += w;  // (NaN stays visible)
-            const int top = min(n - c0, 64);
+            const int top = min(n - c0, LANES);
             constexpr int UNROLL = 8;
             for (int c = 0; c < top; c += UNROLL) {
-                vec x[UNROLL];
+                f32x4r x[UNROLL][RUNS];
 #pragma unroll
                 for (int u = 0; u < UNROLL; ++u) {
                     const int cc = c0 + min(c + u, top - 1);
                     const float *from = cc < n_pre ? (n_pre == 1 ? a.pre_row_o : a.pre_slot_o)
                                                    : (n_own == 1 ? a.row_o : a.slot_o);
-                    x[u] = *reinterpret_cast<const vec *>(from + index(cc) * D + PER * lane);
+                    from += index(cc) * D + 4 * lane;
+#pragma unroll
+                    for (int i = 0; i < RUNS; ++i)
+                        x[u][i] = *reinterpret_cast<const f32x4r *>(from + 4 * LANES * i);
                 }
 #pragma unroll
                 for (int u = 0; u < UNROLL; ++u) {
-                    const float f = __shfl(w, min(c + u, top - 1));
+                    const float f = __shfl(w, min(c + u, top - 1), LANES);
                     if (c + u < top)
 #pragma unroll
-                        for (int e = 0; e < PER; ++e)
-                            acc[e] += f * x[u][e];
+                        for (int i = 0; i < RUNS; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                acc[i][e] += f * x[u][i][e];
                 }
             }
         }
 #pragma unroll
-        for (int o = 32; o >= 1; o >>= 1)
+        for (int o = LANES / 2; o >= 1; o >>= 1)
             den += __shfl_xor(den, o);
         const float inv = den == 0.f ? 0.f : 1.f / den;
 #pragma unroll
-        for (int e = 0; e < PER; ++e) {
-            const int64_t to = orow * D + PER * lane + e;
+        for (int i = 0; i < RUNS; ++i) {
+            const int64_t to = orow * D + 4 * LANES * i + 4 * lane;
+            const f32x4r y = acc[i] * inv;
             if (a.o_f32)
-                static_cast<float *>(a.o)[to] = acc[e] * inv;
+                *reinterpret_cast<f32x4r *>(static_cast<float *>(a.o) + to) = y;
             else
-                static_cast<__bf16 *>(a.o)[to] = (__bf16)(acc[e] * inv);
+                *reinterpret_cast<bf16x4r *>(static_cast<__bf16 *>(a.o) + to) =
+                    __builtin_convertvector(y, bf16x4r);
         }
         if (a.lse && lane == 0)
             a.lse[(int64_t)h * a.total_tokens + q0 + qt] =
@@ -1037,9 +1066,8 @@ extern "C" ta_status paged_attn_fwd(const void *q, const void *k_cache, const vo
         j.tile_rows = 32 * p.own_rb;
         j.max_tiles = p.max_tiles;
         j.slots = p.own_slots;
-        // a wave to a row, but four rows to a wave in tiles of 128
         const int rows = cu_q ? j.tile_rows : (int)group;
-        j.chunk_rows = p.own_rb == 4 ? 16 : 4;
+        j.chunk_rows = std::min(rows, kJoinThreads / 16);
         j.chunks = (rows + j.chunk_rows - 1) / j.chunk_rows;
         j.row_o = a.row_o;
         j.row_lse = a.row_lse;

@@ -308,36 +308,26 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void scored_attn_kernel(ScoredArgs
     using Stage0 = std::integral_constant<int, 0>;
     using Stage1 = std::integral_constant<int, 1>;
 
-    // One pass over the steps, every wave in the same one.  With `careful`,
-    // infinite or NaN values in masked steps are kept from the rows that do not
-    // keep their keys; otherwise `odd` tells whether a masked step holds any.
-    auto together = [&](auto careful) TA_INLINE {
-        constexpr bool CAREFUL = decltype(careful)::value;
+    // One pass over the steps, every wave in the same one; `odd` tells
+    // whether a masked step holds infinite or NaN values.
+    auto together = [&]() TA_INLINE {
         Place now = place(0);
-        auto copies = [&](const Place &x, int stage) TA_INLINE {
-            if (NW == 4 || wave < 4) {
-                copy_k(x, stage);
-                copy_v(x, stage);
-            }
-        };
-        copies(now, 0);
+        copy_k(now, 0);
+        copy_v(now, 0);
         auto step = [&](int i, auto stage) TA_INLINE {
             constexpr int ST = decltype(stage)::value;
             // this step's tile has landed for every wave, and every wave is
             // done with the other stage
             end_phase(true);
             const Place next = place(min(i + 1, n - 1));
-            if (i + 1 < n)
-                copies(next, 1 - ST);
+            if (i + 1 < n) {
+                copy_k(next, 1 - ST);
+                copy_v(next, 1 - ST);
+            }
             const unsigned char *kt = smem + ST * STAGE_BYTES;
             products(kt);
             softmax(now);
-            if (!CAREFUL)
-                values(now, kt + TILE_BYTES);
-            else if (now.masked)
-                rb.accumulate_by_key(kt + TILE_BYTES, p);
-            else
-                rb.accumulate(kt + TILE_BYTES, p);
+            values(now, kt + TILE_BYTES);
             now = next;
         };
         int i = 0;
@@ -347,6 +337,22 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void scored_attn_kernel(ScoredArgs
         }
         if (i < n)
             step(i, Stage0{});
+    };
+    // The pass that keeps infinite and NaN values in masked steps from the
+    // rows that do not keep their keys.
+    auto careful = [&]() TA_INLINE {
+        for (int i = 0; i < n; ++i) {
+            const Place now = place(i);
+            if (wave < 4) {
+                copy_k(now, 0);
+                copy_v(now, 0);
+            }
+            end_phase(true);
+            products(smem);
+            softmax(now);
+            rb.accumulate_by_key(smem + TILE_BYTES, p);
+            end_phase(false);
+        }
     };
     // The same in two groups of four waves, one wave of each on a SIMD, in
     // turns: M(j) = {S(j) = K(j) Q^T, O += V(j - 1) P(j - 1)} on the matrix
@@ -446,10 +452,10 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void scored_attn_kernel(ScoredArgs
         if constexpr (NW == 8)
             in_turns();
         else
-            together(std::false_type{});
+            together();
         if (__builtin_expect(__syncthreads_or(odd), 0)) {
             start();
-            together(std::true_type{});
+            careful();
         }
     }
     if (!active || row_base + rb.col >= r1)
