@@ -384,33 +384,38 @@ def causal_attn_fwd(q, k, v, o, lse, sched_dev, info, softmax_scale,
         float(softmax_scale), _stream(stream)))
 
 
-class _OnDevice:
-    """Makes a tensor's GPU current for a call, and checks that the stream it
-    is enqueued on (the GPU's current one if None) belongs to that GPU."""
-
-    def __init__(self, device, stream):
-        import torch
-        self.guard = torch.cuda.device(device)
-        if stream is None:
-            stream = torch.cuda.current_stream(device)
-        elif stream.device != device:
-            raise ValueError(f"stream is on {stream.device}, operands on {device}")
-        self.stream = ctypes.c_void_p(stream.cuda_stream)
-
-    def __enter__(self):
-        self.guard.__enter__()
-        return self.stream
-
-    def __exit__(self, *exc):
-        return self.guard.__exit__(*exc)
+def _launch(device, stream, fn, *args):
+    """fn(*args, stream) with the GPU of the operands current, on its current
+    stream if None; a stream of another GPU is refused.  (The stream's handle is
+    asked for without building a Stream object: a microsecond of a call that
+    enqueues one short kernel in eight.)"""
+    import torch
+    index = device.index
+    if stream is None:
+        handle = torch._C._cuda_getCurrentRawStream(index)
+    elif stream.device != device:
+        raise ValueError(f"stream is on {stream.device}, operands on {device}")
+    else:
+        handle = stream.cuda_stream
+    if torch._C._cuda_getDevice() == index:
+        status = fn(*args, handle)
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, handle)
+    if status != TA_OK:
+        raise TriAttnError(status, ta_last_error())
 
 
 def _check_operands(named, dev):
     """named: (name, tensor, dtype, shape); a None in a shape leaves that
     length open, a None in place of the shape leaves it all open."""
     import torch
+    tensor = torch.Tensor
     for name, t, dtype, shape in named:
-        if not isinstance(t, torch.Tensor):
+        if (isinstance(t, tensor) and t.dtype is dtype and t.device == dev and t.is_contiguous()
+                and (shape is None or t.shape == shape)):
+            continue
+        if not isinstance(t, tensor):
             raise ValueError(f"{name} must be a torch tensor")
         if t.dtype != dtype:
             raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
@@ -424,6 +429,18 @@ def _check_operands(named, dev):
                              "one device")
     if dev.type != "cuda":
         raise ValueError(f"operands must be on a GPU, got {dev}")
+
+
+def _open(t, shape):
+    """shape with the tensor's own lengths where it leaves them open."""
+    own = getattr(t, "shape", None)
+    if own is None or len(own) != len(shape):
+        return shape
+    return tuple(a if b is None else b for a, b in zip(own, shape))
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
 
 
 def _nbytes(t):
@@ -442,11 +459,10 @@ def scored_attn_fwd(q, k, v, o, lse, sched_dev, info, softmax_scale, softcap, sl
         import torch
         _check_operands([("slopes", slopes, torch.float32, (hq,))], q.device)
     cap = 0.0 if softcap is None else float(softcap)
-    with _OnDevice(q.device, stream) as s:
-        _check(lib().scored_attn_fwd(
-            _ptr(q), _ptr(k), _ptr(v), _ptr(o), _out_dtype(o), _ptr(lse), _ptr(sched_dev),
-            ctypes.byref(info), total, hq, k.shape[1], d, float(softmax_scale), cap,
-            _ptr(slopes), _ptr(workspace), _nbytes(workspace), s))
+    _launch(q.device, stream, lib().scored_attn_fwd, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+            o.data_ptr(), _out_dtype(o), _addr(lse), sched_dev.data_ptr(), ctypes.byref(info),
+            total, hq, k.shape[1], d, float(softmax_scale), cap, _addr(slopes), _addr(workspace),
+            _nbytes(workspace))
 
 
 # status bits of page_map (state[1])
@@ -474,15 +490,15 @@ def page_map(cached_lens, new_lens, block_table, free_pages, n_free, page_size, 
         raise ValueError("cached_lens must be a tensor [requests]")
     b, dev = cached_lens.shape[0], cached_lens.device
     _check_operands([("cached_lens", cached_lens, i32, (b,)), ("new_lens", new_lens, i32, (b,)),
-                     ("block_table", block_table, i32, (b, None)),
-                     ("free_pages", free_pages, i32, (None,)), ("n_free", n_free, i32, (1,)),
-                     ("kv_lens", kv_lens, i32, (b,)), ("cu_new", cu_new, i32, (b + 1,)),
-                     ("slots", slots, i32, (None,)), ("state", state, i32, (2,))], dev)
-    with _OnDevice(dev, stream) as s:
-        _check(lib().ta_page_map(
-            _ptr(cached_lens), _ptr(new_lens), b, int(page_size), _ptr(block_table),
-            block_table.shape[1], _ptr(free_pages), free_pages.shape[0], _ptr(n_free),
-            _ptr(kv_lens), _ptr(cu_new), _ptr(slots), slots.shape[0], _ptr(state), s))
+                     ("block_table", block_table, i32, _open(block_table, (b, None))),
+                     ("free_pages", free_pages, i32, _open(free_pages, (None,))),
+                     ("n_free", n_free, i32, (1,)), ("kv_lens", kv_lens, i32, (b,)),
+                     ("cu_new", cu_new, i32, (b + 1,)), ("slots", slots, i32, _open(slots, (None,))),
+                     ("state", state, i32, (2,))], dev)
+    _launch(dev, stream, lib().ta_page_map, cached_lens.data_ptr(), new_lens.data_ptr(), b,
+            int(page_size), block_table.data_ptr(), block_table.shape[1], free_pages.data_ptr(),
+            free_pages.shape[0], n_free.data_ptr(), kv_lens.data_ptr(), cu_new.data_ptr(),
+            slots.data_ptr(), slots.shape[0], state.data_ptr())
 
 
 def _cache_shape(k_cache):
@@ -518,10 +534,9 @@ def kv_cache_write(k, v, slots, k_cache, v_cache, stream=None):
     _check_operands([("k_cache", k_cache, torch.bfloat16, shape),
                      ("v_cache", v_cache, torch.bfloat16, shape),
                      ("slots", slots, torch.int32, (total,))], dev)
-    with _OnDevice(dev, stream) as s:
-        _check(lib().kv_cache_write(
-            _ptr(k), _ptr(v), k.stride(0), k.stride(1), v.stride(0), v.stride(1), _ptr(slots),
-            total, _ptr(k_cache), _ptr(v_cache), pages, hkv, page_size, d, s))
+    _launch(dev, stream, lib().kv_cache_write, k.data_ptr(), v.data_ptr(), k.stride(0),
+            k.stride(1), v.stride(0), v.stride(1), slots.data_ptr(), total, k_cache.data_ptr(),
+            v_cache.data_ptr(), pages, hkv, page_size, d)
 
 
 def ta_paged_workspace_bytes(batch, total_tokens, ragged, prefix, hq, hkv, head_dim) -> int:
@@ -559,7 +574,7 @@ def paged_attn_fwd(q, k_cache, v_cache, o, lse, kv_lens, cu_q, block_table, pref
     i32 = torch.int32
     named = [("q", q, torch.bfloat16, None), ("k_cache", k_cache, torch.bfloat16, shape),
              ("v_cache", v_cache, torch.bfloat16, shape), ("o", o, o.dtype, (total, hq, d)),
-             ("kv_lens", kv_lens, i32, (b,)), ("block_table", block_table, i32, (b, None))]
+             ("kv_lens", kv_lens, i32, (b,)), ("block_table", block_table, i32, _open(block_table, (b, None)))]
     if lse is not None:
         named.append(("lse", lse, torch.float32, (hq, total)))
     if cu_q is not None:
@@ -570,7 +585,7 @@ def paged_attn_fwd(q, k_cache, v_cache, o, lse, kv_lens, cu_q, block_table, pref
     if prefix_len < 0:
         raise ValueError(f"prefix_len {prefix_len} < 0")
     if prefix_len > 0:
-        named.append(("prefix_pages", prefix_pages, i32, (None,)))
+        named.append(("prefix_pages", prefix_pages, i32, _open(prefix_pages, (None,))))
     if workspace is not None:
         named.append(("workspace", workspace, workspace.dtype, None))
     if slopes is not None:
@@ -579,13 +594,12 @@ def paged_attn_fwd(q, k_cache, v_cache, o, lse, kv_lens, cu_q, block_table, pref
     if prefix_len > 0 and prefix_pages.shape[0] * page_size < prefix_len:
         raise ValueError(f"{prefix_pages.shape[0]} prefix pages of {page_size} hold no "
                          f"{prefix_len} keys")
-    with _OnDevice(dev, stream) as s:
-        _check(lib().paged_attn_fwd(
-            _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(o), out, _ptr(lse), _ptr(kv_lens),
-            _ptr(cu_q), _ptr(block_table), b, block_table.shape[1],
-            _ptr(prefix_pages) if prefix_len > 0 else None, prefix_len, total, hq, hkv, d, pages,
-            page_size, float(softmax_scale), 0.0 if softcap is None else float(softcap),
-            _ptr(slopes), _ptr(workspace), _nbytes(workspace), s))
+    _launch(dev, stream, lib().paged_attn_fwd, q.data_ptr(), k_cache.data_ptr(),
+            v_cache.data_ptr(), o.data_ptr(), out, _addr(lse), kv_lens.data_ptr(), _addr(cu_q),
+            block_table.data_ptr(), b, block_table.shape[1],
+            prefix_pages.data_ptr() if prefix_len > 0 else None, prefix_len, total, hq, hkv, d,
+            pages, page_size, float(softmax_scale), 0.0 if softcap is None else float(softcap),
+            _addr(slopes), _addr(workspace), _nbytes(workspace))
 
 
 class PagedPlan:

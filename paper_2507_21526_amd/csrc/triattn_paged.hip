@@ -38,12 +38,11 @@ constexpr int kMaxTiles = 2048;    // row tiles of a kv head
 constexpr int kPageEntries = 512;  // page ids held in LDS at a time
 constexpr int kCus = 256;
 
-// Words of the record that the own-keys pass leaves for the join: a header, one
-// entry a row tile, and for each share the row tile that the share's start is
-// the first to cut (-1: none).
-constexpr int kMetaWords = 8;
-enum MetaHeader { MH_TILES = 0, MH_SHARE };
-enum MetaField { MF_Q0 = 0, MF_RHO0, MF_ROWS, MF_POS0, MF_BEGIN, MF_END };
+// What the own-keys pass leaves for the join, eight words a record: of every row
+// tile where a prefix comes before, otherwise of each share the row tile that
+// the share's start is the first to cut.  No rows: nothing to join.
+constexpr int kRecordWords = 8;
+enum RecordField { RF_Q0 = 0, RF_RHO0, RF_ROWS, RF_POS0, RF_BEGIN, RF_END, RF_SHARE };
 
 struct PagedArgs {
     const uint16_t *q, *kc, *vc;
@@ -52,20 +51,16 @@ struct PagedArgs {
     const int32_t *kv_lens, *cu_q, *table, *prefix_pages;
     float *slot_o, *slot_lse;  // pieces of row tiles: [2 slots, hkv, ROWS (, D)]
     float *row_o, *row_lse;    // whole row tiles that the join still needs: [T, hq (, D)]
-    int32_t *meta;
+    int32_t *records;
     ScoreArgs score;
     int32_t total_tokens, batch, width, hq, hkv, group;
     uint32_t group_inv;  // 65536 / group + 1: x * group_inv >> 16 = x / group, x < 2^13
     int32_t page_log2, num_pages, prefix_len;
     int32_t slots;      // shares a kv head
-    int32_t max_tiles;  // row tiles that the record has room for
+    int32_t max_tiles;  // row tiles that the call counts on at most
+    int32_t n_records;
     int32_t o_f32;
 };
-
-__device__ __forceinline__ int32_t *meta_cuts(int32_t *meta, int max_tiles)
-{
-    return meta + kMetaWords * (max_tiles + 1);
-}
 
 // Shapes of the two forms of the pass.
 //   RB = 1: up to 32 rows, bound by the bytes of K and V.  Two waves take 32-key
@@ -239,11 +234,9 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
             n_tiles = uni(s_req[a.batch]);
             // query offsets that are none: nothing is computed, NaN shows it
             if (s_bad != 0 || n_tiles > a.max_tiles) {
-                if (g == 0 && tid == 0) {
-                    meta_cuts(a.meta, a.max_tiles)[slot] = -1;
-                    if (slot == 0)
-                        a.meta[MH_TILES] = 0;
-                }
+                if (g == 0)
+                    for (int i = slot * kThreads + tid; i < a.n_records; i += a.slots * kThreads)
+                        a.records[i * kRecordWords + RF_ROWS] = 0;
                 rows_poison(a.o, a.o_f32, a.lse, (int64_t)a.total_tokens * a.hq, D);
                 return;
             }
@@ -259,31 +252,33 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
     const int share0 = slot * share;
     const int share1 = min(total, share0 + share);
     if constexpr (!PREFIX) {
-        // the record for the join
-        if (blockIdx.x == 0) {
-            if (tid == 0) {
-                a.meta[MH_TILES] = n_tiles;
-                a.meta[MH_SHARE] = share;
+        // the records for the join
+        auto record = [&](int i, int t) TA_INLINE {
+            int32_t *m = a.records + kRecordWords * i;
+            if (t < 0 || t >= n_tiles || s_step[t] == s_step[t + 1]) {
+                m[RF_ROWS] = 0;
+                return;
             }
-            for (int t = tid; t < n_tiles; t += kThreads) {
-                const RowTile r = tile_of(t);
-                int32_t *m = a.meta + kMetaWords * (t + 1);
-                m[MF_Q0] = r.q0;
-                m[MF_RHO0] = r.rho0;
-                m[MF_ROWS] = r.rows;
-                m[MF_POS0] = r.pos0;
-                m[MF_BEGIN] = s_step[t];
-                m[MF_END] = s_step[t + 1];
-            }
-        }
-        if (g == 0 && tid == 0) {
-            int cut = -1;
+            const RowTile r = tile_of(t);
+            m[RF_Q0] = r.q0;
+            m[RF_RHO0] = r.rho0;
+            m[RF_ROWS] = r.rows;
+            m[RF_POS0] = r.pos0;
+            m[RF_BEGIN] = s_step[t];
+            m[RF_END] = s_step[t + 1];
+            m[RF_SHARE] = share;
+        };
+        if (g == 0 && a.row_o) {
+            for (int i = slot * kThreads + tid; i < a.n_records; i += a.slots * kThreads)
+                record(i, i);
+        } else if (g == 0 && tid == 0) {
+            int t = -1;
             if (share0 < total) {
-                const int t = find_start(s_step, n_tiles, share0);
-                if (s_step[t] < share0 && s_step[t] >= share0 - share)
-                    cut = t;
+                t = find_start(s_step, n_tiles, share0);
+                if (s_step[t] == share0 || s_step[t] < share0 - share)
+                    t = -1;  // not cut, or cut by an earlier share's start
             }
-            meta_cuts(a.meta, a.max_tiles)[slot] = cut;
+            record(slot, t);
         }
         // rows without keys, shared out over the slots
         for (int t = slot; t < n_tiles; t += a.slots) {
@@ -690,9 +685,9 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
 struct JoinArgs {
     void *o;
     float *lse;
-    int32_t *meta;
+    const int32_t *records;
     const float *slot_o, *slot_lse;
-    int32_t tile_rows, max_tiles, slots;
+    int32_t tile_rows;
     int32_t chunks, chunk_rows;  // workgroups of a row tile, rows of each
     // the prefix pass (prefix_len 0: none)
     const float *row_o, *row_lse;
@@ -717,17 +712,11 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(JoinArgs a)
     constexpr int RUNS = PER / 4;
     const int g = blockIdx.x % a.hkv, at = blockIdx.x / a.hkv;
     const int chunk = at % a.chunks;
-    int t = at / a.chunks;
-    const int32_t tiles = a.meta[MH_TILES], share = a.meta[MH_SHARE];
-    if (a.prefix_len == 0)
-        t = meta_cuts(a.meta, a.max_tiles)[t];
-    if (t < 0 || t >= tiles)
+    const int32_t *m = a.records + kRecordWords * (at / a.chunks);
+    const int32_t q0 = m[RF_Q0], rho0 = m[RF_RHO0], rows = m[RF_ROWS], pos0 = m[RF_POS0];
+    const int32_t begin = m[RF_BEGIN], end = m[RF_END], share = m[RF_SHARE];
+    if (rows == 0)
         return;
-    const int32_t *m = a.meta + kMetaWords * (t + 1);
-    const int32_t q0 = m[MF_Q0], rho0 = m[MF_RHO0], rows = m[MF_ROWS], pos0 = m[MF_POS0];
-    const int32_t begin = m[MF_BEGIN], end = m[MF_END];
-    if (begin == end)
-        return;  // rows without keys are written
     const int w0 = begin / share;
     const int n_own = (end - 1) / share - w0 + 1;
     const int lane = threadIdx.x % LANES;
@@ -831,8 +820,8 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(JoinArgs a)
 struct PagedLayout {
     int own_rb, pre_rb;        // row blocks of the two passes
     int own_slots, pre_slots;  // shares a kv head
-    int max_tiles;
-    size_t meta, own_slot_o, own_slot_lse, own_row_o, own_row_lse, pre_slot_o, pre_slot_lse,
+    int max_tiles, n_records;
+    size_t records, own_slot_o, own_slot_lse, own_row_o, own_row_lse, pre_slot_o, pre_slot_lse,
         pre_row_o, pre_row_lse, bytes;
 };
 
@@ -863,7 +852,8 @@ PagedLayout paged_layout(int32_t batch, int64_t total_tokens, bool ragged, bool 
         at += (n + 255) / 256 * 256;
         return here;
     };
-    p.meta = take(((size_t)(p.max_tiles + 1) * kMetaWords + p.own_slots) * 4);
+    p.n_records = prefix ? p.max_tiles : p.own_slots;
+    p.records = take((size_t)p.n_records * kRecordWords * 4);
     const size_t own = (size_t)2 * p.own_slots * hkv * rows;
     p.own_slot_o = take(own * d * 4);
     p.own_slot_lse = take(own * 4);
@@ -1027,7 +1017,8 @@ extern "C" ta_status paged_attn_fwd(const void *q, const void *k_cache, const vo
     const bool prefix = prefix_len > 0;
     a.row_o = prefix ? part(p.own_row_o) : nullptr;
     a.row_lse = prefix ? part(p.own_row_lse) : nullptr;
-    a.meta = reinterpret_cast<int32_t *>(ws + p.meta);
+    a.records = reinterpret_cast<int32_t *>(ws + p.records);
+    a.n_records = p.n_records;
     a.score = score_args;
     a.total_tokens = (int32_t)total_tokens;
     a.batch = batch;
@@ -1060,12 +1051,10 @@ extern "C" ta_status paged_attn_fwd(const void *q, const void *k_cache, const vo
         JoinArgs j{};
         j.o = o;
         j.lse = lse;
-        j.meta = a.meta;
+        j.records = a.records;
         j.slot_o = a.slot_o;
         j.slot_lse = a.slot_lse;
         j.tile_rows = 32 * p.own_rb;
-        j.max_tiles = p.max_tiles;
-        j.slots = p.own_slots;
         const int rows = cu_q ? j.tile_rows : (int)group;
         j.chunk_rows = std::min(rows, kJoinThreads / 16);
         j.chunks = (rows + j.chunk_rows - 1) / j.chunk_rows;
@@ -1087,7 +1076,7 @@ extern "C" ta_status paged_attn_fwd(const void *q, const void *k_cache, const vo
         j.hkv = hkv;
         j.group = (int32_t)group;
         j.o_f32 = a.o_f32;
-        const dim3 grid((uint32_t)((prefix ? p.max_tiles : p.own_slots) * j.chunks * hkv));
+        const dim3 grid((uint32_t)(p.n_records * j.chunks * hkv));
         if (head_dim == 128)
             hipLaunchKernelGGL(paged_join_kernel<128>, grid, dim3(kJoinThreads), 0, s, j);
         else
