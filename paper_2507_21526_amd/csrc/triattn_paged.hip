@@ -80,7 +80,10 @@ struct PagedShape {
     static constexpr int TILE_BYTES = TK * 2 * D;
     static constexpr int STAGE_BYTES = 2 * TILE_BYTES;  // K tile, then V tile
     static constexpr int LDS_BYTES = KS * 2 * STAGE_BYTES;
-    static constexpr int WGS_PER_CU = RB == 1 && D == 64 ? 3 : 2;
+    // least steps of a share: one of a 128-row tile leaves partials of twice
+    // its K and V tiles' bytes
+    static constexpr int LEAST = RB == 4 ? 4 : 1;
+    static constexpr int WGS_PER_CU = RB == 1 && D == 64 ? 4 : 2;
     static constexpr int WAVES_PER_SIMD = (WGS_PER_CU * THREADS / 64 + 3) / 4;
 };
 
@@ -158,8 +161,12 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
     constexpr int D_BLOCKS = D / 32;
 
     __shared__ __attribute__((aligned(1024))) unsigned char smem[S::LDS_BYTES];
-    __shared__ int32_t s_req[PREFIX ? 1 : TA_MAX_BATCH + 1];  // first row tile of a request
-    __shared__ int32_t s_step[PREFIX ? 1 : kMaxTiles + 1];    // first step of a row tile
+    // tables of the own-keys pass, as long as the call needs (table_bytes)
+    extern __shared__ int32_t tables[];
+    int32_t *const s_step = tables;                   // first step of a row tile, and the total
+    int32_t *const s_kv = s_step + a.max_tiles + 1;   // own keys of a request
+    int32_t *const s_req = s_kv + a.batch;            // first row tile of a request, and all
+    int32_t *const s_cu = s_req + a.batch + 1;        // query offsets
     __shared__ int32_t s_page[kPageEntries];
     __shared__ int32_t s_wave[kThreads / 64];
     __shared__ float s_ml[S::KS][32][2];
@@ -197,11 +204,11 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
             r.rho0 = 0;
             if (a.cu_q) {
                 r.req = find_start(s_req, a.batch, t);
-                r.q0 = a.cu_q[r.req];
-                nq = a.cu_q[r.req + 1] - r.q0;
+                r.q0 = s_cu[r.req];
+                nq = s_cu[r.req + 1] - r.q0;
                 r.rho0 = (t - s_req[r.req]) * S::ROWS;
             }
-            int32_t kv = a.cu_q ? a.kv_lens[r.req] : s_req[t];
+            int32_t kv = s_kv[r.req];
             r.bad = kv > (a.width << a.page_log2);
             kv = r.bad ? 0 : max(kv, 0);
             r.rows = min(S::ROWS, nq * a.group - r.rho0);
@@ -222,6 +229,10 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
             bool bad = tid == 0 && (a.cu_q[0] != 0);
             block_scan<kThreads>(a.batch, s_req, s_wave, [&](int b) TA_INLINE -> int32_t {
                 const int32_t b0 = a.cu_q[b], b1 = a.cu_q[b + 1];
+                s_kv[b] = a.kv_lens[b];
+                s_cu[b] = b0;
+                if (b + 1 == a.batch)
+                    s_cu[b + 1] = b1;
                 if (b0 < 0 || b1 < b0 || b1 > a.total_tokens) {
                     bad = true;
                     return 0;
@@ -243,12 +254,12 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
         }
         block_scan<kThreads>(n_tiles, s_step, s_wave, [&](int t) TA_INLINE -> int32_t {
             if (!a.cu_q)
-                s_req[t] = a.kv_lens[t];  // (no row tiles to count: the lengths)
+                s_kv[t] = a.kv_lens[t];
             return (tile_of(t).limit + S::STEP - 1) / S::STEP;
         });
         total = uni(s_step[n_tiles]);
     }
-    const int share = max(1, (total + a.slots - 1) / a.slots);
+    const int share = max(S::LEAST, (total + a.slots - 1) / a.slots);
     const int share0 = slot * share;
     const int share1 = min(total, share0 + share);
     if constexpr (!PREFIX) {
@@ -702,8 +713,8 @@ struct JoinArgs {
 // With a prefix every row has partials to join; without one only the row tiles
 // that a share's start cuts, which the shares name.  Sixteen lanes take a row:
 // what bounds this is the chain of loads (cut, record, log-sum-exps, partials), so
-// many rows at once matter more than wide ones (prompt pieces: JOIN16 us, with a
-// wave to a row 50).
+// many rows at once matter more than wide ones (prompt pieces: 22 us, with a wave
+// to a row 50).
 template <int D>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(JoinArgs a)
 {
@@ -871,15 +882,23 @@ PagedLayout paged_layout(int32_t batch, int64_t total_tokens, bool ragged, bool 
     return p;
 }
 
+// LDS of the own-keys pass's tables.
+uint32_t table_bytes(const PagedArgs &a)
+{
+    return 4u * (uint32_t)(a.max_tiles + 1 + a.batch +
+                           (a.cu_q ? 2 * (a.batch + 1) : 0));
+}
+
 template <int D, int RB, bool PREFIX>
 void launch_scores(int score, dim3 grid, hipStream_t s, const PagedArgs &a)
 {
     const dim3 threads(PagedShape<D, RB>::THREADS);
+    const uint32_t lds = PREFIX ? 0 : table_bytes(a);
     switch (score) {
-    case 0: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 0, PREFIX>), grid, threads, 0, s, a); break;
-    case 1: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 1, PREFIX>), grid, threads, 0, s, a); break;
-    case 2: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 2, PREFIX>), grid, threads, 0, s, a); break;
-    default: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 3, PREFIX>), grid, threads, 0, s, a); break;
+    case 0: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 0, PREFIX>), grid, threads, lds, s, a); break;
+    case 1: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 1, PREFIX>), grid, threads, lds, s, a); break;
+    case 2: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 2, PREFIX>), grid, threads, lds, s, a); break;
+    default: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 3, PREFIX>), grid, threads, lds, s, a); break;
     }
 }
 
@@ -1069,7 +1088,9 @@ extern "C" ta_status paged_attn_fwd(const void *q, const void *k_cache, const vo
         const int step = p.pre_rb == 4 ? PagedShape<128, 4>::STEP : PagedShape<128, 1>::STEP;
         j.pre_steps = (prefix_len + step - 1) / step;
         j.pre_share =
-            (int32_t)std::max<int64_t>(1, (pre_tiles * j.pre_steps + p.pre_slots - 1) / p.pre_slots);
+            (int32_t)std::max<int64_t>(p.pre_rb == 4 ? PagedShape<128, 4>::LEAST
+                                                     : PagedShape<128, 1>::LEAST,
+                                       (pre_tiles * j.pre_steps + p.pre_slots - 1) / p.pre_slots);
         j.slopes = slopes;
         j.total_tokens = (int32_t)total_tokens;
         j.hq = hq;
