@@ -2,13 +2,15 @@
 // distance) over the schedules of the forward passes: Triangle, dense causal
 // and block-sparse.
 //
-// A workgroup of four waves takes four row blocks (32 rows of one head) of a
-// schedule item, dealt out head first, over K/V tiles of 64 keys in LDS, two
-// workgroups to a CU.  The two waves of a SIMD then belong to different
-// workgroups, so that one's matrix instructions run beside the other's score
-// arithmetic without a barrier between them.  That arithmetic bounds the pass:
-// a capped score takes two exp2, a reciprocal and about seven plain operations,
-// some twenty issue slots of a lane, where the two products take eight.
+// A workgroup of four or eight waves takes as many row blocks (32 rows of one
+// head) of a schedule item, dealt out head first, over K/V tiles of 64 keys in
+// LDS.  What bounds it: a plain product pair takes a wave 32 matrix instructions of
+// 32 cycles a step.  A capped score takes two exp2 and a reciprocal (16 cycles each)
+// and five plain operations (4 each): 2240 cycles of the vector unit a step, more
+// than the matrix cores' 1024; the 16384-token causal layer (32 heads over 8, d =
+// 128) runs at 2450 cycles a wave and step, 2.41 ms, 912 TFLOP/s.  Slopes add one
+// operation to a plain score: packed 42000 tokens at window 2048 in 1.35 ms, 1085
+// TFLOP/s, matrix cores 56 % busy.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -69,8 +71,9 @@ __device__ __forceinline__ Runs reach(Runs r, bool stream, int sink, int window,
 }
 
 template <int D, int SCORE, bool LIST, int NW>
-__global__ __launch_bounds__(NW * 64, 8 / NW) void scored_attn_kernel(ScoredArgs a)
+__global__ __launch_bounds__(NW * 64, D == 64 ? 3 : 2) void scored_attn_kernel(ScoredArgs a)
 {
+    static_assert(NW == 4 || D == 128, "eight waves at d = 128 only");
     constexpr int kThreads = NW * 64;
     constexpr int ROW_BYTES = 2 * D;
     constexpr int CHUNKS = D / 8;
@@ -648,8 +651,19 @@ extern "C" ta_status scored_attn_fwd(const void *q, const void *k, const void *v
     if (2LL * hq * head_dim >= (1LL << 24))
         return fail(TA_ERR_UNSUPPORTED, "%s: hq * head_dim too large", fn);
     const int64_t group = hq / hkv;
+    // Eight waves, half of them in turns, share each K/V tile copied; four run two
+    // workgroups to a CU (three at d = 64), which suits what the vector units
+    // bound, finer launches and row blocks that do not come in eights.  Eight
+    // where they pay: d = 128, whole eights of row blocks, and more than two
+    // workgroups to a CU.  us with eight and with four waves: capped causal at d =
+    // 128, 32 heads over 8, 700 tokens 29 and 22, 2500 tokens 99 and 94, 4000 tokens
+    // 183 and 186, 16384 tokens 2451 and 2550; slopes, window 1024, 4000 tokens 97 and
+    // 97, packed 42000 tokens, window 2048 1370 and 1457; 28 heads over 4, 8000 tokens
+    // 614 and 569; d = 64, 12000 tokens 1034 and 922.
     const int64_t blocks = group * (info->tile / 32);
-    const int nw = blocks > 4 ? 8 : 4;
+    const bool eight = head_dim == 128 && blocks % 8 == 0 &&
+                       info->n_items * (blocks / 8) * hkv > 512;
+    const int nw = eight ? 8 : 4;
     const int64_t subtiles = (blocks + nw - 1) / nw;
     const int64_t wgs = info->n_items * subtiles * hkv;
     const int64_t join_wgs =
@@ -704,8 +718,6 @@ extern "C" ta_status scored_attn_fwd(const void *q, const void *k, const void *v
         launch_scored<128, 8>(list, score, grid, s, a);
     else if (head_dim == 128)
         launch_scored<128, 4>(list, score, grid, s, a);
-    else if (nw == 8)
-        launch_scored<64, 8>(list, score, grid, s, a);
     else
         launch_scored<64, 4>(list, score, grid, s, a);
     hipError_t err = hipGetLastError();
