@@ -501,7 +501,7 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
                     if (on) {
                         products(smem + wave_lds);
                         softmax(key0);
-                        rb.accumulate_by_key(smem + wave_lds + S::TILE_BYTES, p);
+                        rb.accumulate_by_key(smem + wave_lds + S::TILE_BYTES, s, p);
                     }
                     barrier_no_fence();
                 }

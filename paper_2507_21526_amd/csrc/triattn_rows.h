@@ -365,9 +365,10 @@ struct RowBlock {
         return __builtin_amdgcn_ballot_w64((carry & 0x80008000u) != 0) != 0;
     }
 
-    // accumulate() key by key, each only to the rows whose probability of it
-    // is not zero.
+    // accumulate() key by key, each only to the rows that keep it (whose score
+    // x of it, as the mask left it, is not -inf).
     __device__ __forceinline__ void accumulate_by_key(const unsigned char *vt,
+                                                      const f32x16 (&x)[NKB],
                                                       const bf16x8 (&pf)[NKB][2])
     {
         typedef uint16_t u16x8r __attribute__((ext_vector_type(8)));
@@ -375,18 +376,21 @@ struct RowBlock {
 #pragma unroll 1
         for (int j = 0; j < NKB * 32; ++j) {
             // key j: block j / 32, element (j / 16 & 1, j & 7) of half j / 8 & 1
-            uint32_t mine = 0;
+            float mine = 0.f, kept = 0.f;
 #pragma unroll
             for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
                 for (int s2 = 0; s2 < 2; ++s2) {
                     const u16x8r pb = __builtin_bit_cast(u16x8r, pf[kb][s2]);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        mine = kb * 32 + s2 * 16 + 8 * half + e == j ? (uint32_t)pb[e] : mine;
+                    for (int e = 0; e < 8; ++e) {
+                        const bool on = kb * 32 + s2 * 16 + 8 * half + e == j;
+                        mine = on ? __uint_as_float((uint32_t)pb[e] << 16) : mine;
+                        kept = on && x[kb][8 * s2 + e] != -INFINITY ? 1.f : kept;
+                    }
                 }
-            const float p = rows_pair_sum(__uint_as_float(mine << 16));
-            const bool keeps = !(p == 0.f);
+            const float p = rows_pair_sum(mine);
+            const bool keeps = rows_pair_sum(kept) != 0.f;
             const unsigned char *row = vt + j * ROW_BYTES;
 #pragma unroll
             for (int b = 0; b < D_BLOCKS; ++b)

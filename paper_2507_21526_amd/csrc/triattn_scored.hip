@@ -353,7 +353,7 @@ __global__ __launch_bounds__(NW * 64, D == 64 ? 3 : 2) void scored_attn_kernel(S
             end_phase(true);
             products(smem);
             softmax(now);
-            rb.accumulate_by_key(smem + TILE_BYTES, p);
+            rb.accumulate_by_key(smem + TILE_BYTES, s, p);
             end_phase(false);
         }
     };

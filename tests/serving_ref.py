@@ -61,13 +61,19 @@ def attend(q, k, v, keep, dist, scale, softcap=None, slopes=None):
     return o, lse, absw
 
 
-def check(o, lse, ref, dtype, label):
-    """o [R, hq, d], lse [R, hq] or None against attend()'s result."""
+def check(o, lse, ref, dtype, label, underflow=False):
+    """o [R, hq, d], lse [R, hq] or None against attend()'s result.  With
+    `underflow`, an infinite value whose key has a score of 104 or more below
+    the row's largest may also give NaN: e^-104 = 2^-150 is 0 in fp32, and 0
+    times infinity NaN, where 64 bits hold the probability."""
     ro, rl, absw = ref
     o = o.double()
     fine = torch.isfinite(ro)
-    assert torch.equal(torch.isnan(o), torch.isnan(ro)), label
-    assert torch.equal(o[~fine & ~torch.isnan(ro)], ro[~fine & ~torch.isnan(ro)]), label
+    if underflow:
+        assert torch.equal(torch.isfinite(o), fine), label
+    else:
+        assert torch.equal(torch.isnan(o), torch.isnan(ro)), label
+        assert torch.equal(o[~fine & ~torch.isnan(ro)], ro[~fine & ~torch.isnan(ro)]), label
     err = (o - ro).abs()[fine]
     tol = o_tolerance(ro, absw, dtype)[fine]
     worst = float((err / tol).max()) if err.numel() else 0.0

@@ -116,6 +116,41 @@ def test_pages_past_the_held_ids():
           "segments")
 
 
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_largest_batch(d, ragged):
+    lens = [(7 * i) % 90 for i in range(1024)]
+    ql = [(i % 3) for i in range(1024)] if ragged else [1] * 1024
+    c = Cache(lens, 1, d, 16, prefix=20, seed=8)
+    q = _q(sum(ql), 2, d, 9)
+    o, l = _call(c, q, ql, torch.float32)
+    pick = list(range(0, 1024, 37)) + [1023]
+    starts = [0]
+    for n in ql:
+        starts.append(starts[-1] + n)
+    some = [i for i in pick if ql[i]]
+    at = torch.cat([torch.arange(starts[i], starts[i + 1]) for i in some]).cuda()
+    sub = Cache([1], 1, d, 16)
+    sub.k, sub.v, sub.prefix, sub.prefix_pages = c.k, c.v, c.prefix, c.prefix_pages
+    sub.lens, sub.table = [lens[i] for i in some], c.table[some]
+    check(o[at], l[at], sub.reference(q[at], [ql[i] for i in some], d ** -0.5), torch.float32,
+          "1024 requests")
+
+
+def test_many_row_tiles():
+    """Near the limit of row tiles: a long piece of a prompt, many heads."""
+    c = Cache([30000, 40], 1, 64, 256, seed=9)
+    q = _q(30000 + 2, 8, 64, 10)
+    o, l = _call(c, q, [30000, 2], ragged=True)
+    rows = torch.cat([torch.arange(0, 30000, 1777), torch.tensor([29999])]).cuda()
+    k, v = c.keys(0)
+    dist = rows[:, None] - torch.arange(30000, device="cuda")
+    from tests.serving_ref import attend
+    check(o[rows], l[rows], attend(q[rows], k, v, dist >= 0, dist, 0.125), torch.bfloat16, "piece")
+    c.lens, c.table = [40], c.table[1:]
+    check(o[30000:], l[30000:], c.reference(q[30000:], [2], 0.125), torch.bfloat16, "two rows")
+
+
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
 @pytest.mark.parametrize("d,ql", [(64, 4), (128, 4), (128, 50)])
 def test_values_behind_a_row(bad, d, ql):

@@ -41,7 +41,8 @@ def _run(kind, cu, hq, hkv, d, tile, S, W, L, cap, slopes, dtype, splits=0, seed
     return q, k, v, o, lse, plan
 
 
-def _verify(kind, cu, q, k, v, o, lse, tile, S, W, L, cap, slopes, label, lists=None, rows=None):
+def _verify(kind, cu, q, k, v, o, lse, tile, S, W, L, cap, slopes, label, lists=None, rows=None,
+            underflow=False):
     for i, (a, b) in enumerate(zip(cu, cu[1:])):
         n = b - a
         if n == 0:
@@ -52,7 +53,8 @@ def _verify(kind, cu, q, k, v, o, lse, tile, S, W, L, cap, slopes, label, lists=
         dist = pick[:, None] - torch.arange(n, device="cuda")
         ref = attend(q[a:b][pick], k[a:b], v[a:b], keep[pick], dist, q.shape[2] ** -0.5, cap,
                      slopes)
-        check(o[a:b][pick], lse[:, a:b].t()[pick], ref, o.dtype, f"{label} sequence {i}")
+        check(o[a:b][pick], lse[:, a:b].t()[pick], ref, o.dtype, f"{label} sequence {i}",
+              underflow)
 
 
 CASES = [
@@ -203,3 +205,49 @@ def test_empty_batches_and_streams():
         torch.cuda.synchronize()
         assert torch.equal(o, o2)
         plan.run(q, k, v, torch.empty_like(o), softcap=9.0)
+
+
+EIGHT = [
+    # kind, cu, hq, hkv, tile, S, W, L: over 512 workgroups of eight waves
+    ("causal", [0, 4500], 32, 8, 128, 0, 1, 0),
+    ("causal", [0, 700, 701, 4500], 32, 4, 64, 0, 1, 0),  # (11 + 1 + 60) 2 4 = 576
+    ("triangle", [0, 3001, 5200], 24, 8, 128, 70, 300, 100),  # a group of three: four waves
+    ("triangle", [0, 3001, 5200], 32, 8, 128, 70, 300, 100),
+    ("blocksparse", [0, 3000, 4700], 32, 8, 128, 0, 1, 0),
+]
+
+
+@pytest.mark.parametrize("case", EIGHT, ids=lambda c: f"{c[0]}-{c[1][-1]}-{c[2]}-{c[3]}-{c[4]}")
+@pytest.mark.parametrize("score", ["cap", "slopes"])
+@pytest.mark.parametrize("odd", [False, True])
+def test_larger_launches(case, score, odd):
+    """The eight-wave form (and, for a group that does not fill it, the
+    four-wave one), also with infinite values in masked steps."""
+    from tests.parity import kernels_of
+    kind, cu, hq, hkv, tile, S, W, L = case
+    cap, sl = (20.0, None) if score == "cap" else (None, geometric_slopes(hq))
+    blocks, per = _lists(cu, tile, 4) if kind == "blocksparse" else (None, None)
+    q, k, v = (t.cuda() for t in draw_qkv(cu, hq, hkv, 128, 21, key0_boost=8.0))
+    if odd:
+        for j in (cu[1] - 1, cu[-1] - 30, 100):
+            v[j, 0, 7] = math.inf
+    out = {}
+    names = kernels_of(lambda: out.update(r=_run(
+        kind, cu, hq, hkv, 128, tile, S, W, L, cap, sl, torch.bfloat16, blocks=blocks,
+        qkv=(q, k, v))))
+    waves = 8 if (hq // hkv * tile // 32) % 8 == 0 else 4
+    assert any(f"{waves}>" in n for n in names if "scored_attn" in n), names
+    q, k, v, o, lse, _ = out["r"]
+    heads = [0, hq // hkv, hq - 1]
+
+    def rows(n):
+        g = torch.Generator().manual_seed(n)
+        r = torch.cat([torch.randint(0, n, (50,), generator=g),
+                       torch.tensor([0, n - 1, n // 2, max(0, n - 31)])])
+        return r.unique().cuda()
+
+    for h in heads:
+        one = [h * hkv // hq]
+        _verify(kind, cu, q[:, [h]], k[:, one], v[:, one], o[:, [h]], lse[[h]], tile, S, W, L, cap,
+                sl[[h]] if sl is not None else None, f"{case} {score} {odd} head {h}", per, rows,
+                underflow=odd and score == "slopes")
