@@ -534,9 +534,12 @@ def kv_cache_write(k, v, slots, k_cache, v_cache, stream=None):
     _check_operands([("k_cache", k_cache, torch.bfloat16, shape),
                      ("v_cache", v_cache, torch.bfloat16, shape),
                      ("slots", slots, torch.int32, (total,))], dev)
-    _launch(dev, stream, lib().kv_cache_write, k.data_ptr(), v.data_ptr(), k.stride(0),
-            k.stride(1), v.stride(0), v.stride(1), slots.data_ptr(), total, k_cache.data_ptr(),
-            v_cache.data_ptr(), pages, hkv, page_size, d)
+    # (the stride of a dimension of one says nothing)
+    many, heads = total > 1, hkv > 1
+    _launch(dev, stream, lib().kv_cache_write, k.data_ptr(), v.data_ptr(),
+            k.stride(0) if many else 0, k.stride(1) if heads else 0,
+            v.stride(0) if many else 0, v.stride(1) if heads else 0, slots.data_ptr(), total,
+            k_cache.data_ptr(), v_cache.data_ptr(), pages, hkv, page_size, d)
 
 
 def ta_paged_workspace_bytes(batch, total_tokens, ragged, prefix, hq, hkv, head_dim) -> int:
@@ -764,11 +767,11 @@ class Plan:
 
     def run(self, q, k, v, o, lse=None, softmax_scale=None, stream=None, softcap=None,
             slopes=None):
-        """softcap, slopes: modified scores (scored_attn_fwd); plain where
-        neither is given."""
+        """softcap, slopes: modified scores (scored_attn_fwd); plain scores
+        where neither is given (or softcap is 0)."""
         if softmax_scale is None:
             softmax_scale = 1.0 / float(q.shape[-1]) ** 0.5
-        if softcap is not None or slopes is not None:
+        if softcap or slopes is not None:
             scored_attn_fwd(q, k, v, o, lse, self.sched, self.info, softmax_scale, softcap,
                             slopes, self.workspace, stream)
         elif self.kind == TRIANGLE:

@@ -125,6 +125,16 @@ def test_cache_write(tokens, hkv, d, page, fused):
     assert torch.equal(kc, wk) and torch.equal(vc, wv)
 
 
+def test_cache_write_of_one_row_and_head():
+    """Dimensions of one may have any stride."""
+    x = torch.randn(40 * 64, device="cuda").bfloat16()
+    k, v = x.as_strided((1, 1, 64), (3, 5, 1)), x.as_strided((1, 1, 64), (1, 1, 1), 64)
+    kc = torch.zeros(2, 1, 16, 64, dtype=torch.bfloat16, device="cuda")
+    vc = torch.zeros_like(kc)
+    B.kv_cache_write(k, v, _ints([20]), kc, vc)
+    assert torch.equal(kc[1, 0, 4], x[:64]) and torch.equal(vc[1, 0, 4], x[64:128])
+
+
 def test_cache_write_keeps_bits():
     """Rows are moved as they are: NaN payloads, infinities, denormals."""
     bits = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)

@@ -103,6 +103,16 @@ def test_long_triangle_and_causal_rows():
         _verify(kind, cu, *out[:5], 128, 128, 1024, 128, cap, slopes, f"long {kind}", rows=rows)
 
 
+def test_a_cap_of_zero_is_none():
+    cu = [0, 300]
+    q, k, v = (t.cuda() for t in draw_qkv(cu, 4, 1, 64, 3))
+    plan = B.Plan("causal", cu, 0, 1, 0, 64, 4, 64)
+    a, b = torch.empty_like(q), torch.empty_like(q)
+    plan.run(q, k, v, a)
+    plan.run(q, k, v, b, softcap=0.0)
+    assert torch.equal(a, b)
+
+
 def test_a_wide_cap_and_no_slope_are_the_plain_pass():
     """Slopes of zero change nothing but the order of roundings."""
     cu = [0, 500, 800]
