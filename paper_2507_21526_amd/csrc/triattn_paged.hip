@@ -547,14 +547,40 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
                     step(i, std::integral_constant<int, 0>{});
             } else {
                 const int n = (key_end - seg0 * S::STEP + S::STEP - 1) / S::STEP;
-                auto key_of = [&](int i) TA_INLINE -> int {
-                    return (seg0 + (BACK ? n - 1 - i : i)) * S::STEP;
+                // Where step i's keys are: wave w copies the tile's w-th group.
+                // Found a step ahead, so that the copies go out between the first
+                // matrix instructions of a step without waiting for page ids.
+                struct Place {
+                    int key0;
+                    uint32_t lim;  // byte offset of the group's last row
+                    int64_t off;   // bytes to its first row
                 };
-                auto copies = [&](int key0, int stage) TA_INLINE {
-                    copy(key0, stage * S::STAGE_BYTES, K{});
-                    copy(key0, stage * S::STAGE_BYTES + S::TILE_BYTES, V{});
+                auto place = [&](int i) TA_INLINE -> Place {
+                    Place x;
+                    x.key0 = (seg0 + (BACK ? n - 1 - i : i)) * S::STEP;
+                    const int first = min(x.key0 + wave * GROUP, rt.limit - 1);
+                    x.lim = (uint32_t)(min(rt.limit - 1 - first, GROUP - 1) * ROW_BYTES);
+                    const int id = uni(s_page[(first >> a.page_log2) - page0]);
+                    x.off = (int64_t)id * page_stride + (first & page_mask) * ROW_BYTES;
+                    return x;
                 };
-                copies(key_of(0), 0);
+                const uint32_t row_off = (uint32_t)(dma_row * ROW_BYTES);
+                auto copy_block = [&](const Place &x, int c, int stage) TA_INLINE {
+                    const bool v = c >= COPIES;
+                    const int m = v ? c - COPIES : c;
+                    const uint32_t swz =
+                        v ? dma_v - row_off
+                          : (dma_k - row_off) ^ (uint32_t)(rows_kswz<D>(m * COPY_ROWS) << 4);
+                    copy_to_lds16((v ? vc : kc) + x.off,
+                                  min(row_off + (uint32_t)(m * 1024), x.lim) + swz,
+                                  smem_addr + stage * S::STAGE_BYTES + (v ? S::TILE_BYTES : 0) +
+                                      wave * GROUP * ROW_BYTES + m * 1024);
+                };
+                constexpr int STRIDE = S::NKB * (D / 16) / (2 * COPIES);
+                Place now = place(0), next = place(min(1, n - 1));
+#pragma unroll
+                for (int c = 0; c < 2 * COPIES; ++c)
+                    copy_block(now, c, 0);
                 auto step = [&](int i, auto stage) TA_INLINE {
                     constexpr int ST = decltype(stage)::value;
                     // this step's tile has landed for every wave, and every
@@ -563,12 +589,20 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
                     rows_wait_copies<0>();
                     barrier_no_fence();
                     __builtin_amdgcn_sched_barrier(0);
-                    if (i + 1 < n)
-                        copies(key_of(i + 1), 1 - ST);
+                    // (after the last step the copies repeat its tile, into the
+                    // stage that nothing reads any more)
                     const unsigned char *kt = smem + ST * S::STAGE_BYTES;
-                    products(kt);
-                    softmax(key_of(i));
-                    values(key_of(i), kt + S::TILE_BYTES);
+                    rb.products(kt, s, [&](int m) TA_INLINE {
+                        if (m % STRIDE == STRIDE - 1 && m / STRIDE < 2 * COPIES)
+                            copy_block(next, m / STRIDE, 1 - ST);
+                    });
+                    rb.template schedule<true, false>();
+                    __builtin_amdgcn_sched_barrier(0);
+                    const int key0 = now.key0;
+                    now = next;
+                    next = place(min(i + 2, n - 1));
+                    softmax(key0);
+                    values(key0, kt + S::TILE_BYTES);
                 };
                 int i = 0;
                 for (; i + 1 < n; i += 2) {
@@ -577,6 +611,7 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
                 }
                 if (i < n)
                     step(i, std::integral_constant<int, 0>{});
+                rows_wait_copies<0>();
             }
         }
         return odd;
