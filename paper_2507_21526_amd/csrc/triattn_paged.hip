@@ -382,6 +382,8 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
         const int first_last =
             PREFIX ? a.prefix_len - 1
                    : rt.pos0 + div_group(rt.rho0 + min(block0, rt.rows - 1));
+        const int tile_first_last =
+            PREFIX ? a.prefix_len - 1 : rt.pos0 + div_group(rt.rho0);
         // distances in the prefix pass are taken from the prefix's end: the
         // join adds what each row is past it
         const int dist_row = PREFIX ? a.prefix_len : last;
@@ -468,8 +470,9 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
                 fresh = false;
             };
             auto values = [&](int key0, const unsigned char *vt) TA_INLINE {
-                const bool masked = key0 + S::TK - 1 > first_last;
-                if (__builtin_expect(masked, 0)) {
+                // (a step that any of the tile's rows masks: the waves look at a
+                // part of the values each)
+                if (__builtin_expect(key0 + S::TK - 1 > tile_first_last, 0)) {
                     asm volatile("");
                     odd |= rb.odd_values(vt, lane, RB == 1 ? 0 : wave, RB);
                 }
@@ -1021,7 +1024,7 @@ extern "C" ta_status paged_attn_fwd(const void *q, const void *k_cache, const vo
     // steps are counted in 32 bits
     const int64_t steps = (int64_t)p.max_tiles * ((int64_t)table_width * page_size / 64 + 1);
     const int64_t pre_tiles = (total_tokens * group + 32 * p.pre_rb - 1) / (32 * p.pre_rb);
-    if (steps > INT32_MAX || pre_tiles * (prefix_len / 64 + 1) > INT32_MAX)
+    if (steps > INT32_MAX / 2 || pre_tiles * (prefix_len / 64 + 1) > INT32_MAX / 2)
         return fail(TA_ERR_UNSUPPORTED, "%s: too many steps", fn);
     if (total_tokens == 0 || batch == 0)
         return TA_OK;

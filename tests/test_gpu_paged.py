@@ -171,6 +171,26 @@ def test_values_behind_a_row(bad, d, ql):
     check(o, l, ref, torch.float32, f"{bad} d {d} rows {ql}")
 
 
+@pytest.mark.parametrize("hq,d", [(1, 128), (1, 64), (3, 128), (8, 64)])
+def test_values_in_every_part_of_a_step(hq, d):
+    """Rows of one head or few: at one step some waves of a row tile drop keys
+    and others keep all of them.  A value of each key in turn is infinite; no
+    row before the key sees it."""
+    n = 128
+    c = Cache([n], 1, d, 16, seed=5)
+    q = _q(n, hq, d, 12)
+    clean, _ = _call(c, q, [n], torch.float32, ragged=True)
+    keep = c.v.clone()
+    for j in range(0, n, 3):
+        c.v.copy_(keep)
+        c.v[int(c.table[0, j // 16]), 0, j % 16, j % d] = math.inf
+        o, _ = _call(c, q, [n], torch.float32, ragged=True)
+        assert bool(torch.isfinite(o[:j]).all()), j
+        # the same sums, key by key: bits may differ by their order
+        assert float((o[:j] - clean[:j]).abs().max() if j else 0.0) < 1e-5, j
+        assert not bool(torch.isfinite(o[j:, :, j % d]).any()), j
+
+
 def test_bad_pages_and_lengths_show():
     """A page id outside the cache, and a length past the table, give NaN in
     the rows of that request and nowhere else; bad query offsets in all."""

@@ -155,6 +155,23 @@ def test_values_of_masked_keys(bad, kind, d, W):
     _verify(kind, cu, *out[:5], 64, 0, W, 0, 20.0, None, f"{kind} {bad}")
 
 
+@pytest.mark.parametrize("hq,d,tile", [(1, 128, 128), (1, 64, 128), (3, 128, 128), (2, 64, 64)])
+def test_values_in_every_part_of_a_step(hq, d, tile):
+    """Waves of one workgroup with other rows: at one step some drop keys and
+    others keep all of them."""
+    n = 128
+    q, k, v = (t.cuda() for t in draw_qkv([0, n], hq, 1, d, 13))
+    args = ("causal", [0, n], hq, 1, d, tile, 0, 1, 0, 20.0, None, torch.float32)
+    clean = _run(*args, qkv=(q, k, v))[3]
+    for j in range(0, n, 3):
+        w = v.clone()
+        w[j, 0, j % d] = math.inf
+        o = _run(*args, qkv=(q, k, w))[3]
+        assert bool(torch.isfinite(o[:j]).all()), j
+        assert float((o[:j] - clean[:j]).abs().max() if j else 0.0) < 1e-5, j
+        assert not bool(torch.isfinite(o[j:, :, j % d]).any()), j
+
+
 def test_infinite_keys_at_masked_places():
     """A NaN key that a row does not keep changes nothing for it."""
     cu = [0, 200]
