@@ -4,13 +4,13 @@
 //
 // A workgroup of four or eight waves takes as many row blocks (32 rows of one
 // head) of a schedule item, dealt out head first, over K/V tiles of 64 keys in
-// LDS.  What bounds it: a plain product pair takes a wave 32 matrix instructions of
-// 32 cycles a step.  A capped score takes two exp2 and a reciprocal (16 cycles each)
-// and five plain operations (4 each): 2240 cycles of the vector unit a step, more
-// than the matrix cores' 1024; the 16384-token causal layer (32 heads over 8, d =
-// 128) runs at 2450 cycles a wave and step, 2.41 ms, 912 TFLOP/s.  Slopes add one
-// operation to a plain score: packed 42000 tokens at window 2048 in 1.35 ms, 1085
-// TFLOP/s, matrix cores 56 % busy.
+// LDS.  What bounds it: the two products take a wave 32 matrix instructions of 32
+// cycles a step.  A capped score takes two exp2 and a reciprocal, quarter-rate
+// instructions, and five plain ones: some 2200 cycles of the vector unit a step,
+// more than the matrix cores' 1024.  The 16384-token causal layer (32 heads over 8,
+// d = 128) runs at 2230 cycles a wave and step, 2.44 ms, 902 TFLOP/s.  Slopes add
+// one operation to a plain score: packed 42000 tokens at window 2048 in 1.37 ms,
+// 1072 TFLOP/s, matrix cores 55 % busy.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
