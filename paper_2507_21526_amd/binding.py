@@ -407,8 +407,7 @@ def _launch(device, stream, fn, *args):
 
 
 def _check_operands(named, dev):
-    """named: (name, tensor, dtype, shape); a None in a shape leaves that
-    length open, a None in place of the shape leaves it all open."""
+    """named: (name, tensor, dtype, shape or None: any)."""
     import torch
     tensor = torch.Tensor
     for name, t, dtype, shape in named:
@@ -419,24 +418,28 @@ def _check_operands(named, dev):
             raise ValueError(f"{name} must be a torch tensor")
         if t.dtype != dtype:
             raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-        if shape is not None and (t.dim() != len(shape) or any(
-                b is not None and a != b for a, b in zip(t.shape, shape))):
+        if shape is not None and t.shape != shape:
             raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
         if not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
         if t.device != dev:
             raise ValueError(f"{name} is on {t.device}, not on {dev}: all operands must be on "
                              "one device")
+
+
+def _check_gpu(dev):
     if dev.type != "cuda":
         raise ValueError(f"operands must be on a GPU, got {dev}")
 
 
-def _open(t, shape):
-    """shape with the tensor's own lengths where it leaves them open."""
-    own = getattr(t, "shape", None)
-    if own is None or len(own) != len(shape):
-        return shape
-    return tuple(a if b is None else b for a, b in zip(own, shape))
+def _check_vector(name, t):
+    if t.dim() != 1:
+        raise ValueError(f"{name} must have one dimension, got {tuple(t.shape)}")
+
+
+def _check_table(t, batch):
+    if t.dim() != 2 or t.shape[0] != batch:
+        raise ValueError(f"block_table must be ({batch}, pages), got {tuple(t.shape)}")
 
 
 def _addr(t):
@@ -490,11 +493,14 @@ def page_map(cached_lens, new_lens, block_table, free_pages, n_free, page_size, 
         raise ValueError("cached_lens must be a tensor [requests]")
     b, dev = cached_lens.shape[0], cached_lens.device
     _check_operands([("cached_lens", cached_lens, i32, (b,)), ("new_lens", new_lens, i32, (b,)),
-                     ("block_table", block_table, i32, _open(block_table, (b, None))),
-                     ("free_pages", free_pages, i32, _open(free_pages, (None,))),
+                     ("block_table", block_table, i32, None), ("free_pages", free_pages, i32, None),
                      ("n_free", n_free, i32, (1,)), ("kv_lens", kv_lens, i32, (b,)),
-                     ("cu_new", cu_new, i32, (b + 1,)), ("slots", slots, i32, _open(slots, (None,))),
+                     ("cu_new", cu_new, i32, (b + 1,)), ("slots", slots, i32, None),
                      ("state", state, i32, (2,))], dev)
+    _check_table(block_table, b)
+    _check_vector("free_pages", free_pages)
+    _check_vector("slots", slots)
+    _check_gpu(dev)
     _launch(dev, stream, lib().ta_page_map, cached_lens.data_ptr(), new_lens.data_ptr(), b,
             int(page_size), block_table.data_ptr(), block_table.shape[1], free_pages.data_ptr(),
             free_pages.shape[0], n_free.data_ptr(), kv_lens.data_ptr(), cu_new.data_ptr(),
@@ -534,6 +540,7 @@ def kv_cache_write(k, v, slots, k_cache, v_cache, stream=None):
     _check_operands([("k_cache", k_cache, torch.bfloat16, shape),
                      ("v_cache", v_cache, torch.bfloat16, shape),
                      ("slots", slots, torch.int32, (total,))], dev)
+    _check_gpu(dev)
     # (the stride of a dimension of one says nothing)
     many, heads = total > 1, hkv > 1
     _launch(dev, stream, lib().kv_cache_write, k.data_ptr(), v.data_ptr(),
@@ -577,7 +584,7 @@ def paged_attn_fwd(q, k_cache, v_cache, o, lse, kv_lens, cu_q, block_table, pref
     i32 = torch.int32
     named = [("q", q, torch.bfloat16, None), ("k_cache", k_cache, torch.bfloat16, shape),
              ("v_cache", v_cache, torch.bfloat16, shape), ("o", o, o.dtype, (total, hq, d)),
-             ("kv_lens", kv_lens, i32, (b,)), ("block_table", block_table, i32, _open(block_table, (b, None)))]
+             ("kv_lens", kv_lens, i32, (b,)), ("block_table", block_table, i32, None)]
     if lse is not None:
         named.append(("lse", lse, torch.float32, (hq, total)))
     if cu_q is not None:
@@ -588,12 +595,16 @@ def paged_attn_fwd(q, k_cache, v_cache, o, lse, kv_lens, cu_q, block_table, pref
     if prefix_len < 0:
         raise ValueError(f"prefix_len {prefix_len} < 0")
     if prefix_len > 0:
-        named.append(("prefix_pages", prefix_pages, i32, _open(prefix_pages, (None,))))
+        named.append(("prefix_pages", prefix_pages, i32, None))
     if workspace is not None:
         named.append(("workspace", workspace, workspace.dtype, None))
     if slopes is not None:
         named.append(("slopes", slopes, torch.float32, (hq,)))
     _check_operands(named, dev)
+    _check_table(block_table, b)
+    if prefix_len > 0:
+        _check_vector("prefix_pages", prefix_pages)
+    _check_gpu(dev)
     if prefix_len > 0 and prefix_pages.shape[0] * page_size < prefix_len:
         raise ValueError(f"{prefix_pages.shape[0]} prefix pages of {page_size} hold no "
                          f"{prefix_len} keys")
