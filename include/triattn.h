@@ -405,9 +405,11 @@ ta_status kv_cache_write(const void *k, const void *v, int64_t k_token_stride,
  *                streams) need workspaces of their own.
  * Device data that cannot be followed shows as NaN: a page id outside the
  * cache in the rows that need it, a length past the block table in its
- * request's rows, cu_q that is not 0 <= ... <= total_tokens from 0 on in every
- * row.  No access leaves the caller's buffers.  Unsupported: more than 2048
- * row tiles, total_tokens * (hq / hkv) / 128 + batch with long query lengths.
+ * request's rows, and in every row a cu_q that does not start at 0, decreases
+ * or passes total_tokens.  No access leaves the caller's buffers.
+ * Unsupported: more than 2048 row tiles a kv head, that is
+ * total_tokens * (hq / hkv) / 128 + batch > 2048 where requests have more than 32
+ * query rows a kv head on average (longer prompts go in pieces).
  */
 size_t ta_paged_workspace_bytes(int32_t batch, int64_t total_tokens,
                                 int32_t ragged, int32_t prefix, int32_t hq,

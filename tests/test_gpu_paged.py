@@ -274,6 +274,37 @@ def test_same_bits_again_and_on_another_stream():
     assert torch.equal(o, o3)
 
 
+def test_two_calls_at_once():
+    """Two plans on two streams, several calls in flight."""
+    c = Cache([5000, 40, 2000], 2, 128, 16, prefix=500, seed=16)
+    side, calls = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for i in range(2):
+        q = _q(3, 8, 128, 30 + i)
+        plan = B.PagedPlan(3, 3, 8, 2, 128, prefix=True)
+        want = torch.empty_like(q)
+        plan.run(q, c.k, c.v, want, c.kv_lens, c.table, prefix_pages=c.prefix_pages,
+                 prefix_len=500)
+        calls.append((q, plan, want, [torch.zeros_like(q) for _ in range(8)]))
+    torch.cuda.synchronize()
+    for j in range(8):
+        for (q, plan, _, outs), stream in zip(calls, side):
+            plan.run(q, c.k, c.v, outs[j], c.kv_lens, c.table, prefix_pages=c.prefix_pages,
+                     prefix_len=500, stream=stream)
+    torch.cuda.synchronize()
+    for _, _, want, outs in calls:
+        assert all(torch.equal(o, want) for o in outs)
+
+
+@pytest.mark.parametrize("ql", [1, 40])
+def test_slopes_of_either_sign(ql):
+    """Scores that grow with the distance, fall with it, or do not change."""
+    sl = torch.tensor([-0.1, 0.0, 0.05, -0.01, 0.5, -0.03, 1.0, 0.2], device="cuda")
+    c = Cache([700, 90], 2, 64, 16, prefix=130, seed=17)
+    q = _q(2 * ql, 8, 64, 18)
+    o, l = _call(c, q, [ql, ql], torch.float32, None, sl, ragged=ql > 1)
+    check(o, l, c.reference(q, [ql, ql], 0.125, None, sl), torch.float32, f"signs {ql}")
+
+
 def test_captured_call_follows_lengths_and_tables():
     lens = [700, 33, 64]
     c = Cache(lens, 2, 64, 16, seed=13)

@@ -103,6 +103,15 @@ def test_long_triangle_and_causal_rows():
         _verify(kind, cu, *out[:5], 128, 128, 1024, 128, cap, slopes, f"long {kind}", rows=rows)
 
 
+@pytest.mark.parametrize("kind", ["causal", "triangle"])
+def test_slopes_of_either_sign(kind):
+    """Scores that grow with the distance, fall with it, or do not change."""
+    sl = torch.tensor([-0.1, 0.0, 0.05, -0.01, 0.5, -0.03, 1.0, 0.2], device="cuda")
+    cu = [0, 600, 777]
+    out = _run(kind, cu, 8, 2, 128, 128, 8, 100, 30, None, sl, torch.float32)
+    _verify(kind, cu, *out[:5], 128, 8, 100, 30, None, sl, f"signs {kind}")
+
+
 def test_a_cap_of_zero_is_none():
     cu = [0, 300]
     q, k, v = (t.cuda() for t in draw_qkv(cu, 4, 1, 64, 3))
