@@ -54,7 +54,9 @@ __device__ __forceinline__ Runs reach(Runs r, bool stream, int sink, int window,
 {
     if (stream) {
         const int band = max(wr0 - window + 1, 0) / kKeys;
-        const int sinks = (sink + kKeys - 1) / kKeys;
+        // (a sink past the rows is one of all their keys; its own length may be
+        // any number of 32 bits)
+        const int sinks = (min(sink, wr1 + 1) + kKeys - 1) / kKeys;
         if (r.b_hi > r.b_lo) {
             r.a_hi = max(min(r.a_hi, sinks), r.a_lo);
             r.b_lo = min(max(r.b_lo, band), r.b_hi);

@@ -287,3 +287,25 @@ def test_larger_launches(case, score, odd):
         _verify(kind, cu, q[:, [h]], k[:, one], v[:, one], o[:, [h]], lse[[h]], tile, S, W, L, cap,
                 sl[[h]] if sl is not None else None, f"{case} {score} {odd} head {h}", per, rows,
                 underflow=odd and score == "slopes")
+
+
+@pytest.mark.parametrize("sink", [2 ** 31 - 1, 2 ** 31 - 63, 2 ** 31 - 64])
+@pytest.mark.parametrize("d,hq,last", [(128, 4, 0), (64, 3, 40)])
+@pytest.mark.parametrize("score", ["cap", "slopes"])
+def test_every_key_a_sink(sink, d, hq, last, score):
+    """A sink longer than any sequence, up to the largest number: every row
+    keeps all earlier keys."""
+    cu = [0, 1000, 1013, 1300]
+    cap, sl = (20.0, None) if score == "cap" else (None, geometric_slopes(hq))
+    out = _run("triangle", cu, hq, 1, d, 64, sink, 64, last, cap, sl, torch.float32)
+    _verify("triangle", cu, *out[:5], 64, sink, 64, last, cap, sl, f"sink {sink} {score}")
+
+
+def test_every_key_a_sink_in_eight_waves():
+    cu = [0, 4500]  # 36 items of 2 workgroups a kv head
+    sl = geometric_slopes(32)
+    qkv = tuple(t.cuda() for t in draw_qkv(cu, 32, 8, 128, 22))
+    want = _run("triangle", cu, 32, 8, 128, 128, 4500, 128, 0, None, sl, torch.bfloat16, qkv=qkv)
+    got = _run("triangle", cu, 32, 8, 128, 128, 2 ** 31 - 1, 128, 0, None, sl, torch.bfloat16,
+               qkv=qkv)
+    assert torch.equal(got[3], want[3]) and torch.equal(got[4], want[4])
