@@ -279,7 +279,9 @@ __device__ __forceinline__ void trim_runs(bool stream, int sink, int window, int
     if (stream) {
         const int first = wr0 - window + 1;
         const int fs = first > 0 ? first / kStep : 0;  // first step with a window key
-        const int ss = (sink + kStep - 1) / kStep;     // steps with a sink key
+        // steps with a sink key (cut at the rows: a sink may be any number of
+        // 32 bits)
+        const int ss = (min(sink, wr_last + 1) + kStep - 1) / kStep;
         if (b_hi > b_lo) {
             // run a holds the sink k-tiles, run b the band
             b_lo = min(max(b_lo, fs), b_hi);

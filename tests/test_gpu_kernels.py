@@ -377,3 +377,23 @@ def test_graph_replay_matches_eager(kind):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(o, o_ref) and torch.equal(lse, l_ref)
+
+
+@pytest.mark.parametrize("sink", [2 ** 31 - 1, 2 ** 31 - 63, 2 ** 31 - 64])
+@pytest.mark.parametrize("d,last", [(128, 0), (64, 40)])
+def test_every_key_a_sink(sink, d, last):
+    """A sink longer than any sequence, up to the largest number: every row
+    keeps all earlier keys."""
+    _full_check("triangle", [0, 1000, 1013, 1300], 4, 1, d, sink, 64, last, 64, seed=31,
+                label=f"sink {sink} d {d}")
+
+
+@pytest.mark.parametrize("cu,hq,hkv,d,W,T", [
+    ([0, 6000], 32, 8, 128, 128, 128), ([0, 6000], 28, 4, 128, 128, 128),
+    ([0, 6000], 32, 8, 64, 128, 128), (list(range(0, 9000, 300)), 32, 8, 128, 64, 64)])
+def test_every_key_a_sink_in_larger_launches(cu, hq, hkv, d, W, T):
+    q, k, v = _cuda(*draw_qkv(cu, hq, hkv, d, 32))
+    n = max(b - a for a, b in zip(cu, cu[1:]))
+    want = run_pass("triangle", q, k, v, cu, n, W, 0, T, poison=True)
+    got = run_pass("triangle", q, k, v, cu, 2 ** 31 - 1, W, 0, T, poison=True)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
