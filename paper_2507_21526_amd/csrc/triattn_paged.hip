@@ -170,7 +170,8 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
     __shared__ int32_t s_page[kPageEntries];
     __shared__ int32_t s_wave[kThreads / 64];
     __shared__ float s_ml[S::KS][32][2];
-    __shared__ int32_t s_bad;
+    __shared__ int32_t s_bad;      // query offsets that are none
+    __shared__ int32_t s_bad_key;  // first key of the piece in a page that is none
 
     const int tid = threadIdx.x;
     const int lane = tid & 63;
@@ -389,7 +390,7 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
         const int dist_row = PREFIX ? a.prefix_len : last;
         const int32_t *pages = PREFIX ? a.prefix_pages : a.table + (int64_t)rt.req * a.width;
         if (tid == 0)
-            s_bad = 0;
+            s_bad_key = INT32_MAX;
         // One pass over the piece's steps.  Returns whether a masked step holds
         // infinite or NaN values; the `careful` pass then keeps them from the
         // rows that do not keep their keys.
@@ -413,7 +414,7 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
                 int32_t id = pages[page0 + i];
                 if (id < 0 || id >= a.num_pages) {
                     id = 0;
-                    s_bad = 1;
+                    atomicMin(&s_bad_key, (page0 + i) << a.page_log2);
                 }
                 s_page[i] = id;
             }
@@ -651,8 +652,13 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
                 a.slot_lse[((int64_t)piece * a.hkv + g) * S::ROWS + r] = x;
             }
         };
-        __syncthreads();  // the stages are done with, and s_bad is final
-        const float nan_if_bad = s_bad != 0 ? __builtin_nanf("") : 0.f;
+        __syncthreads();  // the stages are done with, and s_bad_key is final
+        // what a row whose last key is this one shows: NaN from the first page
+        // that is none on (earlier rows of the tile do not keep its keys)
+        const int bad_key = s_bad_key;
+        auto nan_if_bad = [&](int last_key) TA_INLINE -> float {
+            return last_key >= bad_key ? __builtin_nanf("") : 0.f;
+        };
         if constexpr (RB == 1) {
             // join the waves: each leaves its accumulators in its buffers,
             // 16-byte chunks of row r permuted by r against bank conflicts
@@ -700,20 +706,22 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
                     for (int e = 0; e < 4; ++e)
                         x[e] += f * y[e];
                 }
-                const float inv = (den == 0.f ? 0.f : 1.f / den) + nan_if_bad;
+                const float nan = nan_if_bad(PREFIX ? last : rt.pos0 + div_group(rt.rho0 + r));
+                const float inv = (den == 0.f ? 0.f : 1.f / den) + nan;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     x[e] *= inv;
                 store4(x, r, d0);
                 if (d0 == 0)
-                    store_lse((den == 0.f ? -INFINITY : (m + __log2f(den)) * kRowsLn2) +
-                                  nan_if_bad, r);
+                    store_lse((den == 0.f ? -INFINITY : (m + __log2f(den)) * kRowsLn2) + nan,
+                              r);
             }
         } else if (block0 + rb.col < rt.rows) {
             float inv, lse;
             rb.finish(inv, lse);
-            inv += nan_if_bad;
-            lse += nan_if_bad;
+            const float nan = nan_if_bad(last);
+            inv += nan;
+            lse += nan;
 #pragma unroll
             for (int b = 0; b < D_BLOCKS; ++b)
 #pragma unroll
@@ -727,7 +735,7 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
             if (rb.half == 0)
                 store_lse(lse, block0 + rb.col);
         }
-        __syncthreads();  // s_bad and the accumulators are read
+        __syncthreads();  // s_bad_key and the accumulators are read
     }
 }
 

@@ -380,3 +380,19 @@ def test_offsets_past_32_bits():
         assert torch.equal(k[s // 256, :, s % 256], rows[i])
         assert torch.equal(v[s // 256, :, s % 256], -rows[i])
     del small
+
+
+@pytest.mark.parametrize("ql,hq,hkv", [(2, 4, 1), (4, 8, 1), (60, 4, 2)])
+def test_a_bad_page_shows_in_the_rows_that_need_it(ql, hq, hkv):
+    """Rows of one row tile on both sides of a page that is none: the earlier
+    ones do not keep its keys."""
+    n, page = 64 + ql // 2, 16
+    c = Cache([n, 40], hkv, 64, page, seed=19)
+    q = _q(2 * ql, hq, 64, 19)
+    ref = c.reference(q, [ql, ql], 0.125)
+    c.table[0, 64 // page] = -1
+    o, l = _call(c, q, [ql, ql], torch.float32, ragged=True)
+    first = ql - ql // 2  # the row at position 64
+    assert bool(torch.isnan(o[first:ql]).all()) and bool(torch.isnan(l[first:ql]).all())
+    rest = torch.cat([torch.arange(first), torch.arange(ql, 2 * ql)]).cuda()
+    check(o[rest], l[rest], tuple(x[rest] for x in ref), torch.float32, f"bad page {ql}")
