@@ -1020,8 +1020,10 @@ extern "C" ta_status paged_attn_fwd(const void *q, const void *k_cache, const vo
                     (long long)total_tokens, batch);
     if (batch > TA_MAX_BATCH)
         return fail(TA_ERR_UNSUPPORTED, "%s: batch %d > %d", fn, batch, TA_MAX_BATCH);
-    if (num_pages > INT32_MAX / page_size || (int64_t)table_width * page_size > INT32_MAX ||
-        prefix_len > INT32_MAX - 256 || (int64_t)total_tokens * hq > INT32_MAX)
+    // (keys are walked in whole steps, whose ends stay in 32 bits too)
+    if (num_pages > INT32_MAX / page_size ||
+        (int64_t)table_width * page_size > INT32_MAX - 256 || prefix_len > INT32_MAX - 256 ||
+        (int64_t)total_tokens * hq > INT32_MAX)
         return fail(TA_ERR_UNSUPPORTED, "%s: positions, slots or rows past 32 bits", fn);
     const PagedLayout p =
         paged_layout(batch, total_tokens, cu_q != nullptr, prefix_len > 0, hq, hkv, head_dim);

@@ -190,3 +190,15 @@ def test_scored_binding_checks():
     with pytest.raises(ValueError, match="q must be bfloat16"):
         B.scored_attn_fwd(q.float(), _b(3, 2, 64), _b(3, 2, 64), q.clone(), None, sched, info, 0.1,
                           5.0, None, None)
+
+
+def test_paged_positions_stay_in_32_bits():
+    """Tables whose last step of keys would end past 2^31."""
+    far = FAKE + (1 << 40)  # half a gigabyte and more: behind every other argument
+    kw = dict(batch=1, total=1, table=far, hq=1, hkv=1)
+    for width, page in (((1 << 27) - 1, 16), ((1 << 27) - 16, 16), ((1 << 23) - 1, 256)):
+        assert _paged(width=width, page=page, **kw) == B.TA_ERR_UNSUPPORTED, (width, page)
+        assert "32 bits" in B.ta_last_error()
+    # the longest tables pass that check (and fail a later one)
+    assert _paged(width=(1 << 27) - 17, q=0, **kw) == B.TA_ERR_INVALID_ARG
+    assert _paged(width=(1 << 23) - 2, page=256, q=0, **kw) == B.TA_ERR_INVALID_ARG
