@@ -146,6 +146,13 @@ struct RowTile {
     int32_t bad;    // a length past the block table
 };
 
+// Log-sum-exps of rows whose scores grow with the distance count it from the
+// first key: what the row's own distance from there, `past` keys, adds.
+__device__ __forceinline__ float lse_shift(float slope, int past)
+{
+    return slope < 0.f ? -slope * (float)past : 0.f;
+}
+
 template <int D, int RB, int SCORE, bool PREFIX>
 __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
                              (PagedShape<D, RB>::WAVES_PER_SIMD)) void paged_attn_kernel(PagedArgs a)
@@ -385,9 +392,15 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
                    : rt.pos0 + div_group(rt.rho0 + min(block0, rt.rows - 1));
         const int tile_first_last =
             PREFIX ? a.prefix_len - 1 : rt.pos0 + div_group(rt.rho0);
-        // distances in the prefix pass are taken from the prefix's end: the
-        // join adds what each row is past it
-        const int dist_row = PREFIX ? a.prefix_len : last;
+        // Where distances are taken from, so that they are short at the keys
+        // that weigh most and round to little there: the row where scores fall
+        // with the distance (in the prefix pass the prefix's end: the join adds
+        // what each row is past it), the first key of all where they grow with
+        // it (the log-sum-exp gets what the row is past that at its very end).
+        int dist_row = PREFIX ? a.prefix_len : last;
+        if constexpr ((SCORE & kScoreSlope) != 0)
+            if (slope < 0.f)
+                dist_row = PREFIX ? 0 : -a.prefix_len;
         const int32_t *pages = PREFIX ? a.prefix_pages : a.table + (int64_t)rt.req * a.width;
         if (tid == 0)
             s_bad_key = INT32_MAX;
@@ -644,6 +657,8 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
             const int rr = rt.rho0 + r, qt = div_group(rr);
             const int h = g * a.group + rr - qt * a.group;
             if (to_o) {
+                if constexpr ((SCORE & kScoreSlope) != 0)
+                    x += lse_shift(a.score.slopes[h], rt.pos0 + qt);
                 if (a.lse)
                     a.lse[(int64_t)h * a.total_tokens + rt.q0 + qt] = x;
             } else if (whole) {
@@ -793,7 +808,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(JoinArgs a)
             prow = prho % a.pre_rows;
             pw0 = pbegin / a.pre_share;
             n_pre = (pbegin + a.pre_steps - 1) / a.pre_share - pw0 + 1;
-            if (a.slopes)  // its distances end at the prefix's end
+            if (a.slopes && a.slopes[h] > 0.f)  // its distances end at the prefix's end
                 shift = -a.slopes[h] * (float)(pos0 + qt);
         }
         const int n = n_pre + n_own;
@@ -869,7 +884,10 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(JoinArgs a)
         }
         if (a.lse && lane == 0)
             a.lse[(int64_t)h * a.total_tokens + q0 + qt] =
-                den == 0.f ? -INFINITY : m_use + __logf(den);
+                den == 0.f ? -INFINITY
+                           : m_use + __logf(den) +
+                                 (a.slopes ? lse_shift(a.slopes[h], a.prefix_len + pos0 + qt)
+                                           : 0.f);
     }
 }
 
@@ -1023,6 +1041,7 @@ extern "C" ta_status paged_attn_fwd(const void *q, const void *k_cache, const vo
     // (keys are walked in whole steps, whose ends stay in 32 bits too)
     if (num_pages > INT32_MAX / page_size ||
         (int64_t)table_width * page_size > INT32_MAX - 256 || prefix_len > INT32_MAX - 256 ||
+        (slopes && (int64_t)table_width * page_size + prefix_len > INT32_MAX - 256) ||
         (int64_t)total_tokens * hq > INT32_MAX)
         return fail(TA_ERR_UNSUPPORTED, "%s: positions, slots or rows past 32 bits", fn);
     const PagedLayout p =

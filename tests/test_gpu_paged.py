@@ -396,3 +396,36 @@ def test_a_bad_page_shows_in_the_rows_that_need_it(ql, hq, hkv):
     assert bool(torch.isnan(o[first:ql]).all()) and bool(torch.isnan(l[first:ql]).all())
     rest = torch.cat([torch.arange(first), torch.arange(ql, 2 * ql)]).cuda()
     check(o[rest], l[rest], tuple(x[rest] for x in ref), torch.float32, f"bad page {ql}")
+
+
+def _equal_far_keys(c, hq, places):
+    """Queries of one direction, and keys whose products make up for the bias
+    of slope -4 at these places from the first key (of the prefix): their
+    scores are equal, all others far below.  bf16 holds 2 x these places."""
+    c.k.zero_()
+    for j in places:
+        if j < c.prefix:
+            page, at = int(c.prefix_pages[j // c.page]), j % c.page
+        else:
+            page, at = int(c.table[0, (j - c.prefix) // c.page]), (j - c.prefix) % c.page
+        c.k[page, :, at, 0] = 2.0 * j  # 0.125 * 16 * 2 j = 4 j
+    return torch.full((hq,), -4.0, device="cuda")
+
+
+@pytest.mark.parametrize("d,ql,prefix", [(64, 1, 0), (64, 5, 0), (128, 40, 0), (64, 1, 300),
+                                         (128, 7, 300)])
+def test_scores_that_grow_over_far_distances(d, ql, prefix):
+    """Biases of 280000 between a row and the keys that it attends to, some
+    tiles apart, in the prefix and behind it: equal scores stay equal."""
+    c = Cache([70001], 1, d, 256, prefix=prefix, seed=20)
+    c.v.nan_to_num_()
+    sl = _equal_far_keys(c, 2, [0, 70, 140, 210, 350])
+    q = torch.zeros(ql, 2, d, dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 16.0
+    plan = B.PagedPlan(1, ql, 2, 1, d, prefix=prefix > 0, ragged=True)
+    cu = torch.tensor([0, ql], dtype=torch.int32, device="cuda")
+    o, l = torch.empty(ql, 2, d, device="cuda"), torch.empty(2, ql, device="cuda")
+    plan.run(q, c.k, c.v, o, c.kv_lens, c.table, cu_q=cu,
+             prefix_pages=c.prefix_pages if prefix else None, prefix_len=prefix, lse=l,
+             softmax_scale=0.125, slopes=sl)
+    check(o, l.t(), c.reference(q, [ql], 0.125, None, sl), torch.float32, f"far {d} {ql} {prefix}")

@@ -202,3 +202,18 @@ def test_paged_positions_stay_in_32_bits():
     # the longest tables pass that check (and fail a later one)
     assert _paged(width=(1 << 27) - 17, q=0, **kw) == B.TA_ERR_INVALID_ARG
     assert _paged(width=(1 << 23) - 2, page=256, q=0, **kw) == B.TA_ERR_INVALID_ARG
+
+
+def test_paged_distances_stay_in_32_bits():
+    """With slopes, distances from the prefix's first key are counted too."""
+    def call(slopes, prefix_len):
+        far = FAKE + (1 << 40)
+        return B.lib().paged_attn_fwd(
+            None, P(FAKE), P(FAKE + M), P(FAKE + 2 * M), 0, None, P(FAKE + 3 * M), None, P(far), 1,
+            1 << 22, P(far * 2), prefix_len, 1, 1, 1, 64, 9, 256, 0.1, 0.0, P(slopes),
+            P(FAKE + 4 * M), 1 << 40, None)
+
+    rest = 2 ** 31 - 257 - (1 << 30)
+    assert call(FAKE + 5 * M, rest + 1) == B.TA_ERR_UNSUPPORTED
+    assert call(FAKE + 5 * M, rest) == B.TA_ERR_INVALID_ARG  # q is NULL
+    assert call(0, rest + 1) == B.TA_ERR_INVALID_ARG
