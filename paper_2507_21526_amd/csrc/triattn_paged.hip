@@ -146,13 +146,6 @@ struct RowTile {
     int32_t bad;    // a length past the block table
 };
 
-// Log-sum-exps of rows whose scores grow with the distance count it from the
-// first key: what the row's own distance from there, `past` keys, adds.
-__device__ __forceinline__ float lse_shift(float slope, int past)
-{
-    return slope < 0.f ? -slope * (float)past : 0.f;
-}
-
 template <int D, int RB, int SCORE, bool PREFIX>
 __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
                              (PagedShape<D, RB>::WAVES_PER_SIMD)) void paged_attn_kernel(PagedArgs a)
@@ -658,7 +651,7 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
             const int h = g * a.group + rr - qt * a.group;
             if (to_o) {
                 if constexpr ((SCORE & kScoreSlope) != 0)
-                    x += lse_shift(a.score.slopes[h], rt.pos0 + qt);
+                    x += rows_lse_shift(a.score.slopes[h], rt.pos0 + qt);
                 if (a.lse)
                     a.lse[(int64_t)h * a.total_tokens + rt.q0 + qt] = x;
             } else if (whole) {
@@ -886,7 +879,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(JoinArgs a)
             a.lse[(int64_t)h * a.total_tokens + q0 + qt] =
                 den == 0.f ? -INFINITY
                            : m_use + __logf(den) +
-                                 (a.slopes ? lse_shift(a.slopes[h], a.prefix_len + pos0 + qt)
+                                 (a.slopes ? rows_lse_shift(a.slopes[h], a.prefix_len + pos0 + qt)
                                            : 0.f);
     }
 }

@@ -117,6 +117,13 @@ __device__ __forceinline__ void rows_poison(void *o, int o_f32, float *lse, int6
     }
 }
 
+// Log-sum-exps of rows whose scores grow with the distance count it from the
+// first key: what the row's own distance from there, `past` keys, adds.
+__device__ __forceinline__ float rows_lse_shift(float slope, int past)
+{
+    return slope < 0.f ? -slope * (float)past : 0.f;
+}
+
 // Score arguments of a call; false where a cap's factors leave fp32.
 inline bool rows_score_args(ScoreArgs &a, float softmax_scale, float softcap, const float *slopes)
 {
@@ -245,8 +252,8 @@ struct RowBlock {
     // is >= 0, so where their sum is at most kRowsRebase none exceeds it.
     // Otherwise (also when no reference is set yet: the sum is then infinite
     // or NaN) the row maxima are taken and the accumulators rescaled.
-    // dist0 = first key of the tile - this lane's row; fresh: the first step,
-    // which has no reference on any lane.
+    // dist0 = first key of the tile - the key that this lane's row counts
+    // distances from; fresh: the first step, which has no reference on any lane.
     __device__ __forceinline__ void softmax(const f32x16 (&s)[NKB], const ScoreArgs &a,
                                             float slope_log2, int dist0, bf16x8 (&pf)[NKB][2],
                                             bool fresh)

@@ -157,6 +157,15 @@ __global__ __launch_bounds__(NW * 64, D == 64 ? 3 : 2) void scored_attn_kernel(S
     float slope = 0.f;
     if constexpr ((SCORE & kScoreSlope) != 0)
         slope = a.score.slopes[head] * kRowsLog2e;
+    // Where distances are taken from, so that they are short at the keys that
+    // weigh most and round to little there: the row where scores fall with the
+    // distance, its first key where they grow with it (of all rows that have
+    // partials or a sink the sequence's first; the log-sum-exp gets what the row
+    // is past that at its very end).
+    int from = row;
+    if constexpr ((SCORE & kScoreSlope) != 0)
+        if (slope < 0.f)
+            from = stream && a.sink == 0 ? max(0, row - a.window + 1) : 0;
 
     // steps
     const int tps = a.tile / kKeys;
@@ -285,7 +294,7 @@ __global__ __launch_bounds__(NW * 64, D == 64 ? 3 : 2) void scored_attn_kernel(S
             asm volatile("");  // a branch: most steps have no mask
             mask(x.key0);
         }
-        rb.softmax(s, a.score, slope, x.key0 - row, p, fresh);
+        rb.softmax(s, a.score, slope, x.key0 - from, p, fresh);
         fresh = false;
     };
     // The values of a masked step, each wave its part of the tile (apart from
@@ -489,10 +498,13 @@ __global__ __launch_bounds__(NW * 64, D == 64 ? 3 : 2) void scored_attn_kernel(S
                     __builtin_convertvector(x, bf16x4r);
         }
     if (rb.half == 0) {
-        if (part_base >= 0)
+        if (part_base >= 0) {
             a.part_lse[prow * a.hq + head] = lse;
-        else if (a.lse)
+        } else if (a.lse) {
+            if constexpr ((SCORE & kScoreSlope) != 0)
+                lse += rows_lse_shift(a.score.slopes[head], row - from);
             a.lse[(int64_t)head * a.total_tokens + tok] = lse;
+        }
     }
 }
 
@@ -570,7 +582,9 @@ __global__ __launch_bounds__(kJoinThreads) void scored_join_kernel(ScoredArgs a)
     }
     if (a.lse && lane == 0)
         a.lse[(int64_t)head * a.total_tokens + tok] =
-            den == 0.f ? -INFINITY : m_use + __logf(den);
+            den == 0.f ? -INFINITY
+                       : m_use + __logf(den) +
+                             (a.score.slopes ? rows_lse_shift(a.score.slopes[head], r0 + r) : 0.f);
 }
 
 template <int D, bool LIST, int NW>

@@ -309,3 +309,69 @@ def test_every_key_a_sink_in_eight_waves():
     got = _run("triangle", cu, 32, 8, 128, 128, 2 ** 31 - 1, 128, 0, None, sl, torch.bfloat16,
                qkv=qkv)
     assert torch.equal(got[3], want[3]) and torch.equal(got[4], want[4])
+
+
+@pytest.mark.parametrize("kind,d", [("causal", 64), ("causal", 128), ("triangle", 128),
+                                    ("blocksparse", 64)])
+def test_scores_that_grow_over_far_distances(kind, d):
+    """Biases of 260000 between a row and the keys that it attends to, some
+    steps apart: equal scores stay equal.  (0.125 * 16 * 2 j makes up for slope
+    -4 at key j; bf16 holds these 2 j.)"""
+    n, tile, sl = 66000, 128, torch.full((2,), -4.0, device="cuda")
+    cu, blocks = [0, n], None
+    if kind == "blocksparse":  # the first tiles, in some q-tiles cut in three
+        lists = [list(range(min(t + 1, 3 if t % 2 else 40))) for t in range(-(-n // tile))]
+        blocks = (np.cumsum([0] + [len(x) for x in lists]).tolist(), sum(lists, []))
+    g = torch.Generator().manual_seed(23)
+    q = torch.zeros(n, 2, d, dtype=torch.bfloat16, device="cuda")
+    q[..., 0] = 16.0
+    k = torch.zeros(n, 1, d, dtype=torch.bfloat16, device="cuda")
+    v = torch.randn(n, 1, d, generator=g).bfloat16().cuda()
+    places = torch.tensor([0, 70, 140, 210, 350], device="cuda")
+    k[places, 0, 0] = 2.0 * places.to(torch.bfloat16)
+    S, W, L = 360, 256, 200
+    plan = B.Plan(kind, cu, S, W, L, tile, 2, d, 16 if kind == "blocksparse" else 0,
+                  blocks=blocks)
+    o, l = torch.empty(n, 2, d, device="cuda"), torch.empty(2, n, device="cuda")
+    plan.run(q, k, v, o, l, softmax_scale=0.125, slopes=sl)
+    rows = torch.cat([torch.arange(5000, n, 3001), torch.arange(n - 250, n, 7)]).cuda()
+    key = torch.arange(n, device="cuda")
+    keep = key <= rows[:, None]
+    if kind == "triangle":
+        keep &= (key < S) | (rows[:, None] - key < W) | (rows[:, None] >= n - L)
+    if kind == "blocksparse":
+        many = torch.where((rows // tile) % 2 == 1, 3, 40)
+        keep &= key // tile < many[:, None]
+    ref = attend(q[rows], k, v, keep, rows[:, None] - key, 0.125, None, sl)
+    check(o[rows], l.t()[rows], ref, torch.float32, f"far {kind} {d}")
+
+
+def test_scores_that_grow_within_a_window():
+    """Without a sink a streaming row's first key is its window's."""
+    n, W = 5000, 400
+    q = torch.zeros(n, 2, 64, dtype=torch.bfloat16, device="cuda")
+    k = torch.zeros(n, 1, 64, dtype=torch.bfloat16, device="cuda")
+    v = torch.randn(n, 1, 64, generator=torch.Generator().manual_seed(24)).bfloat16().cuda()
+    q[..., 0] = 16.0
+    row = 4700
+    keys = row - W + 1 + torch.tensor([0, 50, 100, 150, 350], device="cuda")
+    # 0.125 * 16 * k makes up for slope -512 from the window's start on
+    k[keys, 0, 0] = 256.0 * (keys - keys[0]).to(torch.bfloat16)
+    sl = torch.full((2,), -512.0, device="cuda")
+    plan = B.Plan("triangle", [0, n], 0, W, 0, 64, 2, 64)
+    o, l = torch.empty(n, 2, 64, device="cuda"), torch.empty(2, n, device="cuda")
+    plan.run(q, k, v, o, l, softmax_scale=0.125, slopes=sl)
+    at = torch.arange(n, device="cuda")
+    rows = torch.cat([torch.arange(100), torch.arange(row - 2, row + 3)]).cuda()
+    gap = rows[:, None] - at
+    ref = attend(q[rows], k, v, (gap >= 0) & (gap < W), gap, 0.125, None, sl)
+    # In the log2 domain products and biases are below 512 * 400 * 1.4427 < 2^19,
+    # half a step of which is 2^-6: the tile's bias, its difference to the
+    # reference and a key's own bias round by that each, the sum of product and
+    # bias is small.  A probability is off by a factor of e^(+-e) at most, an
+    # output by e^(2 e) - 1 beside the rounding of probabilities to bf16.
+    e = 3 * 2.0 ** -6 * math.log(2.0)
+    ro, rl, absw = ref
+    assert bool(((o[rows].double() - ro).abs() <= (2.0 ** -8 + math.expm1(2 * e)) * absw
+                 + 1e-5).all())
+    assert bool(((l.t()[rows].double() - rl).abs() <= e + 2.0 ** -22 * rl.abs()).all())
