@@ -93,9 +93,8 @@ __global__ __launch_bounds__(NW * 64, D == 64 ? 3 : 2) void scored_attn_kernel(S
     const int g = bid % a.hkv;
     bid /= a.hkv;
     const int sub = bid % a.subtiles;
-    // a causal schedule lists the short rows first: the long ones start first
-    const int item = a.kind == TA_KIND_CAUSAL ? a.n_items - 1 - bid / a.subtiles
-                                              : bid / a.subtiles;
+    // (causal and block-sparse schedules list the longest items first)
+    const int item = bid / a.subtiles;
     const int32_t *it = sched + kHdrWords + (int64_t)item * kItemWords;
     const int64_t seq_off = it[I_SEQ_OFF];
     const int32_t seq_len = it[I_SEQ_LEN];
@@ -672,10 +671,11 @@ extern "C" ta_status scored_attn_fwd(const void *q, const void *k, const void *v
     // bound, finer launches and row blocks that do not come in eights.  Eight
     // where they pay: d = 128, whole eights of row blocks, and more than two
     // workgroups to a CU.  us with eight and with four waves: capped causal at d =
-    // 128, 32 heads over 8, 700 tokens 29 and 22, 2500 tokens 99 and 94, 4000 tokens
-    // 183 and 186, 16384 tokens 2451 and 2550; slopes, window 1024, 4000 tokens 97 and
-    // 97, packed 42000 tokens, window 2048 1370 and 1457; 28 heads over 4, 8000 tokens
-    // 614 and 569; d = 64, 12000 tokens 1034 and 922.
+    // 128, 32 heads over 8, 700 tokens 28 and 21, 2500 tokens 79 and 74, 4000 tokens
+    // (512 workgroups of eight) 150 and 163, 5500 tokens 285 and 282, 16384 tokens
+    // 2205 and 2318; slopes, window 1024, 4000 tokens 94 and 94, packed 42000 tokens,
+    // window 2048 1397 and 1504; 28 heads over 4, 8000 tokens 541 and 507; d = 64,
+    // 12000 tokens 920 and 848.
     const int64_t blocks = group * (info->tile / 32);
     const bool eight = head_dim == 128 && blocks % 8 == 0 &&
                        info->n_items * (blocks / 8) * hkv > 512;

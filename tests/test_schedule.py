@@ -114,3 +114,12 @@ def test_schedule_llama_128k_matches_oracle():
     got, _, want = _both("triangle", w.cu_seqlens, w.sink, w.window, w.last,
                          w.tile)
     np.testing.assert_array_equal(got, want)
+
+
+def test_causal_items_are_listed_longest_first():
+    """The kernels start the items in the order of the schedule: no launch ends
+    with its longest rows."""
+    words, info = binding.ta_build_schedule("causal", [0, 300, 5000, 5001, 7000], 0, 1, 0, 128)
+    items = words[16:16 + 12 * info.n_items].reshape(-1, 12)
+    tiles = items[:, 5] - items[:, 4]
+    assert info.n_items == len(tiles) > 50 and (np.diff(tiles) <= 0).all()
