@@ -429,3 +429,42 @@ def test_scores_that_grow_over_far_distances(d, ql, prefix):
              prefix_pages=c.prefix_pages if prefix else None, prefix_len=prefix, lse=l,
              softmax_scale=0.125, slopes=sl)
     check(o, l.t(), c.reference(q, [ql], 0.125, None, sl), torch.float32, f"far {d} {ql} {prefix}")
+
+
+@pytest.mark.parametrize("form,d,ql,n,prefix", [
+    ("two waves", 128, [1], 33001, 0), ("four waves", 64, [100], 33001, 0),
+    ("prefix, two waves", 128, [1] * 20, 40, 33001),
+    ("prefix, four waves", 64, [1] * 40, 40, 33001)])
+@pytest.mark.parametrize("score", ["plain", "slopes"])
+@pytest.mark.parametrize("odd", [False, True])
+def test_every_form_past_the_held_ids(form, d, ql, n, prefix, score, odd):
+    """Shares of more pages than a workgroup holds ids for at a time, from the
+    first key on and (with slopes) from the last one on; with `odd` also the
+    pass that looks at masked values key by key.  Few pages under many ids."""
+    heads, batch = 128, len(ql)
+    c = Cache([16 * 90], heads, d, 16, seed=25, spare=0)
+    g = torch.Generator().manual_seed(26)
+    far = max(n, prefix)
+    ids = torch.randint(0, 88, (-(-far // 16),), generator=g).to(torch.int32)
+    ids[-1] = 88  # the last page is its own: 9 keys, then NaN
+    c.k[88, :, far % 16:] = math.nan
+    c.v[88, :, far % 16:] = math.nan
+    own = torch.randint(0, 88, (batch, -(-n // 16)), generator=g).to(torch.int32)
+    if prefix:
+        c.prefix, c.prefix_pages = prefix, ids.cuda()
+    else:
+        own = ids[None].repeat(batch, 1)
+    c.table, c.lens = own.cuda(), [n] * batch
+    c.kv_lens = torch.tensor(c.lens, dtype=torch.int32, device="cuda")
+    if odd:
+        c.v[88, :, (far - 2) % 16, 5] = math.inf
+    sl = None
+    if score == "slopes":  # flat, so that every segment weighs
+        sl = torch.linspace(-2e-4, 2e-4, heads, device="cuda")
+    q = _q(sum(ql), heads, d, 27)
+    o, l = _call(c, q, ql, torch.float32, None, sl, ragged=max(ql) > 1)
+    some = [0, 77, 127]
+    c.k, c.v = c.k[:, some], c.v[:, some]
+    check(o[:, some], l[:, some], c.reference(q[:, some], ql, d ** -0.5, None,
+                                              sl[some] if sl is not None else None),
+          torch.float32, f"{form} {score} {odd}")

@@ -375,3 +375,27 @@ def test_scores_that_grow_within_a_window():
     assert bool(((o[rows].double() - ro).abs() <= (2.0 ** -8 + math.expm1(2 * e)) * absw
                  + 1e-5).all())
     assert bool(((l.t()[rows].double() - rl).abs() <= e + 2.0 ** -22 * rl.abs()).all())
+
+
+@pytest.mark.parametrize("score", ["cap", "slopes"])
+def test_lists_longer_than_a_workgroup_holds(score):
+    """Items of more listed steps than a workgroup keeps in LDS."""
+    n, tile = 64 * 2200 + 17, 64
+    count = -(-n // tile)
+    full = {count - 1, count - 3}  # two q-tiles list all earlier tiles
+    lists = [list(range(t + 1)) if t in full else [t] for t in range(count)]
+    blocks = (np.cumsum([0] + [len(x) for x in lists]).tolist(), sum(lists, []))
+    cap = 20.0 if score == "cap" else None
+    sl = torch.tensor([1e-5, -1e-5], device="cuda") if score == "slopes" else None
+    cu = [0, n]
+    q, k, v, o, lse, plan = _run("blocksparse", cu, 2, 1, 64, tile, 0, 1, 0, cap, sl,
+                                 torch.float32, 4000, blocks=blocks)
+    assert plan.info.max_item_tiles > 2100
+    rows = torch.cat([torch.arange(n - 210, n, 9), torch.tensor([0, 63, 64, n - 1])]).cuda()
+    key = torch.arange(n, device="cuda")
+    dist = rows[:, None] - key
+    keep = dist >= 0
+    t = rows // tile
+    keep &= ((key // tile == t[:, None]) | (t == count - 1)[:, None] | (t == count - 3)[:, None])
+    ref = attend(q[rows], k, v, keep, dist, 0.125, cap, sl)
+    check(o[rows], lse.t()[rows], ref, torch.float32, f"long lists {score}")
