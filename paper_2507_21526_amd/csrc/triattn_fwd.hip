@@ -149,70 +149,6 @@ __device__ __forceinline__ bool header_ok(const int32_t *s, int64_t total,
            (s[H_KIND] == kind) & (t == total) & (s[H_ITEMS] == n_items);
 }
 
-// A schedule that does not match the launch (wrong header, malformed item)
-// leaves the workgroup without rows it can trust: every workgroup that finds
-// one fills its slice of O (and of LSE) with NaN instead, the slices of the
-// whole grid together covering every element, so that the caller sees the
-// failure in the output (Appendix A.1 initialises O before the loops; here
-// a rejected schedule leaves it NaN, not stale).  Vector stores only.
-__device__ __forceinline__ void poison_outputs(void *o, int o_f32, float *lse,
-                                            int64_t total_tokens, int32_t hq, int d,
-                                            int64_t block, int64_t n_blocks)
-{
-    const int64_t n_o = total_tokens * hq * d;
-    const int64_t n_l = lse ? total_tokens * hq : 0;
-    const int64_t co = (n_o + n_blocks - 1) / n_blocks;
-    const int64_t cl = (n_l + n_blocks - 1) / n_blocks;
-    const int64_t o0 = block * co, o1 = min(o0 + co, n_o);
-    const int64_t l0 = block * cl, l1 = min(l0 + cl, n_l);
-    for (int64_t i = o0 + threadIdx.x; i < o1; i += blockDim.x) {
-        if (o_f32)
-            reinterpret_cast<float *>(o)[i] = __builtin_nanf("");
-        else
-            reinterpret_cast<uint16_t *>(o)[i] = 0x7fc0;  // bf16 quiet NaN
-    }
-    for (int64_t i = l0 + threadIdx.x; i < l1; i += blockDim.x)
-        lse[i] = __builtin_nanf("");
-}
-
-// A rejected item's own rows (every head), as far as its words say where
-// they are (clamped into the buffers, one q-tile at most), filled with NaN,
-// and its split partial rows when it names some: no other workgroup writes
-// these rows (a split item's O rows are the merge's, which then reads the
-// NaN partials), so a malformed item is visible in O and LSE, which the
-// slice of poison_outputs alone does not ensure (later workgroups may
-// overwrite that slice).  Every index stays inside the buffers the host
-// checked, whatever the words hold.
-__device__ __forceinline__ void poison_item_rows(void *o, int o_f32, float *lse, float *part_o,
-                                                 float *part_lse, int64_t total_tokens,
-                                                 int32_t hq, int d, int64_t n_partial_rows,
-                                                 int tile, int64_t seq_off, int64_t r0,
-                                                 int64_t r1, int64_t part_base)
-{
-    const int64_t lo = min(max(seq_off + r0, (int64_t)0), total_tokens);
-    int64_t hi = min(max(seq_off + r1, lo), lo + tile);
-    if (hi == lo)
-        hi = lo + tile;  // an empty or reversed row range: the tile from lo
-    hi = min(hi, total_tokens);
-    const int64_t rows = hi - lo;
-    for (int64_t i = threadIdx.x; i < rows * hq * d; i += blockDim.x) {
-        if (o_f32)
-            reinterpret_cast<float *>(o)[lo * hq * d + i] = __builtin_nanf("");
-        else
-            reinterpret_cast<uint16_t *>(o)[lo * hq * d + i] = 0x7fc0;  // bf16 quiet NaN
-    }
-    if (lse)
-        for (int64_t i = threadIdx.x; i < rows * hq; i += blockDim.x)
-            lse[(i / rows) * total_tokens + lo + i % rows] = __builtin_nanf("");
-    if (part_o && part_base >= 0 && part_base < n_partial_rows) {
-        const int64_t prows = min(rows, n_partial_rows - part_base);
-        for (int64_t i = threadIdx.x; i < prows * hq * d; i += blockDim.x)
-            part_o[part_base * hq * d + i] = __builtin_nanf("");
-        for (int64_t i = threadIdx.x; i < prows * hq; i += blockDim.x)
-            part_lse[part_base * hq + i] = __builtin_nanf("");
-    }
-}
-
 // Key offset (within a 32-key block) held by register v of lane half h in
 // the S^T accumulator, given the permuted K row order.
 __device__ __forceinline__ int key_of_reg(int v, int h)

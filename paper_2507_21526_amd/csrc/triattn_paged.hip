@@ -249,7 +249,7 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
                 if (g == 0)
                     for (int i = slot * kThreads + tid; i < a.n_records; i += a.slots * kThreads)
                         a.records[i * kRecordWords + RF_ROWS] = 0;
-                rows_poison(a.o, a.o_f32, a.lse, (int64_t)a.total_tokens * a.hq, D);
+                poison_outputs(a.o, a.o_f32, a.lse, a.total_tokens, a.hq, D, blockIdx.x, gridDim.x);
                 return;
             }
         }

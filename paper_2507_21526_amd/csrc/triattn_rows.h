@@ -102,21 +102,6 @@ __device__ __forceinline__ void rows_wait_copies()
     asm volatile("" ::: "memory");
 }
 
-// Fills O (and LSE) of `rows` (token, head) rows with NaN, each workgroup its
-// share: what a call shows of device data that it cannot follow.
-__device__ __forceinline__ void rows_poison(void *o, int o_f32, float *lse, int64_t rows, int d)
-{
-    const int64_t n = (int64_t)gridDim.x * blockDim.x;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < rows * d; i += n) {
-        if (o_f32)
-            static_cast<float *>(o)[i] = __builtin_nanf("");
-        else
-            static_cast<uint16_t *>(o)[i] = 0x7fc0;  // bf16 quiet NaN
-        if (lse && i < rows)
-            lse[i] = __builtin_nanf("");
-    }
-}
-
 // Log-sum-exps of rows whose scores grow with the distance count it from the
 // first key: what the row's own distance from there, `past` keys, adds.
 __device__ __forceinline__ float rows_lse_shift(float slope, int past)

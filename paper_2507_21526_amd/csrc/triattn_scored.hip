@@ -115,21 +115,9 @@ __global__ __launch_bounds__(NW * 64, D == 64 ? 3 : 2) void scored_attn_kernel(S
         (list ? (ka1 < 0) | (kb1 != kb0) | ((int64_t)ka0 + ka1 > a.list_words) : ka1 < ka0) |
         (part_base >= 0 && (int64_t)part_base + (r1 - r0) > a.n_partial_rows);
     if (bad) {
-        rows_poison(a.o, a.o_f32, a.lse, a.total_tokens * a.hq, D);
-        // the item's own rows, as far as its words say where they are, are
-        // written by no other workgroup of this pass
-        const int64_t lo = min(max(seq_off + r0, (int64_t)0), a.total_tokens);
-        const int64_t hi = min(lo + a.tile, a.total_tokens);
-        for (int64_t i = lo * a.hq * D + threadIdx.x; i < hi * a.hq * D; i += kThreads) {
-            if (a.o_f32)
-                static_cast<float *>(a.o)[i] = __builtin_nanf("");
-            else
-                static_cast<uint16_t *>(a.o)[i] = 0x7fc0;
-        }
-        if (part_base >= 0 && part_base < a.n_partial_rows)
-            for (int64_t i = threadIdx.x;
-                 i < (int64_t)min(a.tile, a.n_partial_rows - part_base) * a.hq; i += kThreads)
-                a.part_lse[(int64_t)part_base * a.hq + i] = __builtin_nanf("");
+        poison_outputs(a.o, a.o_f32, a.lse, a.total_tokens, a.hq, D, blockIdx.x, gridDim.x);
+        poison_item_rows(a.o, a.o_f32, a.lse, a.part_o, a.part_lse, a.total_tokens, a.hq, D,
+                         a.n_partial_rows, a.tile, seq_off, r0, r1, part_base);
         return;
     }
     const int max_ktile = (seq_len - 1) / a.tile;
@@ -529,7 +517,9 @@ __global__ __launch_bounds__(kJoinThreads) void scored_join_kernel(ScoredArgs a)
         (rows > a.tile) | (ns < 1) | (pb < 0) |
         ((int64_t)pb + (int64_t)ns * rows > a.n_partial_rows) | (seq_off < 0) | (r0 < 0) |
         (seq_off + r1 > a.total_tokens)) {
-        rows_poison(a.o, a.o_f32, a.lse, a.total_tokens * a.hq, D);
+        poison_outputs(a.o, a.o_f32, a.lse, a.total_tokens, a.hq, D, blockIdx.x, gridDim.x);
+        poison_item_rows(a.o, a.o_f32, a.lse, nullptr, nullptr, a.total_tokens, a.hq, D, 0, a.tile,
+                         seq_off, r0, r1, -1);
         return;
     }
     const int lane = threadIdx.x & 63;

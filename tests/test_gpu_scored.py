@@ -399,3 +399,42 @@ def test_lists_longer_than_a_workgroup_holds(score):
     keep &= ((key // tile == t[:, None]) | (t == count - 1)[:, None] | (t == count - 3)[:, None])
     ref = attend(q[rows], k, v, keep, dist, 0.125, cap, sl)
     check(o[rows], lse.t()[rows], ref, torch.float32, f"long lists {score}")
+
+
+@pytest.mark.parametrize("kind", ["triangle", "causal", "blocksparse"])
+@pytest.mark.parametrize("word,value", [(8, 9), (4, -1), (5, -1)])  # mode, first and last k-tile
+def test_an_item_that_does_not_fit_shows_in_its_rows(kind, word, value):
+    """One item's words out of range: the rows that it names are NaN, in the
+    row normaliser too."""
+    cu = [0, 70, 600, 1100]
+    blocks, _ = _lists(cu, 64, 3)
+    q, k, v = (t.cuda() for t in draw_qkv(cu, 4, 1, 64, 2))
+    plan = B.Plan(kind, cu, 8, 100, 70, 64, 4, 64, 2, blocks=blocks)
+    words = plan.sched.tolist()
+    for item in (0, plan.info.n_items // 2, plan.info.n_items - 1):
+        at = 16 + 12 * item
+        lo, hi = words[at] + words[at + 2], words[at] + words[at + 3]
+        plan.sched[at + word] = value
+        o = torch.zeros(q.shape, device="cuda")
+        lse = torch.zeros(4, cu[-1], device="cuda")
+        plan.run(q, k, v, o, lse, softcap=5.0)
+        assert bool(torch.isnan(o[lo:hi]).all()), item
+        assert bool(torch.isnan(lse[:, lo:hi]).all()), item
+        plan.sched[at + word] = words[at + word]
+
+
+@pytest.mark.parametrize("word,value", [(1, -5), (3, 10 ** 6), (4, -1)])  # r0, splits, partials
+def test_a_merge_item_that_does_not_fit_shows_in_its_rows(word, value):
+    cu = [0, 70, 600, 1100]
+    q, k, v = (t.cuda() for t in draw_qkv(cu, 4, 1, 64, 2))
+    plan = B.Plan("triangle", cu, 8, 100, 70, 64, 4, 64, 2)
+    words = plan.sched.tolist()
+    at = 16 + 12 * plan.info.n_items + 8 * (plan.info.n_merge_items - 1)
+    lo, hi = words[at] + words[at + 1], words[at] + words[at + 2]
+    plan.sched[at + word] = value
+    o = torch.zeros(q.shape, device="cuda")
+    lse = torch.zeros(4, cu[-1], device="cuda")
+    plan.run(q, k, v, o, lse, softcap=5.0)
+    if word != 1:  # (a row that is none names no rows)
+        assert bool(torch.isnan(o[lo:hi]).all()) and bool(torch.isnan(lse[:, lo:hi]).all())
+    assert bool(torch.isnan(o).any()) and bool(torch.isnan(lse).any())
