@@ -302,9 +302,16 @@ ta_status blocksparse_attn_fwd(const void *q, const void *k, const void *v,
  *                layouts and the workspace (ta_workspace_bytes) are those of
  *                that kind's forward function.
  *   softcap      0 (none) to 1024; a score's absolute error is at most
- *                2^-22 softcap beside that of the product.
+ *                2^-20 softcap beside that of the product.
  *   slopes       [hq] fp32 device array of finite values, or NULL.  The last
- *                keys weigh most where a slope is positive.
+ *                keys weigh most where a slope is positive, the first where it
+ *                is negative.  A bias's absolute error is at most
+ *                2^-21 |slope| times the key's distance from the row, or, where
+ *                the slope is negative, from the sequence's first key (the
+ *                window's, of rows that keep a window alone).
+ * As in the other passes scores, sums and accumulators are fp32 and each
+ * probability is rounded to bf16 for the product with v, whatever o_dtype: an
+ * output is off by at most 2^-8 of the probability-weighted mean of |v| for it.
  * A key that a row does not keep adds nothing to it, whatever its value
  * (infinities and NaN included).  Errors as triangle_attn_fwd.
  */
@@ -395,9 +402,9 @@ ta_status kv_cache_write(const void *k, const void *v, int64_t k_token_stride,
  *                which come before every request's own ones; any length.
  * Row t of request b has position p = kv_lens[b] - (cu_q[b + 1] - cu_q[b]) + t
  * among its own keys and keeps the whole prefix and the own keys up to p; a
- * row whose p is negative keeps nothing (o = 0, lse = -inf).  Scores, softcap
- * and slopes as for scored_attn_fwd, both optional here, positions counted
- * from the start of the prefix.  Values behind a row's last key, in the pages
+ * row whose p is negative keeps nothing (o = 0, lse = -inf).  Scores, softcap,
+ * slopes and roundings as for scored_attn_fwd, both optional here, positions
+ * counted from the start of the prefix.  Values behind a row's last key, in the pages
  * or past them, are never used, whatever they are.
  *   workspace    at least ta_paged_workspace_bytes() bytes, 16-byte aligned,
  *                ragged = cu_q is given, prefix = prefix_len > 0; its contents

@@ -9,8 +9,9 @@
 // reference m (one pass).  Scores are carried in the log2 domain, so that the
 // exponentials are single exp2 instructions:
 //   cap tanh(x / cap) = cap (1 - 2 / (1 + e^(2 x / cap))),
-// one exp2, one reciprocal and three plain operations; its absolute error is
-// a few 2^-24 of the cap, as for a score of the cap's size in fp32.
+// one exp2, one reciprocal and three plain operations.  Its absolute error is at
+// most 10 2^-24 of the cap, term by term (exponent 1.5, exp2 1, sum 2, reciprocal
+// 2, the cap's factor 1.2, difference to the reference 2); 5.4 were measured.
 //
 // Layout, as in the forward tile kernel: S^T = K Q^T by bf16 MFMA 32x32x16
 // (keys on the rows, queries on the columns), so that a lane holds scores of
@@ -119,7 +120,7 @@ inline bool rows_score_args(ScoreArgs &a, float softmax_scale, float softcap, co
     return a.cap_in <= 3.0e38f;
 }
 
-// Largest cap: an error of 2^-22 of it is 2.4e-4 then.
+// Largest cap: an error of 10 2^-24 of it is 6.1e-4 then.
 constexpr float kRowsMaxCap = 1024.f;
 
 // One wave's 32 rows.  NKB: 32-key blocks of a tile.

@@ -438,3 +438,30 @@ def test_a_merge_item_that_does_not_fit_shows_in_its_rows(word, value):
     if word != 1:  # (a row that is none names no rows)
         assert bool(torch.isnan(o[lo:hi]).all()) and bool(torch.isnan(lse[:, lo:hi]).all())
     assert bool(torch.isnan(o).any()) and bool(torch.isnan(lse).any())
+
+
+@pytest.mark.parametrize("cap", [0.5, 30.0, 1024.0])
+def test_error_of_a_cap(cap):
+    """Rows of one key each, whose log-sum-exp is the capped score: products
+    from far below to far past the cap, both signs.  With u = 2^-24, relative
+    to the cap and in the order of the arithmetic: 1.5 u from the exponent's
+    factor (3.3 u of it, times t (1 - tanh^2 t) <= 0.448), 1 u and 2 u from the
+    exponential (an ulp of it) and its sum with one, 2 u from the reciprocal (an
+    ulp), 1.2 u from the cap's factor, 2 u from the difference to a reference:
+    9.7 u; the log-sum-exp adds 2.3 u of itself (two products, a constant)."""
+    n, hq, d = 4000, 8, 64
+    g = torch.Generator().manual_seed(28)
+    q = torch.zeros(n, hq, d, dtype=torch.bfloat16)
+    k = torch.zeros(n, 1, d, dtype=torch.bfloat16)
+    size = torch.exp2(12.0 * torch.rand(n, generator=g) - 8.0) * cap  # |x|: cap 2^-8 .. 2^4
+    k[:, 0, 0] = (8.0 * size * torch.sign(torch.randn(n, generator=g))).bfloat16()
+    q[:, :, 0] = (1.0 + torch.rand(n, hq, generator=g)).bfloat16()
+    q, k = q.cuda(), k.cuda()
+    v = torch.zeros_like(k)
+    plan = B.Plan("causal", list(range(n + 1)), 0, 1, 0, 64, hq, d)
+    o, lse = torch.empty(n, hq, d, device="cuda"), torch.empty(hq, n, device="cuda")
+    plan.run(q, k, v, o, lse, softmax_scale=0.125, softcap=cap)
+    x = 0.125 * q[:, :, 0].double() * k[:, :, 0].double()  # [n, hq]
+    err = (lse.t().double() - cap * torch.tanh(x / cap)).abs().max().item() / cap
+    print(f"cap {cap}: {err * 2 ** 24:.2f} 2^-24")
+    assert err <= 2.0 ** -20
