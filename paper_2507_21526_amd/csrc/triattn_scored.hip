@@ -498,12 +498,10 @@ __global__ __launch_bounds__(NW * 64, D == 64 ? 3 : 2) void scored_attn_kernel(S
 // Joins the partials of the schedule's split q-tiles, a wave to a (row, head):
 // O = sum_c w_c O_c / sum_c w_c with w_c = exp(LSE_c - max_c LSE_c).
 template <int D>
-__global__ __launch_bounds__(kJoinThreads) void scored_join_kernel(ScoredArgs a)
+__device__ __forceinline__ void join_item(const ScoredArgs &a, int m)
 {
     constexpr int PER = D / 64, kWaves = kJoinThreads / 64;
     const int32_t *sched = a.sched;
-    const int blocks = (a.tile * a.hq + kWaves - 1) / kWaves;  // workgroups of a merge item
-    const int m = blockIdx.x / blocks;
     const int32_t *x = sched + kHdrWords + (int64_t)a.n_items * kItemWords +
                        (int64_t)m * kMergeWords;
     const int64_t seq_off = x[M_SEQ_OFF];
@@ -517,13 +515,15 @@ __global__ __launch_bounds__(kJoinThreads) void scored_join_kernel(ScoredArgs a)
         (rows > a.tile) | (ns < 1) | (pb < 0) |
         ((int64_t)pb + (int64_t)ns * rows > a.n_partial_rows) | (seq_off < 0) | (r0 < 0) |
         (seq_off + r1 > a.total_tokens)) {
-        poison_outputs(a.o, a.o_f32, a.lse, a.total_tokens, a.hq, D, blockIdx.x, gridDim.x);
+        poison_outputs(a.o, a.o_f32, a.lse, a.total_tokens, a.hq, D,
+                       (int64_t)blockIdx.y * gridDim.x + blockIdx.x,
+                       (int64_t)gridDim.x * gridDim.y);
         poison_item_rows(a.o, a.o_f32, a.lse, nullptr, nullptr, a.total_tokens, a.hq, D, 0, a.tile,
                          seq_off, r0, r1, -1);
         return;
     }
     const int lane = threadIdx.x & 63;
-    const int w = (int)(blockIdx.x % blocks) * kWaves + (threadIdx.x >> 6);
+    const int w = (int)blockIdx.x * kWaves + (threadIdx.x >> 6);
     const int head = w % a.hq, r = w / a.hq;
     if (r >= rows)
         return;
@@ -574,6 +574,15 @@ __global__ __launch_bounds__(kJoinThreads) void scored_join_kernel(ScoredArgs a)
             den == 0.f ? -INFINITY
                        : m_use + __logf(den) +
                              (a.score.slopes ? rows_lse_shift(a.score.slopes[head], r0 + r) : 0.f);
+}
+
+// Grid: x covers the tile * hq (row, head) waves of a merge item, y the merge
+// items, in turn where there are more than it holds.
+template <int D>
+__global__ __launch_bounds__(kJoinThreads) void scored_join_kernel(ScoredArgs a)
+{
+    for (int m = blockIdx.y; m < a.n_merges; m += gridDim.y)
+        join_item<D>(a, m);
 }
 
 template <int D, bool LIST, int NW>
@@ -672,9 +681,7 @@ extern "C" ta_status scored_attn_fwd(const void *q, const void *k, const void *v
     const int nw = eight ? 8 : 4;
     const int64_t subtiles = (blocks + nw - 1) / nw;
     const int64_t wgs = info->n_items * subtiles * hkv;
-    const int64_t join_wgs =
-        info->n_merge_items * (((int64_t)info->tile * hq + 3) / 4);
-    if (wgs > INT32_MAX || join_wgs > INT32_MAX)
+    if (wgs * nw * 64 > UINT32_MAX)  // threads of a launch
         return fail(TA_ERR_UNSUPPORTED, "%s: grid too large", fn);
     if (info->n_items == 0)
         return TA_OK;
@@ -727,13 +734,13 @@ extern "C" ta_status scored_attn_fwd(const void *q, const void *k, const void *v
     else
         launch_scored<64, 4>(list, score, grid, s, a);
     hipError_t err = hipGetLastError();
-    if (err == hipSuccess && join_wgs > 0) {
+    if (err == hipSuccess && a.n_merges > 0) {
+        const dim3 join((uint32_t)((info->tile * hq + 3) / 4),
+                        (uint32_t)std::min(a.n_merges, 65535));
         if (head_dim == 128)
-            hipLaunchKernelGGL(scored_join_kernel<128>, dim3((uint32_t)join_wgs),
-                               dim3(kJoinThreads), 0, s, a);
+            hipLaunchKernelGGL(scored_join_kernel<128>, join, dim3(kJoinThreads), 0, s, a);
         else
-            hipLaunchKernelGGL(scored_join_kernel<64>, dim3((uint32_t)join_wgs),
-                               dim3(kJoinThreads), 0, s, a);
+            hipLaunchKernelGGL(scored_join_kernel<64>, join, dim3(kJoinThreads), 0, s, a);
         err = hipGetLastError();
     }
     if (err != hipSuccess)

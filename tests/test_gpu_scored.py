@@ -465,3 +465,25 @@ def test_error_of_a_cap(cap):
     err = (lse.t().double() - cap * torch.tanh(x / cap)).abs().max().item() / cap
     print(f"cap {cap}: {err * 2 ** 24:.2f} 2^-24")
     assert err <= 2.0 ** -20
+
+
+def test_many_short_sequences_with_last_rows():
+    """More q-tiles to join than a launch has rows of workgroups: 70000 packed
+    sequences of one to three tokens, all of them Last rows."""
+    lens = [1 + i % 3 for i in range(70000)]
+    cu = [0]
+    for n in lens:
+        cu.append(cu[-1] + n)
+    g = torch.Generator().manual_seed(29)
+    q = torch.randn(cu[-1], 32, 64, generator=g).bfloat16().cuda()
+    k = torch.randn(cu[-1], 8, 64, generator=g).bfloat16().cuda()
+    v = torch.randn(cu[-1], 8, 64, generator=g).bfloat16().cuda()
+    args = (32, 8, 64, 128, 8, 64, 128, 20.0, None, torch.float32)
+    o, lse = _run("triangle", cu, *args, qkv=(q, k, v))[3:5]
+    assert bool(torch.isfinite(o).all()) and bool(torch.isfinite(lse).all())
+    for a, b in ((0, 40), (33000, 33040), (65530, 65545), (69950, 70000)):
+        t0, t1 = cu[a], cu[b]
+        part = [x - t0 for x in cu[a:b + 1]]
+        out = _run("triangle", part, *args, qkv=(q[t0:t1], k[t0:t1], v[t0:t1]))
+        assert torch.equal(out[3], o[t0:t1]) and torch.equal(out[4], lse[:, t0:t1])
+        _verify("triangle", part, *out[:5], 128, 8, 64, 128, 20.0, None, f"sequences {a}..{b}")
