@@ -332,11 +332,15 @@ extern "C" ta_status kv_cache_write(const void *k, const void *v, int64_t k_toke
     a.n_slots = num_pages << lp;
     a.hkv = hkv;
     a.page_log2 = lp;
-    a.rows = 256 / (head_dim / 8);
-    const int64_t rows = total_tokens * hkv;
+    // one row a thread group, more where a launch (2^32 threads at most) does
+    // not hold that many
+    constexpr int64_t kMaxWgs = 1 << 22;
+    const int64_t rows = total_tokens * hkv, turn = 256 / (head_dim / 8);
+    const int64_t turns = std::max<int64_t>(1, (rows + turn * kMaxWgs - 1) / (turn * kMaxWgs));
+    if (turns * turn > INT32_MAX)
+        return fail(TA_ERR_UNSUPPORTED, "%s: too many rows", fn);
+    a.rows = (uint32_t)(turns * turn);
     const int64_t wgs = (rows + a.rows - 1) / a.rows;
-    if (wgs > INT32_MAX)
-        return fail(TA_ERR_UNSUPPORTED, "%s: grid too large", fn);
     if (head_dim == 128)
         hipLaunchKernelGGL(cache_write_kernel<128>, dim3((uint32_t)wgs), dim3(256), 0,
                            static_cast<hipStream_t>(stream), a);

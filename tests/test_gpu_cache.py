@@ -209,3 +209,20 @@ def test_a_serving_run(score):
         ref = attend(seqs[i][0][:n], seqs[i][1][:n], seqs[i][2][:n], dist >= 0, dist, d ** -0.5,
                      cap, sl)
         check(o[cu[i]:cu[i + 1]], None, ref, torch.bfloat16, f"prompt {i}")
+
+
+def test_cache_write_of_more_rows_than_threads():
+    """2^28 rows and more, 2^32 chunks: one row's views repeated (strides of
+    zero), a few of them with a slot."""
+    n, hkv, d = (1 << 25) + 5, 8, 128
+    k = torch.randn(1, hkv, d, device="cuda").bfloat16()
+    v = torch.randn(1, hkv, d, device="cuda").bfloat16()
+    kc = torch.zeros(2, hkv, 16, d, dtype=torch.bfloat16, device="cuda")
+    vc = torch.zeros_like(kc)
+    slots = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    at = torch.tensor([0, 1, 1 << 24, n - 6, n - 1], device="cuda")
+    slots[at] = torch.arange(3, 8, dtype=torch.int32, device="cuda")
+    B.kv_cache_write(k.expand(n, hkv, d), v.expand(n, hkv, d), slots, kc, vc)
+    assert torch.equal(kc[0, :, 3:8], k[0][:, None].expand(hkv, 5, d))
+    assert torch.equal(vc[0, :, 3:8], v[0][:, None].expand(hkv, 5, d))
+    assert not bool(kc[0, :, :3].any()) and not bool(kc[0, :, 8:].any()) and not bool(kc[1].any())
