@@ -1048,6 +1048,14 @@ extern "C" ta_status paged_attn_fwd(const void *q, const void *k_cache, const vo
     const int64_t pre_tiles = (total_tokens * group + 32 * p.pre_rb - 1) / (32 * p.pre_rb);
     if (steps > INT32_MAX / 2 || pre_tiles * (prefix_len / 64 + 1) > INT32_MAX / 2)
         return fail(TA_ERR_UNSUPPORTED, "%s: too many steps", fn);
+    // the join: workgroups of a row tile, rows of each
+    const int join_rows = cu_q ? 32 * p.own_rb : (int)group;
+    const int chunk_rows = std::min(join_rows, kJoinThreads / 16);
+    const int chunks = (join_rows + chunk_rows - 1) / chunk_rows;
+    const int64_t wgs = std::max<int64_t>({p.own_slots, prefix_len > 0 ? p.pre_slots : 0,
+                                           (int64_t)p.n_records * chunks}) * hkv;
+    if (wgs * kJoinThreads > UINT32_MAX)  // threads of a launch
+        return fail(TA_ERR_UNSUPPORTED, "%s: grid too large", fn);
     if (total_tokens == 0 || batch == 0)
         return TA_OK;
     if (!q || !o || !kv_lens || (num_pages > 0 && (!k_cache || !v_cache)) ||
@@ -1134,9 +1142,8 @@ extern "C" ta_status paged_attn_fwd(const void *q, const void *k_cache, const vo
         j.slot_o = a.slot_o;
         j.slot_lse = a.slot_lse;
         j.tile_rows = 32 * p.own_rb;
-        const int rows = cu_q ? j.tile_rows : (int)group;
-        j.chunk_rows = std::min(rows, kJoinThreads / 16);
-        j.chunks = (rows + j.chunk_rows - 1) / j.chunk_rows;
+        j.chunk_rows = chunk_rows;
+        j.chunks = chunks;
         j.row_o = a.row_o;
         j.row_lse = a.row_lse;
         j.pre_slot_o = part(p.pre_slot_o);
@@ -1157,7 +1164,7 @@ extern "C" ta_status paged_attn_fwd(const void *q, const void *k_cache, const vo
         j.hkv = hkv;
         j.group = (int32_t)group;
         j.o_f32 = a.o_f32;
-        const dim3 grid((uint32_t)(p.n_records * j.chunks * hkv));
+        const dim3 grid((uint32_t)(p.n_records * chunks * hkv));
         if (head_dim == 128)
             hipLaunchKernelGGL(paged_join_kernel<128>, grid, dim3(kJoinThreads), 0, s, j);
         else

@@ -217,3 +217,15 @@ def test_paged_distances_stay_in_32_bits():
     assert call(FAKE + 5 * M, rest + 1) == B.TA_ERR_UNSUPPORTED
     assert call(FAKE + 5 * M, rest) == B.TA_ERR_INVALID_ARG  # q is NULL
     assert call(0, rest + 1) == B.TA_ERR_INVALID_ARG
+
+
+def test_paged_launches_stay_in_32_bits():
+    """More kv heads than a launch's threads hold: refused before any work."""
+    kw = dict(q=0, d=64, page=16, width=1)
+    assert _paged(hq=1 << 24, hkv=1 << 24, total=1, batch=1, **kw) == B.TA_ERR_UNSUPPORTED
+    assert "grid" in B.ta_last_error()
+    # the join of 1257 row tiles behind a prefix
+    kw.update(prefix=FAKE + 7 * M, prefix_len=5, batch=1000, total=33000)
+    assert _paged(hq=4096, hkv=4096, **kw) == B.TA_ERR_UNSUPPORTED
+    assert "grid" in B.ta_last_error()
+    assert _paged(hq=1024, hkv=1024, **kw) == B.TA_ERR_INVALID_ARG  # q is NULL
