@@ -66,8 +66,11 @@ struct PagedArgs {
 //   RB = 1: up to 32 rows, bound by the bytes of K and V.  Two waves take 32-key
 //     tiles in turn, each into two stages of its own, and keep their own softmax:
 //     nothing waits on the other wave until they are joined at the end of a
-//     piece.  64 KB of stages at d = 128 let two workgroups share a CU, so that one
-//     loads while the other finds its next request or joins its waves.
+//     piece.  64 KB of stages at d = 128 (32 KB at d = 64) let two workgroups
+//     (four) share a CU, so that one loads while the other finds its next request
+//     or joins its waves.  The tables of lengths come on top, 16 to 20 bytes a
+//     request with query offsets and 8 without: fewer share a CU from some 700
+//     requests with offsets on at d = 128, from 280 (700 without) at d = 64.
 //   RB = 4: four waves of 32 rows each over the same 64-key tiles, in two stages.
 template <int D, int RB>
 struct PagedShape {
@@ -80,8 +83,11 @@ struct PagedShape {
     static constexpr int TILE_BYTES = TK * 2 * D;
     static constexpr int STAGE_BYTES = 2 * TILE_BYTES;  // K tile, then V tile
     static constexpr int LDS_BYTES = KS * 2 * STAGE_BYTES;
-    // least steps of a share: one of a 128-row tile leaves partials of twice
-    // its K and V tiles' bytes
+    // Least steps of a share: one of a 128-row tile leaves partials of twice
+    // its K and V tiles' bytes.  us with 1, 4 and 8 steps (32 heads over 8, d =
+    // 128): the last 64 tokens of 2000 27, 25, 29, of four times 1000 29, 25, 28,
+    // 128 single tokens behind a prefix of 2048 47, 43, 44, the last 100 tokens of
+    // 500 17, 24, 29; from 3000 keys on the same.
     static constexpr int LEAST = RB == 4 ? 4 : 1;
     static constexpr int WGS_PER_CU = RB == 1 && D == 64 ? 4 : 2;
     static constexpr int WAVES_PER_SIMD = (WGS_PER_CU * THREADS / 64 + 3) / 4;
@@ -905,8 +911,14 @@ PagedLayout paged_layout(int32_t batch, int64_t total_tokens, bool ragged, bool 
 {
     PagedLayout p{};
     const int64_t group = hq / hkv;
-    // Up to 32 rows a request on average: tiles of 32 rows, which a step's
-    // four waves share out by keys.
+    // Up to 32 rows a request on average: tiles of 32 rows, which a
+    // workgroup's two waves share out by keys; 128 otherwise.  us with 32 and with
+    // 128 (32 heads over 8, d = 128, 4000 keys a request): 64 requests of one
+    // token 183 and 193, 24 of eight (32 rows) 93 and 96, of nine 133 and 97, of 32
+    // 232 and 113.  One form serves the whole call, also where requests differ:
+    // 64 single tokens and one piece of 400 (behind 8000 keys) 279 (as chosen) and
+    // 242, one of 700 349 and 281 (as chosen; 184 and 113 in calls of their own);
+    // 255 single tokens and one piece of 1024 915 (as chosen) and 823.
     p.own_rb = !ragged || total_tokens * group <= (int64_t)batch * 32 ? 1 : 4;
     p.pre_rb = total_tokens * group <= 32 ? 1 : 4;
     p.own_slots = std::max(1, kCus * wgs_per_cu(p.own_rb, d) / hkv);

@@ -5,12 +5,14 @@
 // A workgroup of four or eight waves takes as many row blocks (32 rows of one
 // head) of a schedule item, dealt out head first, over K/V tiles of 64 keys in
 // LDS.  What bounds it: the two products take a wave 32 matrix instructions of 32
-// cycles a step.  A capped score takes two exp2 and a reciprocal, quarter-rate
-// instructions, and five plain ones: some 2200 cycles of the vector unit a step,
-// more than the matrix cores' 1024.  The 16384-token causal layer (32 heads over 8,
-// d = 128) runs at 2230 cycles a wave and step, 2.44 ms, 902 TFLOP/s.  Slopes add
-// one operation to a plain score: packed 42000 tokens at window 2048 in 1.37 ms,
-// 1072 TFLOP/s, matrix cores 55 % busy.
+// cycles a step.  A capped score takes two exp2, a reciprocal and five plain
+// instructions: 1535 cycles of the vector unit a step by its counter, more than the
+// matrix cores' 1024.  The 16384-token causal layer (32 heads over 8, d = 128) runs
+// at 2050 cycles a wave and step, 2.20 ms, 998 TFLOP/s, vector units 75 % and matrix
+// cores 50 % busy.  Slopes add one operation to a plain score: packed 42000 tokens
+// at window 2048 in 1.39 ms, 1056 TFLOP/s, matrix cores 56 % and vector units 54 %
+// busy.  A slope below zero makes every step outgrow the softmax reference, and
+// rescale: 16384 tokens 2.71 ms, and 1.71 with slopes above zero.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
