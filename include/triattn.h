@@ -386,6 +386,63 @@ ta_status kv_cache_write(const void *k, const void *v, int64_t k_token_stride,
                          int32_t head_dim, void *stream);
 
 /*
+ * The 8-bit form of the cache.  A row, one kv head of one token, is held as
+ * head_dim e4m3 elements, one byte each (four significant bits, magnitudes up
+ * to 448, NaN, no infinities), and a scale 2^(s - 127), one byte s (255: NaN):
+ * its values are element times scale.
+ *   k_cache, v_cache  [num_pages, hkv, page_size, head_dim] e4m3, 16-byte
+ *                aligned; k_scale, v_scale [num_pages, hkv, page_size] bytes,
+ *                4-byte aligned.
+ * kv_cache_write_q8 quantises rows as it writes them; other arguments as
+ * kv_cache_write.  A row's scale is the least power of two, 2^-100 at least,
+ * for which no finite value of the row passes 448 times it; values are rounded
+ * to the nearest element, ties to the even one.  Infinite and NaN values become
+ * NaN and set no scale.  (Under a scale of 2^120, which rows of values past
+ * 1.75 * 2^127 get, elements stop at 240: 256 would come back infinite.)
+ */
+ta_status kv_cache_write_q8(const void *k, const void *v, int64_t k_token_stride,
+                            int64_t k_head_stride, int64_t v_token_stride,
+                            int64_t v_head_stride, const int32_t *slots,
+                            int64_t total_tokens, void *k_cache, void *k_scale,
+                            void *v_cache, void *v_scale, int64_t num_pages,
+                            int32_t hkv, int32_t page_size, int32_t head_dim,
+                            void *stream);
+
+/*
+ * Cached rows back as bf16, from a cache of either form: rows cu[b] .. cu[b + 1)
+ * of k and v get positions starts[b], starts[b] + 1, .. of request b.  8-bit
+ * rows come back exactly (values past bf16's range as infinities).
+ *   block_table  [batch, table_width] int32 device array.
+ *   cu           [batch + 1] int32 device array; rows from cu[batch] on are
+ *                left as they are.
+ *   starts       [batch] int32 device array, or NULL: 0.
+ *   k, v         out: bf16 [total_tokens, hkv, head_dim] with the given
+ *                strides in elements (multiples of 8; the last dimension
+ *                contiguous), 16-byte aligned.  No row may lie on another; the
+ *                two may alternate in one buffer.
+ * Rows whose position no page of the cache holds (a negative position, one past
+ * the block table, a page id outside the cache) are NaN, and so is every row
+ * where cu does not start at 0, decreases or passes total_tokens.
+ */
+ta_status kv_cache_read(const void *k_cache, const void *v_cache,
+                        const int32_t *block_table, int32_t batch,
+                        int32_t table_width, const int32_t *cu,
+                        const int32_t *starts, void *k, void *v,
+                        int64_t k_token_stride, int64_t k_head_stride,
+                        int64_t v_token_stride, int64_t v_head_stride,
+                        int64_t total_tokens, int64_t num_pages, int32_t hkv,
+                        int32_t page_size, int32_t head_dim, void *stream);
+ta_status kv_cache_read_q8(const void *k_cache, const void *k_scale,
+                           const void *v_cache, const void *v_scale,
+                           const int32_t *block_table, int32_t batch,
+                           int32_t table_width, const int32_t *cu,
+                           const int32_t *starts, void *k, void *v,
+                           int64_t k_token_stride, int64_t k_head_stride,
+                           int64_t v_token_stride, int64_t v_head_stride,
+                           int64_t total_tokens, int64_t num_pages, int32_t hkv,
+                           int32_t page_size, int32_t head_dim, void *stream);
+
+/*
  * Attention over the paged cache: single tokens, drafted tokens, or pieces of
  * prompts, optionally behind a prefix that the whole batch shares.
  *   q, o, lse    as for the forward passes: [total_tokens, hq, head_dim], the
@@ -436,6 +493,29 @@ ta_status paged_attn_fwd(const void *q, const void *k_cache,
                          float softmax_scale, float softcap,
                          const float *slopes, void *workspace,
                          size_t workspace_bytes, void *stream);
+
+/*
+ * The same over an 8-bit cache (kv_cache_write_q8): each held value takes part
+ * as what it stands for, element times scale, and everything else is as for
+ * paged_attn_fwd, the workspace apart: at least ta_paged_q8_workspace_bytes()
+ * bytes.  Probabilities are rounded to bf16 there too; the sums of a softmax
+ * take them before.
+ */
+size_t ta_paged_q8_workspace_bytes(int32_t batch, int64_t total_tokens,
+                                   int32_t ragged, int32_t prefix, int32_t hq,
+                                   int32_t hkv, int32_t head_dim);
+ta_status paged_attn_fwd_q8(const void *q, const void *k_cache,
+                            const void *k_scale, const void *v_cache,
+                            const void *v_scale, void *o, int32_t o_dtype,
+                            float *lse, const int32_t *kv_lens,
+                            const int32_t *cu_q, const int32_t *block_table,
+                            int32_t batch, int32_t table_width,
+                            const int32_t *prefix_pages, int32_t prefix_len,
+                            int64_t total_tokens, int32_t hq, int32_t hkv,
+                            int32_t head_dim, int64_t num_pages,
+                            int32_t page_size, float softmax_scale,
+                            float softcap, const float *slopes, void *workspace,
+                            size_t workspace_bytes, void *stream);
 
 /*
  * Region-contribution probe (Sec. 2.2, Grad(M-hat, l); the sections of

@@ -130,12 +130,24 @@ def lib():
     L.kv_cache_write.restype = ctypes.c_int
     L.kv_cache_write.argtypes = [vp, vp, i64, i64, i64, i64, vp, i64, vp, vp, i64, i32, i32, i32,
                                  vp]
+    L.kv_cache_write_q8.restype = ctypes.c_int
+    L.kv_cache_write_q8.argtypes = [vp, vp, i64, i64, i64, i64, vp, i64, vp, vp, vp, vp, i64, i32,
+                                    i32, i32, vp]
+    L.kv_cache_read.restype = ctypes.c_int
+    L.kv_cache_read.argtypes = [vp, vp, vp, i32, i32, vp, vp, vp, vp, i64, i64, i64, i64, i64, i64,
+                                i32, i32, i32, vp]
+    L.kv_cache_read_q8.restype = ctypes.c_int
+    L.kv_cache_read_q8.argtypes = [vp, vp] + list(L.kv_cache_read.argtypes)
     L.ta_paged_workspace_bytes.restype = ctypes.c_size_t
     L.ta_paged_workspace_bytes.argtypes = [i32, i64, i32, i32, i32, i32, i32]
     L.paged_attn_fwd.restype = ctypes.c_int
     L.paged_attn_fwd.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, vp, i32, i32, vp, i32, i64, i32,
                                  i32, i32, i64, i32, ctypes.c_float, ctypes.c_float, vp, vp,
                                  ctypes.c_size_t, vp]
+    L.ta_paged_q8_workspace_bytes.restype = ctypes.c_size_t
+    L.ta_paged_q8_workspace_bytes.argtypes = list(L.ta_paged_workspace_bytes.argtypes)
+    L.paged_attn_fwd_q8.restype = ctypes.c_int
+    L.paged_attn_fwd_q8.argtypes = [vp, vp] + list(L.paged_attn_fwd.argtypes)
     L.ta_region_counts.restype = ctypes.c_int
     L.ta_region_counts.argtypes = [vp, i32, i32, i32, i32, vp]
     L.ta_region_grad_mean.restype = ctypes.c_int
@@ -514,11 +526,22 @@ def _cache_shape(k_cache):
     return tuple(k_cache.shape)
 
 
-def kv_cache_write(k, v, slots, k_cache, v_cache, stream=None):
-    """Enqueue the write of k, v [T, Hkv, d] bf16 (views with any token and
-    head stride that is a multiple of 8) into the slots [T] int32 of the caches
-    [pages, Hkv, page_size, d] bf16.  Rows with a negative slot are skipped;
-    the slots of one call are distinct."""
+def _cache_operands(k_cache, v_cache, k_scale, v_scale):
+    """Operands of a cache [pages, heads, page_size, head_dim]: bf16, or
+    float8_e4m3fn with scales float8_e8m0fnu [pages, heads, page_size]."""
+    import torch
+    shape = _cache_shape(k_cache)
+    if k_scale is None and v_scale is None:
+        return shape, [("k_cache", k_cache, torch.bfloat16, shape),
+                       ("v_cache", v_cache, torch.bfloat16, shape)]
+    return shape, [("k_cache", k_cache, torch.float8_e4m3fn, shape),
+                   ("v_cache", v_cache, torch.float8_e4m3fn, shape),
+                   ("k_scale", k_scale, torch.float8_e8m0fnu, shape[:3]),
+                   ("v_scale", v_scale, torch.float8_e8m0fnu, shape[:3])]
+
+
+def _check_rows(k, v):
+    """k, v [tokens, heads, head_dim] bf16 of any token and head stride."""
     import torch
     for name, t in (("k", k), ("v", v)):
         if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16:
@@ -529,24 +552,85 @@ def kv_cache_write(k, v, slots, k_cache, v_cache, stream=None):
             raise ValueError(f"the last dimension of {name} must be contiguous")
     if k.shape != v.shape:
         raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} differ")
+    if v.device != k.device:
+        raise ValueError(f"v is on {v.device}, k on {k.device}")
+
+
+def _row_strides(k, v):
+    # (the stride of a dimension of one says nothing)
+    many, heads = k.shape[0] > 1, k.shape[1] > 1
+    return (k.stride(0) if many else 0, k.stride(1) if heads else 0,
+            v.stride(0) if many else 0, v.stride(1) if heads else 0)
+
+
+def kv_cache_write(k, v, slots, k_cache, v_cache, stream=None, k_scale=None, v_scale=None):
+    """Enqueue the write of k, v [T, Hkv, d] bf16 (views with any token and
+    head stride that is a multiple of 8) into the slots [T] int32 of the caches
+    [pages, Hkv, page_size, d] bf16.  Rows with a negative slot are skipped;
+    the slots of one call are distinct.
+
+    With k_scale and v_scale [pages, Hkv, page_size] float8_e8m0fnu the caches
+    are float8_e4m3fn and the rows quantised, each with a scale of its own
+    (kv_cache_write_q8).
+    """
+    import torch
+    _check_rows(k, v)
     total, hkv, d = k.shape
     dev = k.device
-    if v.device != dev:
-        raise ValueError(f"v is on {v.device}, k on {dev}")
-    shape = _cache_shape(k_cache)
+    shape, named = _cache_operands(k_cache, v_cache, k_scale, v_scale)
     pages, ch, page_size, cd = shape
     if (ch, cd) != (hkv, d):
         raise ValueError(f"the caches have {ch} heads of {cd}, k has {hkv} of {d}")
-    _check_operands([("k_cache", k_cache, torch.bfloat16, shape),
-                     ("v_cache", v_cache, torch.bfloat16, shape),
-                     ("slots", slots, torch.int32, (total,))], dev)
+    named.append(("slots", slots, torch.int32, (total,)))
+    _check_operands(named, dev)
     _check_gpu(dev)
-    # (the stride of a dimension of one says nothing)
-    many, heads = total > 1, hkv > 1
-    _launch(dev, stream, lib().kv_cache_write, k.data_ptr(), v.data_ptr(),
-            k.stride(0) if many else 0, k.stride(1) if heads else 0,
-            v.stride(0) if many else 0, v.stride(1) if heads else 0, slots.data_ptr(), total,
-            k_cache.data_ptr(), v_cache.data_ptr(), pages, hkv, page_size, d)
+    if k_scale is None:
+        _launch(dev, stream, lib().kv_cache_write, k.data_ptr(), v.data_ptr(),
+                *_row_strides(k, v), slots.data_ptr(), total, k_cache.data_ptr(),
+                v_cache.data_ptr(), pages, hkv, page_size, d)
+    else:
+        _launch(dev, stream, lib().kv_cache_write_q8, k.data_ptr(), v.data_ptr(),
+                *_row_strides(k, v), slots.data_ptr(), total, k_cache.data_ptr(),
+                k_scale.data_ptr(), v_cache.data_ptr(), v_scale.data_ptr(), pages, hkv, page_size,
+                d)
+
+
+def kv_cache_read(k_cache, v_cache, block_table, cu, k, v, starts=None, stream=None, k_scale=None,
+                  v_scale=None):
+    """Enqueue cached rows back into k, v [T, Hkv, d] bf16 (views with any
+    token and head stride that is a multiple of 8): rows cu[b] .. cu[b + 1) get
+    positions starts[b], starts[b] + 1, .. of request b.
+
+    caches [pages, Hkv, page_size, d]: bf16, or float8_e4m3fn with k_scale,
+    v_scale [pages, Hkv, page_size] float8_e8m0fnu; block_table [B, W], cu [B +
+    1] and starts [B] (None: 0) int32.  Rows from cu[B] on are left as they are;
+    rows that no page of the cache holds are NaN.
+    """
+    import torch
+    _check_rows(k, v)
+    total, hkv, d = k.shape
+    dev = k.device
+    shape, named = _cache_operands(k_cache, v_cache, k_scale, v_scale)
+    pages, ch, page_size, cd = shape
+    if (ch, cd) != (hkv, d):
+        raise ValueError(f"the caches have {ch} heads of {cd}, k has {hkv} of {d}")
+    if not isinstance(cu, torch.Tensor) or cu.dim() != 1 or cu.shape[0] < 1:
+        raise ValueError("cu must be a tensor [requests + 1]")
+    b = cu.shape[0] - 1
+    i32 = torch.int32
+    named += [("cu", cu, i32, (b + 1,)), ("block_table", block_table, i32, None)]
+    if starts is not None:
+        named.append(("starts", starts, i32, (b,)))
+    _check_operands(named, dev)
+    _check_table(block_table, b)
+    _check_gpu(dev)
+    rest = (block_table.data_ptr(), b, block_table.shape[1], cu.data_ptr(), _addr(starts),
+            k.data_ptr(), v.data_ptr(), *_row_strides(k, v), total, pages, hkv, page_size, d)
+    if k_scale is None:
+        _launch(dev, stream, lib().kv_cache_read, k_cache.data_ptr(), v_cache.data_ptr(), *rest)
+    else:
+        _launch(dev, stream, lib().kv_cache_read_q8, k_cache.data_ptr(), k_scale.data_ptr(),
+                v_cache.data_ptr(), v_scale.data_ptr(), *rest)
 
 
 def ta_paged_workspace_bytes(batch, total_tokens, ragged, prefix, hq, hkv, head_dim) -> int:
@@ -554,10 +638,18 @@ def ta_paged_workspace_bytes(batch, total_tokens, ragged, prefix, hq, hkv, head_
                                               hkv, head_dim))
 
 
+def ta_paged_q8_workspace_bytes(batch, total_tokens, ragged, prefix, hq, hkv, head_dim) -> int:
+    return int(lib().ta_paged_q8_workspace_bytes(batch, total_tokens, int(ragged), int(prefix), hq,
+                                                 hkv, head_dim))
+
+
 def paged_attn_fwd(q, k_cache, v_cache, o, lse, kv_lens, cu_q, block_table, prefix_pages,
-                   prefix_len, softmax_scale, softcap, slopes, workspace, stream=None):
+                   prefix_len, softmax_scale, softcap, slopes, workspace, stream=None,
+                   k_scale=None, v_scale=None):
     """Enqueue attention of q [T, Hq, d] over the caches [pages, Hkv,
-    page_size, d], all bf16 (o bf16 or fp32).
+    page_size, d], all bf16 (o bf16 or fp32).  With k_scale and v_scale [pages,
+    Hkv, page_size] float8_e8m0fnu the caches are float8_e4m3fn (kv_cache_write)
+    and the workspace is of >= ta_paged_q8_workspace_bytes bytes.
 
     kv_lens [B] int32: own keys of each request, this call's tokens among
     them; cu_q [B + 1] int32 or None (one row a request); block_table [B, W]
@@ -574,7 +666,7 @@ def paged_attn_fwd(q, k_cache, v_cache, o, lse, kv_lens, cu_q, block_table, pref
     if not isinstance(o, torch.Tensor):
         raise ValueError("o must be a torch tensor")
     out = _out_dtype(o)
-    shape = _cache_shape(k_cache)
+    shape, caches = _cache_operands(k_cache, v_cache, k_scale, v_scale)
     pages, hkv, page_size, cd = shape
     if cd != d:
         raise ValueError(f"the caches have head_dim {cd}, q {d}")
@@ -582,8 +674,7 @@ def paged_attn_fwd(q, k_cache, v_cache, o, lse, kv_lens, cu_q, block_table, pref
         raise ValueError("kv_lens must be a tensor [requests]")
     b = kv_lens.shape[0]
     i32 = torch.int32
-    named = [("q", q, torch.bfloat16, None), ("k_cache", k_cache, torch.bfloat16, shape),
-             ("v_cache", v_cache, torch.bfloat16, shape), ("o", o, o.dtype, (total, hq, d)),
+    named = [("q", q, torch.bfloat16, None), *caches, ("o", o, o.dtype, (total, hq, d)),
              ("kv_lens", kv_lens, i32, (b,)), ("block_table", block_table, i32, None)]
     if lse is not None:
         named.append(("lse", lse, torch.float32, (hq, total)))
@@ -608,9 +699,13 @@ def paged_attn_fwd(q, k_cache, v_cache, o, lse, kv_lens, cu_q, block_table, pref
     if prefix_len > 0 and prefix_pages.shape[0] * page_size < prefix_len:
         raise ValueError(f"{prefix_pages.shape[0]} prefix pages of {page_size} hold no "
                          f"{prefix_len} keys")
-    _launch(dev, stream, lib().paged_attn_fwd, q.data_ptr(), k_cache.data_ptr(),
-            v_cache.data_ptr(), o.data_ptr(), out, _addr(lse), kv_lens.data_ptr(), _addr(cu_q),
-            block_table.data_ptr(), b, block_table.shape[1],
+    if k_scale is None:
+        fn, held = lib().paged_attn_fwd, (k_cache.data_ptr(), v_cache.data_ptr())
+    else:
+        fn = lib().paged_attn_fwd_q8
+        held = (k_cache.data_ptr(), k_scale.data_ptr(), v_cache.data_ptr(), v_scale.data_ptr())
+    _launch(dev, stream, fn, q.data_ptr(), *held, o.data_ptr(), out, _addr(lse),
+            kv_lens.data_ptr(), _addr(cu_q), block_table.data_ptr(), b, block_table.shape[1],
             prefix_pages.data_ptr() if prefix_len > 0 else None, prefix_len, total, hq, hkv, d,
             pages, page_size, float(softmax_scale), 0.0 if softcap is None else float(softcap),
             _addr(slopes), _addr(workspace), _nbytes(workspace))
@@ -623,20 +718,24 @@ class PagedPlan:
     and a captured call needs its plan as long as its graph."""
 
     def __init__(self, batch, total_tokens, hq, hkv, head_dim, prefix=False, ragged=False,
-                 device="cuda"):
+                 device="cuda", q8=False):
         """prefix: whether calls have a shared prefix; ragged: whether they
-        give cu_q (otherwise every request has one row)."""
+        give cu_q (otherwise every request has one row); q8: whether the caches
+        hold 8 bits (k_scale and v_scale are then given)."""
         import torch
-        nbytes = ta_paged_workspace_bytes(batch, total_tokens, ragged, prefix, hq, hkv, head_dim)
+        size = ta_paged_q8_workspace_bytes if q8 else ta_paged_workspace_bytes
+        nbytes = size(batch, total_tokens, ragged, prefix, hq, hkv, head_dim)
         self.workspace = (torch.empty(nbytes, dtype=torch.uint8, device=device)
                           if nbytes > 0 else None)
 
     def run(self, q, k_cache, v_cache, o, kv_lens, block_table, cu_q=None, prefix_pages=None,
-            prefix_len=0, lse=None, softmax_scale=None, softcap=None, slopes=None, stream=None):
+            prefix_len=0, lse=None, softmax_scale=None, softcap=None, slopes=None, stream=None,
+            k_scale=None, v_scale=None):
         if softmax_scale is None:
             softmax_scale = 1.0 / float(q.shape[-1]) ** 0.5
         paged_attn_fwd(q, k_cache, v_cache, o, lse, kv_lens, cu_q, block_table, prefix_pages,
-                       prefix_len, softmax_scale, softcap, slopes, self.workspace, stream)
+                       prefix_len, softmax_scale, softcap, slopes, self.workspace, stream,
+                       k_scale, v_scale)
         return o
 
 

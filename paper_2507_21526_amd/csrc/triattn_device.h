@@ -53,6 +53,16 @@ __device__ __forceinline__ void copy_to_lds16(const void *gbase, uint32_t lane_b
                  : "v"(lane_byte_off), "s"(gbase), "{m0}"(lds_addr));
 }
 
+// The same with four bytes a lane and an address of each lane's own.
+__device__ __forceinline__ void copy_to_lds4(const void *from, uint32_t lds_addr)
+{
+    asm volatile("s_nop 0\n\t"
+                 "global_load_lds_dword %0, off"
+                 :
+                 : "v"(from), "{m0}"(lds_addr)
+                 : "memory");
+}
+
 // A burst of N (2 or 4) such copies into consecutive 1 KB blocks of LDS
 // from lds_addr on, with one M0 write and one wait state for all of them:
 // copy i uses the instruction offset i KB, which the hardware adds to both

@@ -25,6 +25,7 @@
 #include "triattn_device.h"
 #include "triattn_internal.h"
 #include "triattn_rows.h"
+#include "triattn_rows8.h"
 #include "triattn_spans.h"
 
 namespace triattn {
@@ -45,7 +46,9 @@ constexpr int kRecordWords = 8;
 enum RecordField { RF_Q0 = 0, RF_RHO0, RF_ROWS, RF_POS0, RF_BEGIN, RF_END, RF_SHARE };
 
 struct PagedArgs {
-    const uint16_t *q, *kc, *vc;
+    const uint16_t *q;
+    const unsigned char *kc, *vc;  // bf16, or 8-bit elements with
+    const unsigned char *ks, *vs;  // a scale a row
     void *o;
     float *lse;
     const int32_t *kv_lens, *cu_q, *table, *prefix_pages;
@@ -72,7 +75,7 @@ struct PagedArgs {
 //     request with query offsets and 8 without: fewer share a CU from some 700
 //     requests with offsets on at d = 128, from 280 (700 without) at d = 64.
 //   RB = 4: four waves of 32 rows each over the same 64-key tiles, in two stages.
-template <int D, int RB>
+template <int D, int RB, bool Q8>
 struct PagedShape {
     static constexpr int NKB = RB == 4 ? 2 : 1;
     static constexpr int TK = 32 * NKB;      // keys of a tile
@@ -80,16 +83,21 @@ struct PagedShape {
     static constexpr int THREADS = 64 * RB * KS;
     static constexpr int STEP = TK * KS;     // keys of a step
     static constexpr int ROWS = 32 * RB;
-    static constexpr int TILE_BYTES = TK * 2 * D;
-    static constexpr int STAGE_BYTES = 2 * TILE_BYTES;  // K tile, then V tile
-    static constexpr int LDS_BYTES = KS * 2 * STAGE_BYTES;
+    static constexpr bool TILES8 = Q8 && RB == 1;  // tiles in LDS hold 8 bits too
+    static constexpr int TILE_BYTES = TK * (TILES8 ? D : 2 * D);
+    // K tile, V tile, and of 8-bit tiles the scales: the bytes as they come (K's,
+    // V's), then V's as fp32
+    static constexpr int STAGE_BYTES = 2 * TILE_BYTES + (TILES8 ? 256 : 0);
+    static constexpr int STAGES = TILES8 && D == 64 ? 4 : 2;
+    static constexpr int BUFFER_BYTES = STAGES * STAGE_BYTES;  // of a wave (RB = 1)
+    static constexpr int LDS_BYTES = KS * BUFFER_BYTES;
     // Least steps of a share: one of a 128-row tile leaves partials of twice
     // its K and V tiles' bytes.  us with 1, 4 and 8 steps (32 heads over 8, d =
     // 128): the last 64 tokens of 2000 27, 25, 29, of four times 1000 29, 25, 28,
     // 128 single tokens behind a prefix of 2048 47, 43, 44, the last 100 tokens of
     // 500 17, 24, 29; from 3000 keys on the same.
     static constexpr int LEAST = RB == 4 ? 4 : 1;
-    static constexpr int WGS_PER_CU = RB == 1 && D == 64 ? 4 : 2;
+    static constexpr int WGS_PER_CU = RB == 1 && (D == 64 || Q8) ? 4 : 2;
     static constexpr int WAVES_PER_SIMD = (WGS_PER_CU * THREADS / 64 + 3) / 4;
 };
 
@@ -152,14 +160,14 @@ struct RowTile {
     int32_t bad;    // a length past the block table
 };
 
-template <int D, int RB, int SCORE, bool PREFIX>
-__global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
-                             (PagedShape<D, RB>::WAVES_PER_SIMD)) void paged_attn_kernel(PagedArgs a)
+template <int D, int RB, int SCORE, bool PREFIX, bool Q8>
+__global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
+                             (PagedShape<D, RB, Q8>::WAVES_PER_SIMD)) void paged_attn_kernel(PagedArgs a)
 {
-    using S = PagedShape<D, RB>;
+    using S = PagedShape<D, RB, Q8>;
     constexpr int kThreads = S::THREADS;
-    constexpr int ROW_BYTES = 2 * D;
-    constexpr int CHUNKS = D / 8;
+    constexpr int ROW_BYTES = Q8 ? D : 2 * D;            // of a cached row
+    constexpr int CHUNKS = ROW_BYTES / 16;
     constexpr int COPY_ROWS = 1024 / ROW_BYTES;          // keys of a 1 KB copy
     constexpr int GROUP = 16;  // keys that surely share a page
     constexpr int COPIES = GROUP / COPY_ROWS;              // 1 KB copies of a group
@@ -323,22 +331,28 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
     const uint32_t smem_addr =
         (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
     // this wave's buffers (RB = 1) or the workgroup's stages (RB = 4)
-    const int wave_lds = RB == 1 ? wave * 2 * S::STAGE_BYTES : 0;
+    const int wave_lds = RB == 1 ? wave * S::BUFFER_BYTES : 0;
     const int first_group = RB == 1 ? 0 : wave * GROUPS;
     const int dma_row = lane / CHUNKS;
     // a copying lane's place in a group's first block; block m flips the K
     // swizzle's bits of m COPY_ROWS
-    const uint32_t dma_k =
-        (uint32_t)(dma_row * ROW_BYTES + (((lane % CHUNKS) ^ rows_kswz<D>(dma_row)) << 4));
+    const uint32_t dma_k = (uint32_t)(
+        dma_row * ROW_BYTES +
+        (((lane % CHUNKS) ^ (Q8 ? rows8_swz<D>(dma_row) : rows_kswz<D>(dma_row))) << 4));
     const uint32_t dma_v =
-        (uint32_t)(dma_row * ROW_BYTES + (((lane % CHUNKS) ^ rows_vswz<D>(dma_row)) << 4));
+        Q8 ? dma_k
+           : (uint32_t)(dma_row * ROW_BYTES + (((lane % CHUNKS) ^ rows_vswz<D>(dma_row)) << 4));
     const int64_t page_stride = ((int64_t)a.hkv << a.page_log2) * ROW_BYTES;
     const int64_t head_off = ((int64_t)g << a.page_log2) * ROW_BYTES;
-    const unsigned char *kc = reinterpret_cast<const unsigned char *>(a.kc) + head_off;
-    const unsigned char *vc = reinterpret_cast<const unsigned char *>(a.vc) + head_off;
+    const unsigned char *kc = a.kc + head_off;
+    const unsigned char *vc = a.vc + head_off;
     const int page_mask = (1 << a.page_log2) - 1;
+    // the scale of a key of this head in a page
+    auto scale_at = [&](const unsigned char *base, int id, int place) TA_INLINE {
+        return base + ((((int64_t)id * a.hkv + g) << a.page_log2) + place);
+    };
 
-    RowBlock<D, S::NKB, SCORE> rb;
+    std::conditional_t<S::TILES8, RowBlock8<D, S::NKB, SCORE>, RowBlock<D, S::NKB, SCORE>> rb;
     rb.init(lane);
 
     for (int at = share0, t = -1; at < share1;) {
@@ -453,9 +467,14 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
                     uint32_t off[COPIES];
 #pragma unroll
                     for (int m = 0; m < COPIES; ++m)
-                        off[m] = V ? dma_v : dma_k ^ (uint32_t)(rows_kswz<D>(m * COPY_ROWS) << 4);
+                        off[m] = V || Q8 ? dma_v
+                                         : dma_k ^ (uint32_t)(rows_kswz<D>(m * COPY_ROWS) << 4);
                     if (inside) {
-                        copy_burst_to_lds16<COPIES>(page + (key & page_mask) * ROW_BYTES, off, to);
+                        if constexpr (COPIES == 1)
+                            copy_to_lds16(page + (key & page_mask) * ROW_BYTES, off[0], to);
+                        else
+                            copy_burst_to_lds16<COPIES>(page + (key & page_mask) * ROW_BYTES, off,
+                                                        to);
                     } else {
 #pragma unroll
                         for (int m = 0; m < COPIES; ++m) {
@@ -471,15 +490,51 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
             };
             using K = std::false_type;
             using V = std::true_type;
+            // The scales of a tile whose copies begin at key0: lane i copies four
+            // bytes, of K's keys or of V's (lanes past them repeat the same).
+            auto copy_scales = [&](int key0, uint32_t lds) TA_INLINE {
+                constexpr int PER = S::TK / 4;  // lanes of K's keys
+                // (keys from rt.limit on: bytes of the last ones, not used)
+                const int key = min(key0 + 4 * (lane & (PER - 1)), (rt.limit - 1) & ~3);
+                const int id = s_page[(key >> a.page_log2) - page0];
+                copy_to_lds4(scale_at(lane & PER ? a.vs : a.ks, id, key & page_mask),
+                             smem_addr + lds + 2 * S::TILE_BYTES);
+            };
             f32x16 s[S::NKB];
             bf16x8 p[S::NKB][2];
-            auto softmax = [&](int key0) TA_INLINE {
+            // scales of an 8-bit tile: K's of this lane's key, V's in LDS
+            float kscale[S::NKB];
+            bool scale_nan = false;
+            auto scales = [&](int key0, unsigned char *stage) TA_INLINE {
+                const unsigned char *raw = stage + 2 * S::TILE_BYTES;
+                kscale[0] = q8_scale_bits(raw[rows_perm(rb.col)]);
+                const uint32_t b = raw[S::TK + rb.col];
+                // a key that no row keeps weighs 0, not NaN
+                const bool on = key0 + rb.col < rt.limit;
+                scale_nan = __builtin_amdgcn_ballot_w64(on && b == 255) != 0;
+                reinterpret_cast<float *>(stage + 2 * S::TILE_BYTES + 128)[rb.col] =
+                    on ? q8_scale(b) : 0.f;
+            };
+            auto softmax = [&](int key0, const unsigned char *stage) TA_INLINE {
                 rb.modify(s, a.score);
                 if (__builtin_expect(key0 + S::TK - 1 > first_last, 0)) {
                     asm volatile("");  // a branch: most steps have no mask
                     rb.mask_above(s, last - key0);
                 }
-                rb.softmax(s, a.score, slope, key0 - dist_row, p, fresh);
+                if constexpr (S::TILES8) {
+                    // V's scales of this lane's keys (rows_key_of_reg)
+                    f32x4r w[4];
+                    const float *vscale =
+                        reinterpret_cast<const float *>(stage + 2 * S::TILE_BYTES + 128);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        w[i] = *reinterpret_cast<const f32x4r *>(vscale + 16 * (i >> 1) +
+                                                                 8 * rb.half + 4 * (i & 1));
+                    rb.softmax(s, a.score, slope, key0 - dist_row, p, fresh,
+                               [&](int, int v, float x) TA_INLINE { return x * w[v / 4][v % 4]; });
+                } else {
+                    rb.softmax(s, a.score, slope, key0 - dist_row, p, fresh);
+                }
                 fresh = false;
             };
             auto values = [&](int key0, const unsigned char *vt) TA_INLINE {
@@ -487,18 +542,68 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
                 // part of the values each)
                 if (__builtin_expect(key0 + S::TK - 1 > tile_first_last, 0)) {
                     asm volatile("");
-                    odd |= rb.odd_values(vt, lane, RB == 1 ? 0 : wave, RB);
+                    if constexpr (S::TILES8)
+                        odd |= scale_nan || rb.odd_elements(vt, lane);
+                    else
+                        odd |= rb.odd_values(vt, lane, RB == 1 ? 0 : wave, RB);
                 }
-                __builtin_amdgcn_sched_barrier(0);
-                rb.accumulate(vt, p);
-                rb.template schedule<false, true>();
-                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (S::TILES8) {
+                    rb.accumulate8(vt, p);
+                } else {
+                    __builtin_amdgcn_sched_barrier(0);
+                    rb.accumulate(vt, p);
+                    rb.template schedule<false, true>();
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             };
             auto products = [&](const unsigned char *kt) TA_INLINE {
-                __builtin_amdgcn_sched_barrier(0);
-                rb.products(kt, s);
-                rb.template schedule<true, false>();
-                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (S::TILES8) {
+                    rb.products8(kt, kscale, s);
+                } else {
+                    __builtin_amdgcn_sched_barrier(0);
+                    rb.products(kt, s);
+                    rb.template schedule<true, false>();
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            };
+            // An 8-bit cache's rows as bf16 tiles (RB = 4): a wave loads a group's
+            // rows and scales into registers, and later leaves them in LDS, each
+            // element times its scale.
+            constexpr int LOADS = Q8 ? GROUP * D / 1024 : 1;  // 16-byte loads of a lane, K or V
+            constexpr int LOAD_ROWS = GROUP / LOADS;
+            u32x4 held[2][LOADS];
+            uint32_t held_scale[2][LOADS];
+            const int load_row = lane / (D / 16), load_chunk = lane % (D / 16);
+            auto load_rows = [&](int key0) TA_INLINE {
+                const int first = min(key0 + wave * GROUP, rt.limit - 1);
+                const int lim = min(rt.limit - 1 - first, GROUP - 1);  // the group's last row
+                const int id = uni(s_page[(first >> a.page_log2) - page0]);
+                const int place = first & page_mask;
+                const int64_t off = (int64_t)id * page_stride + place * ROW_BYTES;
+                const unsigned char *kp = kc + off, *vp = vc + off;
+                const unsigned char *ksp = scale_at(a.ks, id, place);
+                const unsigned char *vsp = scale_at(a.vs, id, place);
+#pragma unroll
+                for (int m = 0; m < LOADS; ++m) {
+                    const uint32_t row = min(m * LOAD_ROWS + load_row, lim);
+                    const uint32_t at = row * D + load_chunk * 16;
+                    held[0][m] = *reinterpret_cast<const u32x4 *>(kp + at);
+                    held[1][m] = *reinterpret_cast<const u32x4 *>(vp + at);
+                    held_scale[0][m] = ksp[row];
+                    held_scale[1][m] = vsp[row];
+                }
+            };
+            auto leave_rows = [&](int c, int stage) TA_INLINE {
+                const int v = c / LOADS, m = c % LOADS;
+                const int row = m * LOAD_ROWS + load_row;  // in the group
+                const int swz = v ? rows_vswz<D>(row) : rows_kswz<D>(row);
+                unsigned char *to = smem + stage * S::STAGE_BYTES + v * S::TILE_BYTES +
+                                    (wave * GROUP + row) * 2 * D;
+                const float f = q8_scale_bits(held_scale[v][m]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    *reinterpret_cast<bf16x8 *>(to + (((2 * load_chunk + i) ^ swz) << 4)) =
+                        q8_fragment(held[v][m][2 * i], held[v][m][2 * i + 1], f);
             };
             if constexpr (CAREFUL) {
                 // tile by tile, in this wave's first stage (RB = 1) or the
@@ -508,16 +613,28 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
                     const int key0 = (seg0 + (BACK ? n - 1 - i : i)) * S::STEP +
                                      (RB == 1 ? wave * S::TK : 0);
                     const bool on = key0 < key_end;
-                    if (on) {
+                    if constexpr (Q8 && RB == 4) {
+                        load_rows(key0);
+#pragma unroll
+                        for (int c = 0; c < 2 * LOADS; ++c)
+                            leave_rows(c, 0);
+                    } else if (on) {
                         copy(key0, wave_lds, K{});
                         copy(key0, wave_lds + S::TILE_BYTES, V{});
+                        if constexpr (Q8)
+                            copy_scales(key0, wave_lds);
                     }
                     rows_wait_copies<0>();
                     barrier_no_fence();
                     if (on) {
+                        if constexpr (S::TILES8)
+                            scales(key0, smem + wave_lds);
                         products(smem + wave_lds);
-                        softmax(key0);
-                        rb.accumulate_by_key(smem + wave_lds + S::TILE_BYTES, s, p);
+                        softmax(key0, smem + wave_lds);
+                        if constexpr (S::TILES8)
+                            rb.accumulate8_by_key(smem + wave_lds + S::TILE_BYTES, s, p);
+                        else
+                            rb.accumulate_by_key(smem + wave_lds + S::TILE_BYTES, s, p);
                     }
                     barrier_no_fence();
                 }
@@ -531,28 +648,91 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
                 auto copies = [&](int key0, int stage) TA_INLINE {
                     copy(key0, wave_lds + stage * S::STAGE_BYTES, K{});
                     copy(key0, wave_lds + stage * S::STAGE_BYTES + S::TILE_BYTES, V{});
+                    if constexpr (Q8)
+                        copy_scales(key0, wave_lds + stage * S::STAGE_BYTES);
                     __builtin_amdgcn_sched_barrier(0);
                 };
-                if (n > 0)
-                    copies(key_of(0), 0);
-                if (n > 1)
-                    copies(key_of(1), 1);
+                constexpr int TILE_COPIES = 2 * GROUPS * COPIES + (Q8 ? 1 : 0);
+#pragma unroll
+                for (int i = 0; i < S::STAGES; ++i)
+                    if (i < n)
+                        copies(key_of(i), i);
                 auto step = [&](int i, auto stage) TA_INLINE {
                     constexpr int ST = decltype(stage)::value;
-                    const unsigned char *kt = smem + wave_lds + ST * S::STAGE_BYTES;
-                    if (i + 1 < n)
-                        rows_wait_copies<2 * GROUPS * COPIES>();
+                    unsigned char *kt = smem + wave_lds + ST * S::STAGE_BYTES;
+                    // the tiles behind this one may still be on their way
+                    if (i + S::STAGES - 1 < n)
+                        rows_wait_copies<(S::STAGES - 1) * TILE_COPIES>();
+                    else if (S::STAGES > 2 && i + 1 < n)
+                        rows_wait_copies<TILE_COPIES>();
                     else
                         rows_wait_copies<0>();
+                    if constexpr (Q8)
+                        scales(key_of(i), kt);
                     products(kt);
-                    softmax(key_of(i));
+                    softmax(key_of(i), kt);
                     values(key_of(i), kt + S::TILE_BYTES);
-                    if (i + 2 < n) {
+                    if (i + S::STAGES < n) {
                         // every read of the stage has returned before it is
                         // written again
                         __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
-                        copies(key_of(i + 2), ST);
+                        copies(key_of(i + S::STAGES), ST);
                     }
+                };
+                int i = 0;
+                if constexpr (S::STAGES == 4)
+                    for (; i + 3 < n; i += 4) {
+                        step(i, std::integral_constant<int, 0>{});
+                        step(i + 1, std::integral_constant<int, 1>{});
+                        step(i + 2, std::integral_constant<int, 2>{});
+                        step(i + 3, std::integral_constant<int, 3>{});
+                    }
+                else
+                    for (; i + 1 < n; i += 2) {
+                        step(i, std::integral_constant<int, 0>{});
+                        step(i + 1, std::integral_constant<int, 1>{});
+                    }
+                if (i < n)
+                    step(i, std::integral_constant<int, 0>{});
+                if constexpr (S::STAGES == 4) {
+                    if (i + 1 < n)
+                        step(i + 1, std::integral_constant<int, 1>{});
+                    if (i + 2 < n)
+                        step(i + 2, std::integral_constant<int, 2>{});
+                }
+            } else if constexpr (Q8) {
+                // As below, but through registers: step i leaves the rows of step
+                // i + 1 in LDS between its matrix instructions, and then loads
+                // those of i + 2.
+                const int n = (key_end - seg0 * S::STEP + S::STEP - 1) / S::STEP;
+                auto key_of = [&](int i) TA_INLINE -> int {
+                    return (seg0 + (BACK ? n - 1 - i : i)) * S::STEP;
+                };
+                load_rows(key_of(0));
+#pragma unroll
+                for (int c = 0; c < 2 * LOADS; ++c)
+                    leave_rows(c, 0);
+                load_rows(key_of(min(1, n - 1)));
+                constexpr int STRIDE = S::NKB * (D / 16) / (2 * LOADS);
+                auto step = [&](int i, auto stage) TA_INLINE {
+                    constexpr int ST = decltype(stage)::value;
+                    // this step's tile is there for every wave, and every wave is
+                    // done with the other stage
+                    __builtin_amdgcn_sched_barrier(0);
+                    barrier_no_fence();
+                    __builtin_amdgcn_sched_barrier(0);
+                    // (after the last step its tile is left once more, in the stage
+                    // that nothing reads any more)
+                    const unsigned char *kt = smem + ST * S::STAGE_BYTES;
+                    rb.products(kt, s, [&](int m) TA_INLINE {
+                        if (m % STRIDE == STRIDE - 1 && m / STRIDE < 2 * LOADS)
+                            leave_rows(m / STRIDE, 1 - ST);
+                    });
+                    __builtin_amdgcn_sched_barrier(0);
+                    load_rows(key_of(min(i + 2, n - 1)));
+                    __builtin_amdgcn_sched_barrier(0);
+                    softmax(key_of(i), kt);
+                    values(key_of(i), kt + S::TILE_BYTES);
                 };
                 int i = 0;
                 for (; i + 1 < n; i += 2) {
@@ -617,7 +797,7 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
                     const int key0 = now.key0;
                     now = next;
                     next = place(min(i + 2, n - 1));
-                    softmax(key0);
+                    softmax(key0, kt);
                     values(key0, kt + S::TILE_BYTES);
                 };
                 int i = 0;
@@ -677,11 +857,11 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
             // join the waves: each leaves its accumulators in its buffers,
             // 16-byte chunks of row r permuted by r against bank conflicts
             constexpr int PITCH = 4 * D;
-            static_assert(32 * PITCH <= 2 * S::STAGE_BYTES, "accumulators fit the wave's stages");
+            static_assert(32 * PITCH <= S::BUFFER_BYTES, "accumulators fit the wave's stages");
             auto place = [&](int r, int chunk) TA_INLINE -> int {
                 return r * PITCH + ((chunk ^ (r & (D / 4 - 1))) << 4);
             };
-            unsigned char *mine = smem + wave * 2 * S::STAGE_BYTES;
+            unsigned char *mine = smem + wave * S::BUFFER_BYTES;
             const float l = rows_pair_sum(rb.l_run);
             if (rb.col < rt.rows) {
                 if (rb.half == 0) {
@@ -715,7 +895,7 @@ __global__ __launch_bounds__((PagedShape<D, RB>::THREADS),
                     const float f = __builtin_amdgcn_exp2f(s_ml[w][r][0] - m_use);
                     den += f * s_ml[w][r][1];
                     const f32x4r y = *reinterpret_cast<const f32x4r *>(
-                        smem + w * 2 * S::STAGE_BYTES + place(r, d0 / 4));
+                        smem + w * S::BUFFER_BYTES + place(r, d0 / 4));
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         x[e] += f * y[e];
@@ -899,16 +1079,18 @@ struct PagedLayout {
         pre_row_o, pre_row_lse, bytes;
 };
 
+template <bool Q8>
 int wgs_per_cu(int rb, int d)
 {
     if (d == 128)
-        return rb == 4 ? PagedShape<128, 4>::WGS_PER_CU : PagedShape<128, 1>::WGS_PER_CU;
-    return rb == 4 ? PagedShape<64, 4>::WGS_PER_CU : PagedShape<64, 1>::WGS_PER_CU;
+        return rb == 4 ? PagedShape<128, 4, Q8>::WGS_PER_CU : PagedShape<128, 1, Q8>::WGS_PER_CU;
+    return rb == 4 ? PagedShape<64, 4, Q8>::WGS_PER_CU : PagedShape<64, 1, Q8>::WGS_PER_CU;
 }
 
 PagedLayout paged_layout(int32_t batch, int64_t total_tokens, bool ragged, bool prefix, int32_t hq,
-                         int32_t hkv, int32_t d)
+                         int32_t hkv, int32_t d, bool q8)
 {
+    auto per_cu = [&](int rb) { return q8 ? wgs_per_cu<true>(rb, d) : wgs_per_cu<false>(rb, d); };
     PagedLayout p{};
     const int64_t group = hq / hkv;
     // Up to 32 rows a request on average: tiles of 32 rows, which a
@@ -921,8 +1103,8 @@ PagedLayout paged_layout(int32_t batch, int64_t total_tokens, bool ragged, bool 
     // 255 single tokens and one piece of 1024 915 (as chosen) and 823.
     p.own_rb = !ragged || total_tokens * group <= (int64_t)batch * 32 ? 1 : 4;
     p.pre_rb = total_tokens * group <= 32 ? 1 : 4;
-    p.own_slots = std::max(1, kCus * wgs_per_cu(p.own_rb, d) / hkv);
-    p.pre_slots = std::max(1, kCus * wgs_per_cu(p.pre_rb, d) / hkv);
+    p.own_slots = std::max(1, kCus * per_cu(p.own_rb) / hkv);
+    p.pre_slots = std::max(1, kCus * per_cu(p.pre_rb) / hkv);
     const int64_t rows = 32 * p.own_rb;
     p.max_tiles = (int)std::min<int64_t>(
         kMaxTiles + 1, ragged ? total_tokens * group / rows + batch : (int64_t)batch);
@@ -958,61 +1140,56 @@ uint32_t table_bytes(const PagedArgs &a)
                            (a.cu_q ? 2 * (a.batch + 1) : 0));
 }
 
-template <int D, int RB, bool PREFIX>
+template <int D, int RB, bool PREFIX, bool Q8>
 void launch_scores(int score, dim3 grid, hipStream_t s, const PagedArgs &a)
 {
-    const dim3 threads(PagedShape<D, RB>::THREADS);
+    const dim3 threads(PagedShape<D, RB, Q8>::THREADS);
     const uint32_t lds = PREFIX ? 0 : table_bytes(a);
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, threads, lds, s, a); };
     switch (score) {
-    case 0: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 0, PREFIX>), grid, threads, lds, s, a); break;
-    case 1: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 1, PREFIX>), grid, threads, lds, s, a); break;
-    case 2: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 2, PREFIX>), grid, threads, lds, s, a); break;
-    default: hipLaunchKernelGGL((paged_attn_kernel<D, RB, 3, PREFIX>), grid, threads, lds, s, a); break;
+    case 0: launch(paged_attn_kernel<D, RB, 0, PREFIX, Q8>); break;
+    case 1: launch(paged_attn_kernel<D, RB, 1, PREFIX, Q8>); break;
+    case 2: launch(paged_attn_kernel<D, RB, 2, PREFIX, Q8>); break;
+    default: launch(paged_attn_kernel<D, RB, 3, PREFIX, Q8>); break;
     }
 }
 
-template <bool PREFIX>
+template <bool PREFIX, bool Q8>
 hipError_t launch_pass(int d, int rb, int score, hipStream_t s, const PagedArgs &a)
 {
     const dim3 grid((uint32_t)(a.slots * a.hkv));
     if (d == 128 && rb == 1)
-        launch_scores<128, 1, PREFIX>(score, grid, s, a);
+        launch_scores<128, 1, PREFIX, Q8>(score, grid, s, a);
     else if (d == 128)
-        launch_scores<128, 4, PREFIX>(score, grid, s, a);
+        launch_scores<128, 4, PREFIX, Q8>(score, grid, s, a);
     else if (rb == 1)
-        launch_scores<64, 1, PREFIX>(score, grid, s, a);
+        launch_scores<64, 1, PREFIX, Q8>(score, grid, s, a);
     else
-        launch_scores<64, 4, PREFIX>(score, grid, s, a);
+        launch_scores<64, 4, PREFIX, Q8>(score, grid, s, a);
     return hipGetLastError();
 }
 
-}  // namespace
-}  // namespace triattn
-
-using namespace triattn;
-
-extern "C" size_t ta_paged_workspace_bytes(int32_t batch, int64_t total_tokens, int32_t ragged,
-                                           int32_t prefix, int32_t hq, int32_t hkv,
-                                           int32_t head_dim)
+size_t workspace_bytes_of(int32_t batch, int64_t total_tokens, int32_t ragged, int32_t prefix,
+                          int32_t hq, int32_t hkv, int32_t head_dim, bool q8)
 {
     if (batch < 0 || total_tokens < 0 || total_tokens > INT32_MAX || hq <= 0 || hkv <= 0 ||
         hq % hkv != 0 || hq / hkv > 8 || (head_dim != 64 && head_dim != 128))
         return 0;
-    return paged_layout(batch, total_tokens, ragged != 0, prefix != 0, hq, hkv, head_dim).bytes;
+    return paged_layout(batch, total_tokens, ragged != 0, prefix != 0, hq, hkv, head_dim, q8)
+        .bytes;
 }
 
-extern "C" ta_status paged_attn_fwd(const void *q, const void *k_cache, const void *v_cache,
-                                    void *o, int32_t o_dtype, float *lse, const int32_t *kv_lens,
-                                    const int32_t *cu_q, const int32_t *block_table, int32_t batch,
-                                    int32_t table_width, const int32_t *prefix_pages,
-                                    int32_t prefix_len, int64_t total_tokens, int32_t hq,
-                                    int32_t hkv, int32_t head_dim, int64_t num_pages,
-                                    int32_t page_size, float softmax_scale, float softcap,
-                                    const float *slopes, void *workspace, size_t workspace_bytes,
-                                    void *stream)
+// A call on either form of the cache (k_scale, v_scale: of the 8-bit one).
+ta_status paged_attn(const char *fn, bool q8, const void *q, const void *k_cache,
+                     const void *k_scale, const void *v_cache, const void *v_scale, void *o,
+                     int32_t o_dtype, float *lse, const int32_t *kv_lens, const int32_t *cu_q,
+                     const int32_t *block_table, int32_t batch, int32_t table_width,
+                     const int32_t *prefix_pages, int32_t prefix_len, int64_t total_tokens,
+                     int32_t hq, int32_t hkv, int32_t head_dim, int64_t num_pages,
+                     int32_t page_size, float softmax_scale, float softcap, const float *slopes,
+                     void *workspace, size_t workspace_bytes, void *stream)
 {
     clear_error();
-    const char *fn = "paged_attn_fwd";
     if (batch < 0 || total_tokens < 0 || table_width < 0 || prefix_len < 0 || num_pages < 0)
         return fail(TA_ERR_INVALID_ARG, "%s: negative size", fn);
     if (hq <= 0 || hkv <= 0)
@@ -1050,7 +1227,7 @@ extern "C" ta_status paged_attn_fwd(const void *q, const void *k_cache, const vo
         (int64_t)total_tokens * hq > INT32_MAX)
         return fail(TA_ERR_UNSUPPORTED, "%s: positions, slots or rows past 32 bits", fn);
     const PagedLayout p =
-        paged_layout(batch, total_tokens, cu_q != nullptr, prefix_len > 0, hq, hkv, head_dim);
+        paged_layout(batch, total_tokens, cu_q != nullptr, prefix_len > 0, hq, hkv, head_dim, q8);
     const int64_t group = hq / hkv;
     if (p.max_tiles > kMaxTiles)
         return fail(TA_ERR_UNSUPPORTED, "%s: more than %d row tiles a kv head (pass fewer query "
@@ -1071,40 +1248,48 @@ extern "C" ta_status paged_attn_fwd(const void *q, const void *k_cache, const vo
     if (total_tokens == 0 || batch == 0)
         return TA_OK;
     if (!q || !o || !kv_lens || (num_pages > 0 && (!k_cache || !v_cache)) ||
+        (q8 && num_pages > 0 && (!k_scale || !v_scale)) ||
         (table_width > 0 && !block_table) || (prefix_len > 0 && !prefix_pages))
         return fail(TA_ERR_INVALID_ARG, "%s: NULL argument", fn);
     if (num_pages == 0)
         return fail(TA_ERR_INVALID_ARG, "%s: a cache without pages", fn);
     if (((uintptr_t)q | (uintptr_t)k_cache | (uintptr_t)v_cache | (uintptr_t)o) & 15)
         return fail(TA_ERR_INVALID_ARG, "%s: q, o and the caches must be 16-byte aligned", fn);
+    if (((uintptr_t)k_scale | (uintptr_t)v_scale) & 3)
+        return fail(TA_ERR_INVALID_ARG, "%s: the scales must be 4-byte aligned", fn);
     if (!workspace || workspace_bytes < p.bytes)
         return fail(TA_ERR_WORKSPACE, "%s: workspace of %zu bytes, need %zu", fn,
                     workspace ? workspace_bytes : (size_t)0, p.bytes);
     if ((uintptr_t)workspace & 15)
         return fail(TA_ERR_WORKSPACE, "%s: workspace must be 16-byte aligned", fn);
     {
-        const int64_t rows = total_tokens * hq, cache = ((num_pages * hkv) << lp) * head_dim * 2;
+        const int64_t rows = total_tokens * hq, held = (num_pages * hkv) << lp;
+        const int64_t cache = held * head_dim * (q8 ? 1 : 2);
         const Span spans[] = {{o, rows * head_dim * (o_dtype == TA_OUT_F32 ? 4 : 2)},
                               {lse, 4 * rows},
                               {workspace, (int64_t)p.bytes},
                               {q, rows * head_dim * 2},
                               {k_cache, cache},
                               {v_cache, cache},
+                              {k_scale, held},
+                              {v_scale, held},
                               {kv_lens, 4LL * batch},
                               {cu_q, 4LL * batch + 4},
                               {block_table, 4LL * batch * table_width},
                               {prefix_len > 0 ? prefix_pages : nullptr,
                                4 * (((int64_t)prefix_len + page_size - 1) >> lp)},
                               {slopes, 4LL * hq}};
-        if (spans_overlap(spans, 3, 11))
+        if (spans_overlap(spans, 3, 13))
             return fail(TA_ERR_INVALID_ARG, "%s: an output overlaps another argument", fn);
     }
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     auto part = [&](size_t off) { return reinterpret_cast<float *>(ws + off); };
     PagedArgs a{};
     a.q = static_cast<const uint16_t *>(q);
-    a.kc = static_cast<const uint16_t *>(k_cache);
-    a.vc = static_cast<const uint16_t *>(v_cache);
+    a.kc = static_cast<const unsigned char *>(k_cache);
+    a.vc = static_cast<const unsigned char *>(v_cache);
+    a.ks = static_cast<const unsigned char *>(k_scale);
+    a.vs = static_cast<const unsigned char *>(v_scale);
     a.o = o;
     a.lse = lse;
     a.kv_lens = kv_lens;
@@ -1142,10 +1327,12 @@ extern "C" ta_status paged_attn_fwd(const void *q, const void *k_cache, const vo
         b.row_o = part(p.pre_row_o);
         b.row_lse = part(p.pre_row_lse);
         b.slots = p.pre_slots;
-        err = launch_pass<true>(head_dim, p.pre_rb, score, s, b);
+        err = q8 ? launch_pass<true, true>(head_dim, p.pre_rb, score, s, b)
+                 : launch_pass<true, false>(head_dim, p.pre_rb, score, s, b);
     }
     if (err == hipSuccess)
-        err = launch_pass<false>(head_dim, p.own_rb, score, s, a);
+        err = q8 ? launch_pass<false, true>(head_dim, p.own_rb, score, s, a)
+                 : launch_pass<false, false>(head_dim, p.own_rb, score, s, a);
     if (err == hipSuccess) {
         JoinArgs j{};
         j.o = o;
@@ -1164,11 +1351,13 @@ extern "C" ta_status paged_attn_fwd(const void *q, const void *k_cache, const vo
         j.pre_row_lse = part(p.pre_row_lse);
         j.prefix_len = prefix_len;
         j.pre_rows = 32 * p.pre_rb;
-        const int step = p.pre_rb == 4 ? PagedShape<128, 4>::STEP : PagedShape<128, 1>::STEP;
+        // (steps are as long for either form of the cache and head_dim)
+        const int step =
+            p.pre_rb == 4 ? PagedShape<128, 4, false>::STEP : PagedShape<128, 1, false>::STEP;
         j.pre_steps = (prefix_len + step - 1) / step;
         j.pre_share =
-            (int32_t)std::max<int64_t>(p.pre_rb == 4 ? PagedShape<128, 4>::LEAST
-                                                     : PagedShape<128, 1>::LEAST,
+            (int32_t)std::max<int64_t>(p.pre_rb == 4 ? PagedShape<128, 4, false>::LEAST
+                                                     : PagedShape<128, 1, false>::LEAST,
                                        (pre_tiles * j.pre_steps + p.pre_slots - 1) / p.pre_slots);
         j.slopes = slopes;
         j.total_tokens = (int32_t)total_tokens;
@@ -1186,4 +1375,53 @@ extern "C" ta_status paged_attn_fwd(const void *q, const void *k_cache, const vo
     if (err != hipSuccess)
         return fail(TA_ERR_HIP, "%s: %s", fn, hipGetErrorString(err));
     return TA_OK;
+}
+
+}  // namespace
+}  // namespace triattn
+
+using namespace triattn;
+
+extern "C" size_t ta_paged_workspace_bytes(int32_t batch, int64_t total_tokens, int32_t ragged,
+                                           int32_t prefix, int32_t hq, int32_t hkv,
+                                           int32_t head_dim)
+{
+    return workspace_bytes_of(batch, total_tokens, ragged, prefix, hq, hkv, head_dim, false);
+}
+
+extern "C" size_t ta_paged_q8_workspace_bytes(int32_t batch, int64_t total_tokens, int32_t ragged,
+                                              int32_t prefix, int32_t hq, int32_t hkv,
+                                              int32_t head_dim)
+{
+    return workspace_bytes_of(batch, total_tokens, ragged, prefix, hq, hkv, head_dim, true);
+}
+
+extern "C" ta_status paged_attn_fwd(const void *q, const void *k_cache, const void *v_cache,
+                                    void *o, int32_t o_dtype, float *lse, const int32_t *kv_lens,
+                                    const int32_t *cu_q, const int32_t *block_table, int32_t batch,
+                                    int32_t table_width, const int32_t *prefix_pages,
+                                    int32_t prefix_len, int64_t total_tokens, int32_t hq,
+                                    int32_t hkv, int32_t head_dim, int64_t num_pages,
+                                    int32_t page_size, float softmax_scale, float softcap,
+                                    const float *slopes, void *workspace, size_t workspace_bytes,
+                                    void *stream)
+{
+    return paged_attn("paged_attn_fwd", false, q, k_cache, nullptr, v_cache, nullptr, o, o_dtype,
+                      lse, kv_lens, cu_q, block_table, batch, table_width, prefix_pages, prefix_len,
+                      total_tokens, hq, hkv, head_dim, num_pages, page_size, softmax_scale,
+                      softcap, slopes, workspace, workspace_bytes, stream);
+}
+
+extern "C" ta_status paged_attn_fwd_q8(
+    const void *q, const void *k_cache, const void *k_scale, const void *v_cache,
+    const void *v_scale, void *o, int32_t o_dtype, float *lse, const int32_t *kv_lens,
+    const int32_t *cu_q, const int32_t *block_table, int32_t batch, int32_t table_width,
+    const int32_t *prefix_pages, int32_t prefix_len, int64_t total_tokens, int32_t hq, int32_t hkv,
+    int32_t head_dim, int64_t num_pages, int32_t page_size, float softmax_scale, float softcap,
+    const float *slopes, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return paged_attn("paged_attn_fwd_q8", true, q, k_cache, k_scale, v_cache, v_scale, o, o_dtype,
+                      lse, kv_lens, cu_q, block_table, batch, table_width, prefix_pages, prefix_len,
+                      total_tokens, hq, hkv, head_dim, num_pages, page_size, softmax_scale,
+                      softcap, slopes, workspace, workspace_bytes, stream);
 }

@@ -239,10 +239,13 @@ struct RowBlock {
     // Otherwise (also when no reference is set yet: the sum is then infinite
     // or NaN) the row maxima are taken and the accumulators rescaled.
     // dist0 = first key of the tile - the key that this lane's row counts
-    // distances from; fresh: the first step, which has no reference on any lane.
+    // distances from; fresh: the first step, which has no reference on any lane;
+    // weight(kb, v, p): what stands for the probability of register v's key in the
+    // PV product (the sums take the probability itself).
+    template <typename F>
     __device__ __forceinline__ void softmax(const f32x16 (&s)[NKB], const ScoreArgs &a,
                                             float slope_log2, int dist0, bf16x8 (&pf)[NKB][2],
-                                            bool fresh)
+                                            bool fresh, F &&weight)
     {
         const float f = factor(a);
         // distances below 2^24 are exact in fp32
@@ -271,6 +274,8 @@ struct RowBlock {
                         t[1] = __builtin_amdgcn_exp2f(score(kb, 8 * s2 + e + 1, b));
                         sum = (kb | s2 | e) ? sum + t[0] : t[0];
                         sum += t[1];
+                        t[0] = weight(kb, 8 * s2 + e, t[0]);
+                        t[1] = weight(kb, 8 * s2 + e + 1, t[1]);
                         packed[e / 2] = __builtin_bit_cast(
                             uint32_t, __builtin_convertvector(t, bf16x2r));
                     }
@@ -305,6 +310,12 @@ struct RowBlock {
             sum = exps(m_use);
         }
         l_run += sum;
+    }
+    __device__ __forceinline__ void softmax(const f32x16 (&s)[NKB], const ScoreArgs &a,
+                                            float slope_log2, int dist0, bf16x8 (&pf)[NKB][2],
+                                            bool fresh)
+    {
+        softmax(s, a, slope_log2, dist0, pf, fresh, [](int, int, float p) { return p; });
     }
 
     __device__ __forceinline__ bf16x8 v_fragment(const unsigned char *vt, int kb, int s2,
@@ -358,32 +369,40 @@ struct RowBlock {
         return __builtin_amdgcn_ballot_w64((carry & 0x80008000u) != 0) != 0;
     }
 
-    // accumulate() key by key, each only to the rows that keep it (whose score
-    // x of it, as the mask left it, is not -inf).
+    // What stands in pf for this lane's row at key j of a tile, and whether the row
+    // keeps that key (whose score x, as the mask left it, is then not -inf).
+    __device__ __forceinline__ bool weight_of_key(int j, const f32x16 (&x)[NKB],
+                                                  const bf16x8 (&pf)[NKB][2], float &p) const
+    {
+        typedef uint16_t u16x8r __attribute__((ext_vector_type(8)));
+        // key j: block j / 32, element (j / 16 & 1, j & 7) of half j / 8 & 1
+        float mine = 0.f, kept = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+            for (int s2 = 0; s2 < 2; ++s2) {
+                const u16x8r pb = __builtin_bit_cast(u16x8r, pf[kb][s2]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const bool on = kb * 32 + s2 * 16 + 8 * half + e == j;
+                    mine = on ? __uint_as_float((uint32_t)pb[e] << 16) : mine;
+                    kept = on && x[kb][8 * s2 + e] != -INFINITY ? 1.f : kept;
+                }
+            }
+        p = rows_pair_sum(mine);
+        return rows_pair_sum(kept) != 0.f;
+    }
+
+    // accumulate() key by key, each only to the rows that keep it.
     __device__ __forceinline__ void accumulate_by_key(const unsigned char *vt,
                                                       const f32x16 (&x)[NKB],
                                                       const bf16x8 (&pf)[NKB][2])
     {
-        typedef uint16_t u16x8r __attribute__((ext_vector_type(8)));
         typedef uint16_t u16x4r __attribute__((ext_vector_type(4)));
 #pragma unroll 1
         for (int j = 0; j < NKB * 32; ++j) {
-            // key j: block j / 32, element (j / 16 & 1, j & 7) of half j / 8 & 1
-            float mine = 0.f, kept = 0.f;
-#pragma unroll
-            for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-                for (int s2 = 0; s2 < 2; ++s2) {
-                    const u16x8r pb = __builtin_bit_cast(u16x8r, pf[kb][s2]);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const bool on = kb * 32 + s2 * 16 + 8 * half + e == j;
-                        mine = on ? __uint_as_float((uint32_t)pb[e] << 16) : mine;
-                        kept = on && x[kb][8 * s2 + e] != -INFINITY ? 1.f : kept;
-                    }
-                }
-            const float p = rows_pair_sum(mine);
-            const bool keeps = rows_pair_sum(kept) != 0.f;
+            float p;
+            const bool keeps = weight_of_key(j, x, pf, p);
             const unsigned char *row = vt + j * ROW_BYTES;
 #pragma unroll
             for (int b = 0; b < D_BLOCKS; ++b)
