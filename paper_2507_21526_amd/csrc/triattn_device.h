@@ -53,6 +53,16 @@ __device__ __forceinline__ void copy_to_lds16(const void *gbase, uint32_t lane_b
                  : "v"(lane_byte_off), "s"(gbase), "{m0}"(lds_addr));
 }
 
+// The same with an address of each lane's own.
+__device__ __forceinline__ void copy_to_lds16_at(const void *from, uint32_t lds_addr)
+{
+    asm volatile("s_nop 0\n\t"
+                 "global_load_lds_dwordx4 %0, off"
+                 :
+                 : "v"(from), "{m0}"(lds_addr)
+                 : "memory");
+}
+
 // The same with four bytes a lane and an address of each lane's own.
 __device__ __forceinline__ void copy_to_lds4(const void *from, uint32_t lds_addr)
 {

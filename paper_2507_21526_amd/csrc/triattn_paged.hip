@@ -62,6 +62,7 @@ struct PagedArgs {
     int32_t slots;      // shares a kv head
     int32_t max_tiles;  // row tiles that the call counts on at most
     int32_t n_records;
+    int32_t by_tile;  // whether a record belongs to each row tile, not to each share
     int32_t o_f32;
 };
 
@@ -77,27 +78,31 @@ struct PagedArgs {
 //   RB = 4: four waves of 32 rows each over the same 64-key tiles, in two stages.
 template <int D, int RB, bool Q8>
 struct PagedShape {
-    static constexpr int NKB = RB == 4 ? 2 : 1;
+    static constexpr bool TILES8 = Q8 && RB == 1;  // tiles in LDS hold 8 bits too
+    static constexpr int NKB = RB == 4 || TILES8 ? 2 : 1;
     static constexpr int TK = 32 * NKB;      // keys of a tile
     static constexpr int KS = RB == 4 ? 1 : 2;  // key splits of a workgroup
     static constexpr int THREADS = 64 * RB * KS;
     static constexpr int STEP = TK * KS;     // keys of a step
     static constexpr int ROWS = 32 * RB;
-    static constexpr bool TILES8 = Q8 && RB == 1;  // tiles in LDS hold 8 bits too
     static constexpr int TILE_BYTES = TK * (TILES8 ? D : 2 * D);
     // K tile, V tile, and of 8-bit tiles the scales: the bytes as they come (K's,
     // V's), then V's as fp32
-    static constexpr int STAGE_BYTES = 2 * TILE_BYTES + (TILES8 ? 256 : 0);
-    static constexpr int STAGES = TILES8 && D == 64 ? 4 : 2;
+    static constexpr int STAGE_BYTES = 2 * TILE_BYTES + (TILES8 ? 512 : 0);
+    static constexpr int STAGES = 2;
     static constexpr int BUFFER_BYTES = STAGES * STAGE_BYTES;  // of a wave (RB = 1)
-    static constexpr int LDS_BYTES = KS * BUFFER_BYTES;
+    static constexpr int Q_BYTES = TILES8 ? ROWS * 2 * D : 0;  // the next piece's query rows
+    static constexpr int LDS_BYTES = KS * BUFFER_BYTES + Q_BYTES;
+    // What a row tile costs a share beside its steps, in steps (8-bit tiles): us of
+    // 96 requests of 150 to 15000 keys (32 heads over 8, d = 128) CHARGE_FIGURES
+    static constexpr int CHARGE = TILES8 ? 2 : 0;
     // Least steps of a share: one of a 128-row tile leaves partials of twice
     // its K and V tiles' bytes.  us with 1, 4 and 8 steps (32 heads over 8, d =
     // 128): the last 64 tokens of 2000 27, 25, 29, of four times 1000 29, 25, 28,
     // 128 single tokens behind a prefix of 2048 47, 43, 44, the last 100 tokens of
     // 500 17, 24, 29; from 3000 keys on the same.
     static constexpr int LEAST = RB == 4 ? 4 : 1;
-    static constexpr int WGS_PER_CU = RB == 1 && (D == 64 || Q8) ? 4 : 2;
+    static constexpr int WGS_PER_CU = RB == 1 && D == 64 ? 4 : 2;
     static constexpr int WAVES_PER_SIMD = (WGS_PER_CU * THREADS / 64 + 3) / 4;
 };
 
@@ -181,7 +186,8 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
     int32_t *const s_kv = s_step + a.max_tiles + 1;   // own keys of a request
     int32_t *const s_req = s_kv + a.batch;            // first row tile of a request, and all
     int32_t *const s_cu = s_req + a.batch + 1;        // query offsets
-    __shared__ int32_t s_page[kPageEntries];
+    __shared__ int32_t s_page[S::TILES8 ? 1 : kPageEntries];
+    __shared__ int32_t s_end[S::KS][3];  // of a wave's piece: bad key, odd values, free stage
     __shared__ int32_t s_wave[kThreads / 64];
     __shared__ float s_ml[S::KS][32][2];
     __shared__ int32_t s_bad;      // query offsets that are none
@@ -270,7 +276,8 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
         block_scan<kThreads>(n_tiles, s_step, s_wave, [&](int t) TA_INLINE -> int32_t {
             if (!a.cu_q)
                 s_kv[t] = a.kv_lens[t];
-            return (tile_of(t).limit + S::STEP - 1) / S::STEP;
+            const int steps = (tile_of(t).limit + S::STEP - 1) / S::STEP;
+            return steps > 0 ? steps + S::CHARGE : 0;
         });
         total = uni(s_step[n_tiles]);
     }
@@ -286,15 +293,18 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
                 return;
             }
             const RowTile r = tile_of(t);
+            // one share's row tile needs no join, unless a prefix's rows do
+            const bool cut =
+                (s_step[t] + S::CHARGE) / share != (s_step[t + 1] - 1) / share;
             m[RF_Q0] = r.q0;
             m[RF_RHO0] = r.rho0;
-            m[RF_ROWS] = r.rows;
+            m[RF_ROWS] = cut || a.row_o ? r.rows : 0;
             m[RF_POS0] = r.pos0;
             m[RF_BEGIN] = s_step[t];
             m[RF_END] = s_step[t + 1];
             m[RF_SHARE] = share;
         };
-        if (g == 0 && a.row_o) {
+        if (g == 0 && a.by_tile) {
             for (int i = slot * kThreads + tid; i < a.n_records; i += a.slots * kThreads)
                 record(i, i);
         } else if (g == 0 && tid == 0) {
@@ -355,6 +365,485 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
     std::conditional_t<S::TILES8, RowBlock8<D, S::NKB, SCORE>, RowBlock<D, S::NKB, SCORE>> rb;
     rb.init(lane);
 
+    if constexpr (S::TILES8) {
+        // One stream of tiles through all pieces of the share: a wave's copies run
+        // STAGES tiles ahead of its products, into the next piece too, so that the
+        // latencies of page ids (which scalar loads bring a tile ahead of the
+        // copies), query rows and first tiles are not paid anew at every request.
+        constexpr bool BACK = (SCORE & kScoreSlope) != 0;  // last keys first, see below
+        constexpr int V_COPIES = GROUPS * COPIES, K_COPIES = V_COPIES + 1;  // K's: scales too
+        constexpr int Q_COPIES = S::Q_BYTES / 1024 / S::KS;  // of a wave
+        constexpr int HALF = D_BLOCKS / 2;
+        const uint32_t q_lds = smem_addr + S::KS * S::BUFFER_BYTES;
+        typedef const __attribute__((address_space(4))) int32_t *ids_ptr;
+
+        struct Piece {
+            RowTile rt;
+            int tile;          // which row tile
+            int begin, cost;   // of it, in the shares' units
+            int step0, step1;  // of the row tile
+            int base, n;       // this wave's tiles: first key of the first one, how many
+            int slot;          // of the partials; -1: the whole row tile
+        };
+        // the first piece from `at` on; n_tiles' end: none
+        auto open = [&](int at, int t, Piece &p) TA_INLINE -> bool {
+            for (;;) {
+                if (at >= share1)
+                    return false;
+                if constexpr (PREFIX) {
+                    t = at / prefix_steps;
+                    p.begin = t * prefix_steps;
+                    p.cost = prefix_steps;
+                } else {
+                    if (t < 0)
+                        t = find_start(s_step, n_tiles, at);
+                    else
+                        do
+                            ++t;
+                        while (s_step[t + 1] <= at);
+                    t = uni(t);
+                    p.begin = uni(s_step[t]);
+                    p.cost = uni(s_step[t + 1]) - p.begin;
+                }
+                constexpr int C = PREFIX ? 0 : S::CHARGE;
+                p.step0 = max(0, at - p.begin - C);
+                p.step1 = min(share1, p.begin + p.cost) - p.begin - C;
+                if (p.step1 > p.step0)
+                    break;
+                at = p.begin + p.cost;  // the share ends within the row tile's charge
+                if (at < share1)
+                    continue;
+                return false;
+            }
+            p.rt = tile_of(t);
+            p.rt.q0 = uni(p.rt.q0);
+            p.rt.rho0 = uni(p.rt.rho0);
+            p.rt.rows = uni(p.rt.rows);
+            p.rt.pos0 = uni(p.rt.pos0);
+            p.rt.limit = uni(p.rt.limit);
+            p.rt.req = uni(p.rt.req);
+            p.tile = t;
+            p.base = p.step0 * S::STEP + wave * S::TK;
+            const int end = min(p.step1 * S::STEP, p.rt.limit);
+            p.n = p.base < end ? (end - p.base + S::STEP - 1) / S::STEP : 0;
+            p.slot = p.step0 == 0 && p.step1 == p.cost - (PREFIX ? 0 : S::CHARGE)
+                         ? -1
+                         : 2 * slot + (p.begin > share0 ? 1 : 0);
+            return true;
+        };
+        auto after = [&](const Piece &p, Piece &q) TA_INLINE -> bool {
+            return open(p.begin + p.cost, p.tile, q);
+        };
+        auto key_of = [&](int base, int n, int i) TA_INLINE -> int {
+            return base + (BACK ? n - 1 - i : i) * S::STEP;
+        };
+        auto pages_of = [&](const Piece &p) TA_INLINE -> ids_ptr {
+            return (ids_ptr)(uintptr_t)(PREFIX ? a.prefix_pages
+                                               : a.table + (int64_t)p.rt.req * a.width);
+        };
+
+        // The tile that is copied next: its first key, and the pages of its two
+        // groups of keys (on their way).
+        struct Next {
+            int key, id[GROUPS];
+        };
+        auto find_ids = [&](ids_ptr ids, int limit, int key0, Next &x) TA_INLINE {
+            x.key = key0;
+#pragma unroll
+            for (int i = 0; i < GROUPS; ++i)
+                x.id[i] = ids[min(key0 + i * GROUP, limit - 1) >> a.page_log2];
+        };
+        // Page ids that are none become 0; returns the first key of such a page.
+        auto check_ids = [&](int limit, Next &x) TA_INLINE -> int {
+            int bad = INT32_MAX;
+#pragma unroll
+            for (int i = 0; i < GROUPS; ++i)
+                if ((uint32_t)x.id[i] >= (uint32_t)a.num_pages) {
+                    x.id[i] = 0;
+                    bad = min(bad, min(x.key + i * GROUP, limit - 1) & ~page_mask);
+                }
+            return bad;
+        };
+        // Copies a tile's K rows and scales, or its V rows, into a stage.  Keys from
+        // rt.limit on repeat the last one before it; they lie past every row's last
+        // key.
+        auto copy_part = [&](int limit, const Next &x, int stage, auto is_v) TA_INLINE {
+            constexpr bool V = decltype(is_v)::value;
+            const uint32_t lds = smem_addr + wave_lds + stage * S::STAGE_BYTES;
+            const bool inside = x.key + S::TK <= limit;
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int i = 0; i < GROUPS; ++i) {
+                const int key = x.key + i * GROUP;
+                const unsigned char *page =
+                    (V ? vc : kc) + (int64_t)uni(x.id[i]) * page_stride;
+                const uint32_t to = lds + (V ? S::TILE_BYTES : 0) + i * GROUP * D;
+                if (inside) {
+                    const unsigned char *from = page + (key & page_mask) * D;
+                    if constexpr (COPIES == 1) {
+                        copy_to_lds16(from, dma_k, to);
+                    } else {
+                        const uint32_t off[2] = {dma_k, dma_k};
+                        copy_burst_to_lds16<2>(from, off, to);
+                    }
+                } else {
+#pragma unroll
+                    for (int m = 0; m < COPIES; ++m) {
+                        const int first = min(key + m * COPY_ROWS, limit - 1);
+                        const int lim = limit - 1 - first;  // rows after the first
+                        copy_to_lds16(page + (first & page_mask) * D,
+                                      dma_k - (uint32_t)(max(dma_row - lim, 0) * D),
+                                      to + m * 1024);
+                    }
+                }
+            }
+            // The scales: lane i copies four bytes, of K's keys or of V's (lanes
+            // past them repeat the same).
+            if constexpr (!V) {
+                constexpr int PER = S::TK / 4;  // lanes of K's keys
+                // (keys from the limit on: bytes of the last ones, not used)
+                const int key = min(x.key + 4 * (lane & (PER - 1)), (limit - 1) & ~3);
+                int mine = x.id[0];
+#pragma unroll
+                for (int i = 1; i < GROUPS; ++i)
+                    mine = key >= x.key + i * GROUP ? x.id[i] : mine;
+                copy_to_lds4(scale_at(lane & PER ? a.vs : a.ks, mine, key & page_mask),
+                             lds + 2 * S::TILE_BYTES);
+            }
+            asm volatile("" ::: "memory");
+        };
+        using K = std::false_type;
+        using V = std::true_type;
+        // This wave's half of the copies of a piece's query rows (rows past the
+        // tile repeat its last one), 16-byte chunks permuted by the row.
+        constexpr int Q_CHUNKS = D / 8, Q_ROWS = 64 / Q_CHUNKS;  // of a 1 KB copy
+        auto copy_q = [&](const Piece &p) TA_INLINE {
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int m = 0; m < Q_COPIES; ++m) {
+                const int r = (wave * Q_COPIES + m) * Q_ROWS + lane / Q_CHUNKS;
+                const int rho = p.rt.rho0 + min(r, p.rt.rows - 1), tq = div_group(rho);
+                const int head = g * a.group + rho - tq * a.group;
+                copy_to_lds16_at(a.q + ((int64_t)(p.rt.q0 + tq) * a.hq + head) * D +
+                                     8 * ((lane % Q_CHUNKS) ^ (r & (Q_CHUNKS - 1))),
+                                 q_lds + (wave * Q_COPIES + m) * 1024);
+            }
+            asm volatile("" ::: "memory");
+        };
+        auto read_q = [&]() TA_INLINE {
+            const unsigned char *row = smem + S::KS * S::BUFFER_BYTES + rb.col * 2 * D;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+                rb.qf[i] = *reinterpret_cast<const bf16x8 *>(
+                    row + (((4 * (i >> 1) + 2 * rb.half + (i & 1)) ^ (rb.col & (Q_CHUNKS - 1)))
+                           << 4));
+        };
+
+        Piece cur, nxt;
+        if (!open(share0, -1, cur))
+            return;
+        bool ahead = false;  // the copies are in nxt, not in cur
+        bool q_due = false;  // nxt's query rows are not on their way yet
+        bool has = false;    // there is a next tile, nt
+        int made = 0;        // tiles of the piece being copied that nt has come to
+        int flying = 0;      // tiles whose copies have begun, not yet multiplied
+        int in_stage = 0, out_stage = 0;
+        int bad_cur = INT32_MAX, bad_nxt = INT32_MAX;
+        Next nt;
+        // of the piece being copied
+        int src_base = cur.base, src_n = cur.n, src_limit = cur.rt.limit;
+        ids_ptr src_pages = pages_of(cur);
+        auto advance = [&]() TA_INLINE {
+            has = false;
+            if (made == src_n) {
+                // at most one piece ahead: there is room for the rows of one
+                if (ahead || !after(cur, nxt))
+                    return;
+                ahead = q_due = true;
+                made = 0;
+                src_base = nxt.base;
+                src_n = nxt.n;
+                src_limit = nxt.rt.limit;
+                src_pages = pages_of(nxt);
+                if (src_n == 0)
+                    return;
+            }
+            find_ids(src_pages, src_limit, key_of(src_base, src_n, made), nt);
+            ++made;
+            has = true;
+        };
+        auto send_q = [&]() TA_INLINE {
+            if (q_due)
+                copy_q(nxt);
+            q_due = false;
+        };
+        // The copies of the next tile: K's where the stage's K has been multiplied,
+        // V's where its V has.
+        auto produce_k = [&]() TA_INLINE {
+            send_q();
+            if (!has)
+                return;
+            const int bad = check_ids(src_limit, nt);
+            bad_nxt = ahead ? min(bad_nxt, bad) : bad_nxt;
+            bad_cur = ahead ? bad_cur : min(bad_cur, bad);
+            copy_part(src_limit, nt, in_stage, K{});
+        };
+        auto produce_v = [&]() TA_INLINE {
+            if (!has)
+                return;
+            copy_part(src_limit, nt, in_stage, V{});
+            in_stage = in_stage + 1 == S::STAGES ? 0 : in_stage + 1;
+            ++flying;
+            advance();
+        };
+        // until the K, and what was sent before it, of the oldest tile has come; its
+        // V (behind it the next tile, and K of the one after where `more`)
+        static_assert(S::STAGES == 2, "what may be behind a tile");
+        auto wait_k = [&]() TA_INLINE {
+            if (flying >= 2)
+                rows_wait_copies<2 * V_COPIES + K_COPIES>();
+            else if (flying == 1)
+                rows_wait_copies<V_COPIES>();
+            else
+                rows_wait_copies<0>();
+        };
+        auto wait_v = [&](bool more) TA_INLINE {
+            if (flying >= 2 && more)
+                rows_wait_copies<V_COPIES + 2 * K_COPIES>();
+            else if (flying >= 2)
+                rows_wait_copies<V_COPIES + K_COPIES>();
+            else
+                rows_wait_copies<0>();
+        };
+        copy_q(cur);
+        advance();
+        while (has && !ahead && flying < S::STAGES) {
+            produce_k();
+            produce_v();
+        }
+        wait_k();
+        barrier_no_fence();
+        read_q();
+        barrier_no_fence();  // its place is free
+
+        for (;;) {
+            while (has && flying < S::STAGES) {
+                produce_k();
+                produce_v();
+            }
+            // this lane's query row (rows past the tile repeat its last one)
+            const RowTile rt = cur.rt;
+            const int rho = rt.rho0 + min(rb.col, rt.rows - 1);
+            const int tq = div_group(rho);
+            const int head = g * a.group + rho - tq * a.group;
+            float slope = 0.f;
+            if constexpr ((SCORE & kScoreSlope) != 0)
+                slope = a.score.slopes[head] * kRowsLog2e;
+            // as in the other forms: the last key that this row keeps, and the
+            // first row's; and where distances are taken from
+            const int last = PREFIX ? a.prefix_len - 1 : rt.pos0 + tq;
+            const int first_last = PREFIX ? a.prefix_len - 1 : rt.pos0 + div_group(rt.rho0);
+            int dist_row = PREFIX ? a.prefix_len : last;
+            if constexpr ((SCORE & kScoreSlope) != 0)
+                if (slope < 0.f)
+                    dist_row = PREFIX ? 0 : -a.prefix_len;
+            bool fresh = true, odd = false;
+            bool refilled = false;  // K of the tile after the next is on its way
+            rb.reset();
+            // between(): after the products with K
+            auto tile = [&](int key0, unsigned char *kt, auto careful, auto &&between)
+                            TA_INLINE {
+                constexpr bool CAREFUL = decltype(careful)::value;
+                // K's scale of this lane's key; V's as fp32 for the weights, 0 for
+                // a key that no row keeps
+                static_assert(S::TK == 64, "a key a lane");
+                unsigned char *raw = kt + 2 * S::TILE_BYTES;
+                float kscale[S::NKB];
+#pragma unroll
+                for (int kb = 0; kb < S::NKB; ++kb)
+                    kscale[kb] = q8_scale_bits(raw[kb * 32 + rows_perm(rb.col)]);
+                const uint32_t byte = raw[S::TK + lane];
+                const bool on = key0 + lane < rt.limit;
+                float *vscale = reinterpret_cast<float *>(raw + 256);
+                vscale[lane] = on ? q8_scale(byte) : 0.f;
+                f32x16 s[S::NKB];
+                bf16x8 p[S::NKB][2];
+                rb.products8(kt, kscale, s);
+                between();
+                rb.modify(s, a.score);
+                const bool masked = key0 + S::TK - 1 > first_last;
+                if (__builtin_expect(masked, 0)) {
+                    asm volatile("");  // a branch: most tiles have no mask
+                    rb.mask_above(s, last - key0);
+                }
+                f32x4r w[S::NKB][4];  // V's scales of this lane's keys (rows_key_of_reg)
+#pragma unroll
+                for (int kb = 0; kb < S::NKB; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        w[kb][i] = *reinterpret_cast<const f32x4r *>(
+                            vscale + 32 * kb + 16 * (i >> 1) + 8 * rb.half + 4 * (i & 1));
+                rb.softmax(s, a.score, slope, key0 - dist_row, p, fresh,
+                           [&](int kb, int v, float x)
+                               TA_INLINE { return x * w[kb][v / 4][v % 4]; });
+                fresh = false;
+                if constexpr (CAREFUL) {
+                    rb.accumulate8_by_key(kt + S::TILE_BYTES, s, p);
+                } else {
+                    wait_v(refilled);
+                    if (__builtin_expect(masked, 0)) {
+                        asm volatile("");
+                        odd |= __builtin_amdgcn_ballot_w64(on && byte == 255) != 0 ||
+                               rb.odd_elements(kt + S::TILE_BYTES, lane);
+                    }
+                    rb.accumulate8(kt + S::TILE_BYTES, p);
+                }
+            };
+            for (int i = 0; i < cur.n; ++i) {
+                wait_k();
+                // every read of a stage has returned before it is written again;
+                // the last tile's stage joins the waves first
+                refilled = i + 1 < cur.n && has;
+                tile(key_of(cur.base, cur.n, i), smem + wave_lds + out_stage * S::STAGE_BYTES,
+                     std::false_type{}, [&]() TA_INLINE {
+                         if (i + 1 < cur.n) {
+                             __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+                             produce_k();
+                         }
+                     });
+                out_stage = out_stage + 1 == S::STAGES ? 0 : out_stage + 1;
+                --flying;
+                if (i + 1 < cur.n) {
+                    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+                    produce_v();
+                }
+            }
+            const int free_stage = (out_stage + S::STAGES - 1) % S::STAGES;
+            unsigned char *const scratch = smem + wave_lds + free_stage * S::STAGE_BYTES;
+
+            // The waves join, each finishing half of the d blocks: it leaves the
+            // other half of its sums in its free stage.
+            static_assert(HALF * 4096 <= S::STAGE_BYTES, "half of the sums fit a stage");
+            float own_l = 0.f;
+            auto leave = [&](int odd_values) TA_INLINE {
+                own_l = rows_pair_sum(rb.l_run);
+                if (rb.half == 0) {
+                    s_ml[wave][rb.col][0] = rb.m_ref;
+                    s_ml[wave][rb.col][1] = own_l;
+                }
+                if (lane == 0) {
+                    s_end[wave][0] = bad_cur;
+                    s_end[wave][1] = odd_values;
+                    s_end[wave][2] = free_stage;
+                }
+                if (cur.n == 0)
+                    return;
+#pragma unroll
+                for (int b = 0; b < HALF; ++b)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        f32x4r x;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            x[e] = wave ? rb.oacc[b][4 * c + e] : rb.oacc[HALF + b][4 * c + e];
+                        *reinterpret_cast<f32x4r *>(scratch + ((b * 4 + c) * 64 + lane) * 16) = x;
+                    }
+            };
+            leave(odd);
+            if (!ahead && !has)
+                advance();
+            send_q();
+            wait_k();  // nxt's first keys, and its query rows before them
+            barrier_no_fence();
+            if (__builtin_expect(s_end[0][1] | s_end[1][1], 0)) {
+                // a masked tile holds NaN values: the piece again, tile by tile in
+                // the free stage, each key only to the rows that keep it
+                barrier_no_fence();
+                fresh = true;
+                rb.reset();
+                for (int i = 0; i < cur.n; ++i) {
+                    Next x;
+                    find_ids(pages_of(cur), rt.limit, key_of(cur.base, cur.n, i), x);
+                    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+                    check_ids(rt.limit, x);
+                    copy_part(rt.limit, x, free_stage, K{});
+                    copy_part(rt.limit, x, free_stage, V{});
+                    rows_wait_copies<0>();
+                    tile(x.key, scratch, std::true_type{}, []() {});
+                }
+                leave(0);
+                barrier_no_fence();
+            }
+            const int bad_key = min(s_end[0][0], s_end[1][0]);
+            const float m0 = s_ml[0][rb.col][0], m1 = s_ml[1][rb.col][0];
+            const float m = fmaxf(m0, m1), m_use = m == -INFINITY ? 0.f : m;
+            const float f0 = __builtin_amdgcn_exp2f(m0 - m_use);
+            const float f1 = __builtin_amdgcn_exp2f(m1 - m_use);
+            const float den = f0 * s_ml[0][rb.col][1] + f1 * s_ml[1][rb.col][1];
+            // NaN from the first page that is none on (earlier rows of the tile do
+            // not keep its keys)
+            const float nan = last >= bad_key ? __builtin_nanf("") : 0.f;
+            const float inv = (den == 0.f ? 0.f : 1.f / den) + nan;
+            const bool to_o = cur.slot < 0 && !a.row_o;
+            const int64_t orow = (int64_t)(rt.q0 + tq) * a.hq + head;
+            const int64_t srow = ((int64_t)cur.slot * a.hkv + g) * S::ROWS + rb.col;
+            const unsigned char *theirs = smem + (1 - wave) * S::BUFFER_BYTES +
+                                          s_end[1 - wave][2] * S::STAGE_BYTES;
+            // (sums that the other wave left nowhere, having no tile, are zero)
+            const bool other = (wave ? m0 : m1) != -INFINITY;
+            if (rb.col < rt.rows) {
+#pragma unroll
+                for (int b = 0; b < HALF; ++b)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        f32x4r x{};
+                        if (other)
+                            x = *reinterpret_cast<const f32x4r *>(theirs +
+                                                                  ((b * 4 + c) * 64 + lane) * 16);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float mine =
+                                wave ? rb.oacc[HALF + b][4 * c + e] : rb.oacc[b][4 * c + e];
+                            x[e] = (f0 * (wave ? x[e] : mine) + f1 * (wave ? mine : x[e])) * inv;
+                        }
+                        const int d0 = 32 * (wave * HALF + b) + 8 * c + 4 * rb.half;
+                        if (to_o && !a.o_f32)
+                            *reinterpret_cast<bf16x4r *>(static_cast<__bf16 *>(a.o) + orow * D +
+                                                         d0) = __builtin_convertvector(x, bf16x4r);
+                        else if (to_o)
+                            *reinterpret_cast<f32x4r *>(static_cast<float *>(a.o) + orow * D +
+                                                        d0) = x;
+                        else
+                            *reinterpret_cast<f32x4r *>(cur.slot < 0 ? a.row_o + orow * D + d0
+                                                                     : a.slot_o + srow * D + d0) =
+                                x;
+                    }
+                if (wave == 0 && rb.half == 0) {
+                    float lse = (den == 0.f ? -INFINITY : (m + __log2f(den)) * kRowsLn2) + nan;
+                    if (to_o) {
+                        if constexpr ((SCORE & kScoreSlope) != 0)
+                            lse += rows_lse_shift(a.score.slopes[head], rt.pos0 + tq);
+                        if (a.lse)
+                            a.lse[(int64_t)head * a.total_tokens + rt.q0 + tq] = lse;
+                    } else if (cur.slot < 0) {
+                        a.row_lse[orow] = lse;
+                    } else {
+                        a.slot_lse[srow] = lse;
+                    }
+                }
+            }
+            if (!ahead)
+                return;
+            cur = nxt;
+            ahead = false;
+            bad_cur = bad_nxt;
+            bad_nxt = INT32_MAX;
+            read_q();
+            barrier_no_fence();  // the free stages and the rows' place are read
+            if (!has)
+                advance();
+        }
+    } else {
     for (int at = share0, t = -1; at < share1;) {
         // the row tile of step `at`
         int t_begin, t_end;
@@ -467,14 +956,9 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
                     uint32_t off[COPIES];
 #pragma unroll
                     for (int m = 0; m < COPIES; ++m)
-                        off[m] = V || Q8 ? dma_v
-                                         : dma_k ^ (uint32_t)(rows_kswz<D>(m * COPY_ROWS) << 4);
+                        off[m] = V ? dma_v : dma_k ^ (uint32_t)(rows_kswz<D>(m * COPY_ROWS) << 4);
                     if (inside) {
-                        if constexpr (COPIES == 1)
-                            copy_to_lds16(page + (key & page_mask) * ROW_BYTES, off[0], to);
-                        else
-                            copy_burst_to_lds16<COPIES>(page + (key & page_mask) * ROW_BYTES, off,
-                                                        to);
+                        copy_burst_to_lds16<COPIES>(page + (key & page_mask) * ROW_BYTES, off, to);
                     } else {
 #pragma unroll
                         for (int m = 0; m < COPIES; ++m) {
@@ -490,51 +974,15 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
             };
             using K = std::false_type;
             using V = std::true_type;
-            // The scales of a tile whose copies begin at key0: lane i copies four
-            // bytes, of K's keys or of V's (lanes past them repeat the same).
-            auto copy_scales = [&](int key0, uint32_t lds) TA_INLINE {
-                constexpr int PER = S::TK / 4;  // lanes of K's keys
-                // (keys from rt.limit on: bytes of the last ones, not used)
-                const int key = min(key0 + 4 * (lane & (PER - 1)), (rt.limit - 1) & ~3);
-                const int id = s_page[(key >> a.page_log2) - page0];
-                copy_to_lds4(scale_at(lane & PER ? a.vs : a.ks, id, key & page_mask),
-                             smem_addr + lds + 2 * S::TILE_BYTES);
-            };
             f32x16 s[S::NKB];
             bf16x8 p[S::NKB][2];
-            // scales of an 8-bit tile: K's of this lane's key, V's in LDS
-            float kscale[S::NKB];
-            bool scale_nan = false;
-            auto scales = [&](int key0, unsigned char *stage) TA_INLINE {
-                const unsigned char *raw = stage + 2 * S::TILE_BYTES;
-                kscale[0] = q8_scale_bits(raw[rows_perm(rb.col)]);
-                const uint32_t b = raw[S::TK + rb.col];
-                // a key that no row keeps weighs 0, not NaN
-                const bool on = key0 + rb.col < rt.limit;
-                scale_nan = __builtin_amdgcn_ballot_w64(on && b == 255) != 0;
-                reinterpret_cast<float *>(stage + 2 * S::TILE_BYTES + 128)[rb.col] =
-                    on ? q8_scale(b) : 0.f;
-            };
-            auto softmax = [&](int key0, const unsigned char *stage) TA_INLINE {
+            auto softmax = [&](int key0) TA_INLINE {
                 rb.modify(s, a.score);
                 if (__builtin_expect(key0 + S::TK - 1 > first_last, 0)) {
                     asm volatile("");  // a branch: most steps have no mask
                     rb.mask_above(s, last - key0);
                 }
-                if constexpr (S::TILES8) {
-                    // V's scales of this lane's keys (rows_key_of_reg)
-                    f32x4r w[4];
-                    const float *vscale =
-                        reinterpret_cast<const float *>(stage + 2 * S::TILE_BYTES + 128);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        w[i] = *reinterpret_cast<const f32x4r *>(vscale + 16 * (i >> 1) +
-                                                                 8 * rb.half + 4 * (i & 1));
-                    rb.softmax(s, a.score, slope, key0 - dist_row, p, fresh,
-                               [&](int, int v, float x) TA_INLINE { return x * w[v / 4][v % 4]; });
-                } else {
-                    rb.softmax(s, a.score, slope, key0 - dist_row, p, fresh);
-                }
+                rb.softmax(s, a.score, slope, key0 - dist_row, p, fresh);
                 fresh = false;
             };
             auto values = [&](int key0, const unsigned char *vt) TA_INLINE {
@@ -542,29 +990,18 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
                 // part of the values each)
                 if (__builtin_expect(key0 + S::TK - 1 > tile_first_last, 0)) {
                     asm volatile("");
-                    if constexpr (S::TILES8)
-                        odd |= scale_nan || rb.odd_elements(vt, lane);
-                    else
-                        odd |= rb.odd_values(vt, lane, RB == 1 ? 0 : wave, RB);
+                    odd |= rb.odd_values(vt, lane, RB == 1 ? 0 : wave, RB);
                 }
-                if constexpr (S::TILES8) {
-                    rb.accumulate8(vt, p);
-                } else {
-                    __builtin_amdgcn_sched_barrier(0);
-                    rb.accumulate(vt, p);
-                    rb.template schedule<false, true>();
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+                __builtin_amdgcn_sched_barrier(0);
+                rb.accumulate(vt, p);
+                rb.template schedule<false, true>();
+                __builtin_amdgcn_sched_barrier(0);
             };
             auto products = [&](const unsigned char *kt) TA_INLINE {
-                if constexpr (S::TILES8) {
-                    rb.products8(kt, kscale, s);
-                } else {
-                    __builtin_amdgcn_sched_barrier(0);
-                    rb.products(kt, s);
-                    rb.template schedule<true, false>();
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+                __builtin_amdgcn_sched_barrier(0);
+                rb.products(kt, s);
+                rb.template schedule<true, false>();
+                __builtin_amdgcn_sched_barrier(0);
             };
             // An 8-bit cache's rows as bf16 tiles (RB = 4): a wave loads a group's
             // rows and scales into registers, and later leaves them in LDS, each
@@ -613,7 +1050,7 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
                     const int key0 = (seg0 + (BACK ? n - 1 - i : i)) * S::STEP +
                                      (RB == 1 ? wave * S::TK : 0);
                     const bool on = key0 < key_end;
-                    if constexpr (Q8 && RB == 4) {
+                    if constexpr (Q8) {
                         load_rows(key0);
 #pragma unroll
                         for (int c = 0; c < 2 * LOADS; ++c)
@@ -621,20 +1058,13 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
                     } else if (on) {
                         copy(key0, wave_lds, K{});
                         copy(key0, wave_lds + S::TILE_BYTES, V{});
-                        if constexpr (Q8)
-                            copy_scales(key0, wave_lds);
                     }
                     rows_wait_copies<0>();
                     barrier_no_fence();
                     if (on) {
-                        if constexpr (S::TILES8)
-                            scales(key0, smem + wave_lds);
                         products(smem + wave_lds);
-                        softmax(key0, smem + wave_lds);
-                        if constexpr (S::TILES8)
-                            rb.accumulate8_by_key(smem + wave_lds + S::TILE_BYTES, s, p);
-                        else
-                            rb.accumulate_by_key(smem + wave_lds + S::TILE_BYTES, s, p);
+                        softmax(key0);
+                        rb.accumulate_by_key(smem + wave_lds + S::TILE_BYTES, s, p);
                     }
                     barrier_no_fence();
                 }
@@ -648,58 +1078,36 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
                 auto copies = [&](int key0, int stage) TA_INLINE {
                     copy(key0, wave_lds + stage * S::STAGE_BYTES, K{});
                     copy(key0, wave_lds + stage * S::STAGE_BYTES + S::TILE_BYTES, V{});
-                    if constexpr (Q8)
-                        copy_scales(key0, wave_lds + stage * S::STAGE_BYTES);
                     __builtin_amdgcn_sched_barrier(0);
                 };
-                constexpr int TILE_COPIES = 2 * GROUPS * COPIES + (Q8 ? 1 : 0);
-#pragma unroll
-                for (int i = 0; i < S::STAGES; ++i)
-                    if (i < n)
-                        copies(key_of(i), i);
+                if (n > 0)
+                    copies(key_of(0), 0);
+                if (n > 1)
+                    copies(key_of(1), 1);
                 auto step = [&](int i, auto stage) TA_INLINE {
                     constexpr int ST = decltype(stage)::value;
-                    unsigned char *kt = smem + wave_lds + ST * S::STAGE_BYTES;
-                    // the tiles behind this one may still be on their way
-                    if (i + S::STAGES - 1 < n)
-                        rows_wait_copies<(S::STAGES - 1) * TILE_COPIES>();
-                    else if (S::STAGES > 2 && i + 1 < n)
-                        rows_wait_copies<TILE_COPIES>();
+                    const unsigned char *kt = smem + wave_lds + ST * S::STAGE_BYTES;
+                    if (i + 1 < n)
+                        rows_wait_copies<2 * GROUPS * COPIES>();
                     else
                         rows_wait_copies<0>();
-                    if constexpr (Q8)
-                        scales(key_of(i), kt);
                     products(kt);
-                    softmax(key_of(i), kt);
+                    softmax(key_of(i));
                     values(key_of(i), kt + S::TILE_BYTES);
-                    if (i + S::STAGES < n) {
+                    if (i + 2 < n) {
                         // every read of the stage has returned before it is
                         // written again
                         __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
-                        copies(key_of(i + S::STAGES), ST);
+                        copies(key_of(i + 2), ST);
                     }
                 };
                 int i = 0;
-                if constexpr (S::STAGES == 4)
-                    for (; i + 3 < n; i += 4) {
-                        step(i, std::integral_constant<int, 0>{});
-                        step(i + 1, std::integral_constant<int, 1>{});
-                        step(i + 2, std::integral_constant<int, 2>{});
-                        step(i + 3, std::integral_constant<int, 3>{});
-                    }
-                else
-                    for (; i + 1 < n; i += 2) {
-                        step(i, std::integral_constant<int, 0>{});
-                        step(i + 1, std::integral_constant<int, 1>{});
-                    }
+                for (; i + 1 < n; i += 2) {
+                    step(i, std::integral_constant<int, 0>{});
+                    step(i + 1, std::integral_constant<int, 1>{});
+                }
                 if (i < n)
                     step(i, std::integral_constant<int, 0>{});
-                if constexpr (S::STAGES == 4) {
-                    if (i + 1 < n)
-                        step(i + 1, std::integral_constant<int, 1>{});
-                    if (i + 2 < n)
-                        step(i + 2, std::integral_constant<int, 2>{});
-                }
             } else if constexpr (Q8) {
                 // As below, but through registers: step i leaves the rows of step
                 // i + 1 in LDS between its matrix instructions, and then loads
@@ -731,7 +1139,7 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
                     __builtin_amdgcn_sched_barrier(0);
                     load_rows(key_of(min(i + 2, n - 1)));
                     __builtin_amdgcn_sched_barrier(0);
-                    softmax(key_of(i), kt);
+                    softmax(key_of(i));
                     values(key_of(i), kt + S::TILE_BYTES);
                 };
                 int i = 0;
@@ -797,7 +1205,7 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
                     const int key0 = now.key0;
                     now = next;
                     next = place(min(i + 2, n - 1));
-                    softmax(key0, kt);
+                    softmax(key0);
                     values(key0, kt + S::TILE_BYTES);
                 };
                 int i = 0;
@@ -931,6 +1339,7 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
         }
         __syncthreads();  // s_bad_key and the accumulators are read
     }
+    }
 }
 
 struct JoinArgs {
@@ -940,6 +1349,8 @@ struct JoinArgs {
     const float *slot_o, *slot_lse;
     int32_t tile_rows;
     int32_t chunks, chunk_rows;  // workgroups of a row tile, rows of each
+    int32_t ways;                // groups of lanes of a row
+    int32_t charge;              // of a row tile beside its steps
     // the prefix pass (prefix_len 0: none)
     const float *row_o, *row_lse;
     const float *pre_slot_o, *pre_slot_lse, *pre_row_o, *pre_row_lse;
@@ -954,13 +1365,18 @@ struct JoinArgs {
 // that a share's start cuts, which the shares name.  Sixteen lanes take a row:
 // what bounds this is the chain of loads (cut, record, log-sum-exps, partials), so
 // many rows at once matter more than wide ones (prompt pieces: 22 us, with a wave
-// to a row 50).
-template <int D>
+// to a row 50).  Where few requests share the chip a row has many partials: WIDE
+// then gives it `ways` groups of sixteen lanes, which take every ways-th partial each
+// and join in LDS (three requests of 128K keys, 43 partials a row: WIDE_FIGURES).
+template <int D, bool WIDE>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(JoinArgs a)
 {
     constexpr int LANES = 16;        // of a row
     constexpr int PER = D / LANES;   // values of a lane, in runs of four
     constexpr int RUNS = PER / 4;
+    constexpr int GROUPS = kJoinThreads / LANES;
+    __shared__ float s_part[WIDE ? GROUPS : 1][WIDE ? D + 4 : 1];
+    const int ways = WIDE ? a.ways : 1;
     const int g = blockIdx.x % a.hkv, at = blockIdx.x / a.hkv;
     const int chunk = at % a.chunks;
     const int32_t *m = a.records + kRecordWords * (at / a.chunks);
@@ -968,13 +1384,19 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(JoinArgs a)
     const int32_t begin = m[RF_BEGIN], end = m[RF_END], share = m[RF_SHARE];
     if (rows == 0)
         return;
-    const int w0 = begin / share;
+    const int w0 = (begin + a.charge) / share;
     const int n_own = (end - 1) / share - w0 + 1;
     const int lane = threadIdx.x % LANES;
     {
-        const int r = chunk * a.chunk_rows + threadIdx.x / LANES;
-        if (threadIdx.x / LANES >= a.chunk_rows || r >= rows)
-            return;
+        const int way = threadIdx.x / LANES % ways;
+        int r = chunk * a.chunk_rows + threadIdx.x / LANES / ways;
+        const bool mine = (int)(threadIdx.x / LANES) < a.chunk_rows * ways && r < rows;
+        if constexpr (!WIDE) {
+            if (!mine)
+                return;
+        } else {
+            r = min(r, rows - 1);  // (lanes past the rows wait for the others)
+        }
         const int rho = rho0 + r, qt = rho / a.group, h = g * a.group + rho - qt * a.group;
         const int64_t orow = (int64_t)(q0 + qt) * a.hq + h;
         // the prefix pass's pieces of this row: its rows are those of all
@@ -990,9 +1412,12 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(JoinArgs a)
             if (a.slopes && a.slopes[h] > 0.f)  // its distances end at the prefix's end
                 shift = -a.slopes[h] * (float)(pos0 + qt);
         }
-        const int n = n_pre + n_own;
+        // this way's partials: way, way + ways, ..
+        const int all = n_pre + n_own;
+        const int n = WIDE ? max(0, all - way + ways - 1) / ways : all;
         // row of partial c: in the whole rows or the pieces of its pass
-        auto index = [&](int c) TA_INLINE -> int64_t {
+        auto index = [&](int i) TA_INLINE -> int64_t {
+            const int c = WIDE ? way + ways * i : i;
             if (c < n_pre) {
                 const int w = pw0 + c;
                 return n_pre == 1 ? orow
@@ -1004,10 +1429,11 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(JoinArgs a)
                               : ((int64_t)(2 * w + (begin > w * share)) * a.hkv + g) *
                                         a.tile_rows + r;
         };
-        auto lse_of = [&](int c) TA_INLINE -> float {
+        auto lse_of = [&](int i) TA_INLINE -> float {
+            const int c = WIDE ? way + ways * i : i;
             const float *from = c < n_pre ? (n_pre == 1 ? a.pre_row_lse : a.pre_slot_lse)
                                           : (n_own == 1 ? a.row_lse : a.slot_lse);
-            return from[index(c)] + (c < n_pre ? shift : 0.f);
+            return from[index(i)] + (c < n_pre ? shift : 0.f);
         };
         float mx = -INFINITY;
         for (int c = lane; c < n; c += LANES)
@@ -1027,13 +1453,13 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(JoinArgs a)
                 f32x4r x[UNROLL][RUNS];
 #pragma unroll
                 for (int u = 0; u < UNROLL; ++u) {
-                    const int cc = c0 + min(c + u, top - 1);
+                    const int i = c0 + min(c + u, top - 1), cc = WIDE ? way + ways * i : i;
                     const float *from = cc < n_pre ? (n_pre == 1 ? a.pre_row_o : a.pre_slot_o)
                                                    : (n_own == 1 ? a.row_o : a.slot_o);
-                    from += index(cc) * D + 4 * lane;
+                    from += index(i) * D + 4 * lane;
 #pragma unroll
-                    for (int i = 0; i < RUNS; ++i)
-                        x[u][i] = *reinterpret_cast<const f32x4r *>(from + 4 * LANES * i);
+                    for (int k = 0; k < RUNS; ++k)
+                        x[u][k] = *reinterpret_cast<const f32x4r *>(from + 4 * LANES * k);
                 }
 #pragma unroll
                 for (int u = 0; u < UNROLL; ++u) {
@@ -1050,6 +1476,42 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(JoinArgs a)
 #pragma unroll
         for (int o = LANES / 2; o >= 1; o >>= 1)
             den += __shfl_xor(den, o);
+        float m_all = m_use;
+        if constexpr (WIDE) {
+            // the ways of a row, in order
+            float *const to = s_part[threadIdx.x / LANES];
+#pragma unroll
+            for (int i = 0; i < RUNS; ++i)
+                *reinterpret_cast<f32x4r *>(to + 4 * LANES * i + 4 * lane) = acc[i];
+            if (lane == 0) {
+                to[D] = n > 0 ? mx : -INFINITY;
+                to[D + 1] = den;
+            }
+            __syncthreads();
+            if (!mine || way != 0)
+                return;
+            const float(*part)[D + 4] = &s_part[threadIdx.x / LANES];
+            float top = -INFINITY;
+            for (int w = 0; w < ways; ++w)
+                top = fmaxf(top, part[w][D]);
+            m_all = top == -INFINITY ? 0.f : top;
+            den = 0.f;
+#pragma unroll
+            for (int i = 0; i < RUNS; ++i)
+                acc[i] = f32x4r{};
+            for (int w = 0; w < ways; ++w) {
+                const float f = __expf(part[w][D] - m_all);
+                den += f * part[w][D + 1];
+#pragma unroll
+                for (int i = 0; i < RUNS; ++i) {
+                    const f32x4r y =
+                        *reinterpret_cast<const f32x4r *>(part[w] + 4 * LANES * i + 4 * lane);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        acc[i][e] += f * y[e];
+                }
+            }
+        }
         const float inv = den == 0.f ? 0.f : 1.f / den;
 #pragma unroll
         for (int i = 0; i < RUNS; ++i) {
@@ -1064,7 +1526,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(JoinArgs a)
         if (a.lse && lane == 0)
             a.lse[(int64_t)h * a.total_tokens + q0 + qt] =
                 den == 0.f ? -INFINITY
-                           : m_use + __logf(den) +
+                           : m_all + __logf(den) +
                                  (a.slopes ? rows_lse_shift(a.slopes[h], a.prefix_len + pos0 + qt)
                                            : 0.f);
     }
@@ -1075,6 +1537,7 @@ struct PagedLayout {
     int own_rb, pre_rb;        // row blocks of the two passes
     int own_slots, pre_slots;  // shares a kv head
     int max_tiles, n_records;
+    bool by_tile;
     size_t records, own_slot_o, own_slot_lse, own_row_o, own_row_lse, pre_slot_o, pre_slot_lse,
         pre_row_o, pre_row_lse, bytes;
 };
@@ -1114,7 +1577,9 @@ PagedLayout paged_layout(int32_t batch, int64_t total_tokens, bool ragged, bool 
         at += (n + 255) / 256 * 256;
         return here;
     };
-    p.n_records = prefix ? p.max_tiles : p.own_slots;
+    // 8-bit: one a row tile where that is fewer, or where shares cut by charges too
+    p.by_tile = prefix || (q8 && (p.own_rb == 1 || p.max_tiles <= p.own_slots));
+    p.n_records = p.by_tile ? p.max_tiles : p.own_slots;
     p.records = take((size_t)p.n_records * kRecordWords * 4);
     const size_t own = (size_t)2 * p.own_slots * hkv * rows;
     p.own_slot_o = take(own * d * 4);
@@ -1239,7 +1704,11 @@ ta_status paged_attn(const char *fn, bool q8, const void *q, const void *k_cache
         return fail(TA_ERR_UNSUPPORTED, "%s: too many steps", fn);
     // the join: workgroups of a row tile, rows of each
     const int join_rows = cu_q ? 32 * p.own_rb : (int)group;
-    const int chunk_rows = std::min(join_rows, kJoinThreads / 16);
+    // 8-bit: as many ways as a row has partials on average, at most
+    int ways = 1;
+    while (q8 && ways < kJoinThreads / 16 && 2 * ways * p.max_tiles <= p.own_slots)
+        ways *= 2;
+    const int chunk_rows = std::min(join_rows, kJoinThreads / 16 / ways);
     const int chunks = (join_rows + chunk_rows - 1) / chunk_rows;
     const int64_t wgs = std::max<int64_t>({p.own_slots, prefix_len > 0 ? p.pre_slots : 0,
                                            (int64_t)p.n_records * chunks}) * hkv;
@@ -1303,6 +1772,7 @@ ta_status paged_attn(const char *fn, bool q8, const void *q, const void *k_cache
     a.row_lse = prefix ? part(p.own_row_lse) : nullptr;
     a.records = reinterpret_cast<int32_t *>(ws + p.records);
     a.n_records = p.n_records;
+    a.by_tile = p.by_tile;
     a.score = score_args;
     a.total_tokens = (int32_t)total_tokens;
     a.batch = batch;
@@ -1341,7 +1811,9 @@ ta_status paged_attn(const char *fn, bool q8, const void *q, const void *k_cache
         j.slot_o = a.slot_o;
         j.slot_lse = a.slot_lse;
         j.tile_rows = 32 * p.own_rb;
+        j.charge = q8 && p.own_rb == 1 ? PagedShape<128, 1, true>::CHARGE : 0;
         j.chunk_rows = chunk_rows;
+        j.ways = ways;
         j.chunks = chunks;
         j.row_o = a.row_o;
         j.row_lse = a.row_lse;
@@ -1351,9 +1823,10 @@ ta_status paged_attn(const char *fn, bool q8, const void *q, const void *k_cache
         j.pre_row_lse = part(p.pre_row_lse);
         j.prefix_len = prefix_len;
         j.pre_rows = 32 * p.pre_rb;
-        // (steps are as long for either form of the cache and head_dim)
-        const int step =
-            p.pre_rb == 4 ? PagedShape<128, 4, false>::STEP : PagedShape<128, 1, false>::STEP;
+        // (steps are as long for either head_dim)
+        const int step = p.pre_rb == 4 ? PagedShape<128, 4, false>::STEP
+                         : q8          ? PagedShape<128, 1, true>::STEP
+                                       : PagedShape<128, 1, false>::STEP;
         j.pre_steps = (prefix_len + step - 1) / step;
         j.pre_share =
             (int32_t)std::max<int64_t>(p.pre_rb == 4 ? PagedShape<128, 4, false>::LEAST
@@ -1366,10 +1839,11 @@ ta_status paged_attn(const char *fn, bool q8, const void *q, const void *k_cache
         j.group = (int32_t)group;
         j.o_f32 = a.o_f32;
         const dim3 grid((uint32_t)(p.n_records * chunks * hkv));
-        if (head_dim == 128)
-            hipLaunchKernelGGL(paged_join_kernel<128>, grid, dim3(kJoinThreads), 0, s, j);
-        else
-            hipLaunchKernelGGL(paged_join_kernel<64>, grid, dim3(kJoinThreads), 0, s, j);
+        const auto join =
+            head_dim == 128
+                ? (ways > 1 ? paged_join_kernel<128, true> : paged_join_kernel<128, false>)
+                : (ways > 1 ? paged_join_kernel<64, true> : paged_join_kernel<64, false>);
+        hipLaunchKernelGGL(join, grid, dim3(kJoinThreads), 0, s, j);
         err = hipGetLastError();
     }
     if (err != hipSuccess)
