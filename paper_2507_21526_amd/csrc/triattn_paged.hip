@@ -76,15 +76,16 @@ struct PagedArgs {
 //     request with query offsets and 8 without: fewer share a CU from some 700
 //     requests with offsets on at d = 128, from 280 (700 without) at d = 64.
 //   RB = 4: four waves of 32 rows each over the same 64-key tiles, in two stages.
+//   RB = 0 (8-bit caches): as RB = 1, up to 16 rows.
 template <int D, int RB, bool Q8>
 struct PagedShape {
-    static constexpr bool TILES8 = Q8 && RB == 1;  // tiles in LDS hold 8 bits too
+    static constexpr bool TILES8 = Q8 && RB <= 1;  // tiles in LDS hold 8 bits too
     static constexpr int NKB = RB == 4 || TILES8 ? 2 : 1;
     static constexpr int TK = 32 * NKB;      // keys of a tile
     static constexpr int KS = RB == 4 ? 1 : 2;  // key splits of a workgroup
-    static constexpr int THREADS = 64 * RB * KS;
+    static constexpr int THREADS = 64 * (RB == 4 ? 4 : 1) * KS;
     static constexpr int STEP = TK * KS;     // keys of a step
-    static constexpr int ROWS = 32 * RB;
+    static constexpr int ROWS = RB == 0 ? 16 : 32 * RB;
     static constexpr int TILE_BYTES = TK * (TILES8 ? D : 2 * D);
     // K tile, V tile, and of 8-bit tiles the scales: the bytes as they come (K's,
     // V's), then V's as fp32
@@ -94,15 +95,15 @@ struct PagedShape {
     static constexpr int Q_BYTES = TILES8 ? ROWS * 2 * D : 0;  // the next piece's query rows
     static constexpr int LDS_BYTES = KS * BUFFER_BYTES + Q_BYTES;
     // What a row tile costs a share beside its steps, in steps (8-bit tiles): us of
-    // 96 requests of 150 to 15000 keys (32 heads over 8, d = 128) CHARGE_FIGURES
-    static constexpr int CHARGE = TILES8 ? 2 : 0;
+    // 96 requests of 150 to 15000 keys (32 heads over 8, d = 128) none 179, one 145, two 146, three 151
+    static constexpr int CHARGE = TILES8 ? 1 : 0;
     // Least steps of a share: one of a 128-row tile leaves partials of twice
     // its K and V tiles' bytes.  us with 1, 4 and 8 steps (32 heads over 8, d =
     // 128): the last 64 tokens of 2000 27, 25, 29, of four times 1000 29, 25, 28,
     // 128 single tokens behind a prefix of 2048 47, 43, 44, the last 100 tokens of
     // 500 17, 24, 29; from 3000 keys on the same.
     static constexpr int LEAST = RB == 4 ? 4 : 1;
-    static constexpr int WGS_PER_CU = RB == 1 && D == 64 ? 4 : 2;
+    static constexpr int WGS_PER_CU = RB <= 1 && D == 64 ? 4 : 2;
     static constexpr int WAVES_PER_SIMD = (WGS_PER_CU * THREADS / 64 + 3) / 4;
 };
 
@@ -341,8 +342,8 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
     const uint32_t smem_addr =
         (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
     // this wave's buffers (RB = 1) or the workgroup's stages (RB = 4)
-    const int wave_lds = RB == 1 ? wave * S::BUFFER_BYTES : 0;
-    const int first_group = RB == 1 ? 0 : wave * GROUPS;
+    const int wave_lds = RB <= 1 ? wave * S::BUFFER_BYTES : 0;
+    const int first_group = RB <= 1 ? 0 : wave * GROUPS;
     const int dma_row = lane / CHUNKS;
     // a copying lane's place in a group's first block; block m flips the K
     // swizzle's bits of m COPY_ROWS
@@ -362,7 +363,11 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
         return base + ((((int64_t)id * a.hkv + g) << a.page_log2) + place);
     };
 
-    std::conditional_t<S::TILES8, RowBlock8<D, S::NKB, SCORE>, RowBlock<D, S::NKB, SCORE>> rb;
+    std::conditional_t<S::TILES8,
+                       std::conditional_t<RB == 0, RowBlock8x16<D, S::NKB, SCORE>,
+                                          RowBlock8<D, S::NKB, SCORE>>,
+                       RowBlock<D, S::NKB, SCORE>>
+        rb;
     rb.init(lane);
 
     if constexpr (S::TILES8) {
@@ -373,7 +378,7 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
         constexpr bool BACK = (SCORE & kScoreSlope) != 0;  // last keys first, see below
         constexpr int V_COPIES = GROUPS * COPIES, K_COPIES = V_COPIES + 1;  // K's: scales too
         constexpr int Q_COPIES = S::Q_BYTES / 1024 / S::KS;  // of a wave
-        constexpr int HALF = D_BLOCKS / 2;
+        constexpr int HALF = decltype(rb)::CHUNKS / 2;
         const uint32_t q_lds = smem_addr + S::KS * S::BUFFER_BYTES;
         typedef const __attribute__((address_space(4))) int32_t *ids_ptr;
 
@@ -442,41 +447,38 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
                                                : a.table + (int64_t)p.rt.req * a.width);
         };
 
-        // The tile that is copied next: its first key, and the pages of its two
-        // groups of keys (on their way).
-        struct Next {
-            int key, id[GROUPS];
-        };
-        auto find_ids = [&](ids_ptr ids, int limit, int key0, Next &x) TA_INLINE {
-            x.key = key0;
+        // The pages of a tile's groups of keys.
+        using Ids = int[GROUPS];
+        auto find_ids = [&](ids_ptr ids, int limit, int key0, Ids &id) TA_INLINE {
 #pragma unroll
             for (int i = 0; i < GROUPS; ++i)
-                x.id[i] = ids[min(key0 + i * GROUP, limit - 1) >> a.page_log2];
+                id[i] = ids[min(key0 + i * GROUP, limit - 1) >> a.page_log2];
         };
         // Page ids that are none become 0; returns the first key of such a page.
-        auto check_ids = [&](int limit, Next &x) TA_INLINE -> int {
+        auto check_ids = [&](int limit, int key0, Ids &id) TA_INLINE -> int {
             int bad = INT32_MAX;
 #pragma unroll
-            for (int i = 0; i < GROUPS; ++i)
-                if ((uint32_t)x.id[i] >= (uint32_t)a.num_pages) {
-                    x.id[i] = 0;
-                    bad = min(bad, min(x.key + i * GROUP, limit - 1) & ~page_mask);
+            for (int i = 0; i < GROUPS; ++i) {
+                id[i] = uni(id[i]);
+                if ((uint32_t)id[i] >= (uint32_t)a.num_pages) {
+                    id[i] = 0;
+                    bad = min(bad, min(key0 + i * GROUP, limit - 1) & ~page_mask);
                 }
+            }
             return bad;
         };
         // Copies a tile's K rows and scales, or its V rows, into a stage.  Keys from
         // rt.limit on repeat the last one before it; they lie past every row's last
         // key.
-        auto copy_part = [&](int limit, const Next &x, int stage, auto is_v) TA_INLINE {
+        auto copy_part = [&](int limit, int key0, const Ids &id, int stage, auto is_v) TA_INLINE {
             constexpr bool V = decltype(is_v)::value;
             const uint32_t lds = smem_addr + wave_lds + stage * S::STAGE_BYTES;
-            const bool inside = x.key + S::TK <= limit;
+            const bool inside = key0 + S::TK <= limit;
             asm volatile("" ::: "memory");
 #pragma unroll
             for (int i = 0; i < GROUPS; ++i) {
-                const int key = x.key + i * GROUP;
-                const unsigned char *page =
-                    (V ? vc : kc) + (int64_t)uni(x.id[i]) * page_stride;
+                const int key = key0 + i * GROUP;
+                const unsigned char *page = (V ? vc : kc) + (int64_t)uni(id[i]) * page_stride;
                 const uint32_t to = lds + (V ? S::TILE_BYTES : 0) + i * GROUP * D;
                 if (inside) {
                     const unsigned char *from = page + (key & page_mask) * D;
@@ -502,11 +504,11 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
             if constexpr (!V) {
                 constexpr int PER = S::TK / 4;  // lanes of K's keys
                 // (keys from the limit on: bytes of the last ones, not used)
-                const int key = min(x.key + 4 * (lane & (PER - 1)), (limit - 1) & ~3);
-                int mine = x.id[0];
+                const int key = min(key0 + 4 * (lane & (PER - 1)), (limit - 1) & ~3);
+                int mine = id[0];
 #pragma unroll
                 for (int i = 1; i < GROUPS; ++i)
-                    mine = key >= x.key + i * GROUP ? x.id[i] : mine;
+                    mine = key >= key0 + i * GROUP ? id[i] : mine;
                 copy_to_lds4(scale_at(lane & PER ? a.vs : a.ks, mine, key & page_mask),
                              lds + 2 * S::TILE_BYTES);
             }
@@ -533,10 +535,9 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
         auto read_q = [&]() TA_INLINE {
             const unsigned char *row = smem + S::KS * S::BUFFER_BYTES + rb.col * 2 * D;
 #pragma unroll
-            for (int i = 0; i < D / 16; ++i)
+            for (int i = 0; i < decltype(rb)::Q_FRAGMENTS; ++i)
                 rb.qf[i] = *reinterpret_cast<const bf16x8 *>(
-                    row + (((4 * (i >> 1) + 2 * rb.half + (i & 1)) ^ (rb.col & (Q_CHUNKS - 1)))
-                           << 4));
+                    row + ((rb.q_chunk(i) ^ (rb.col & (Q_CHUNKS - 1))) << 4));
         };
 
         Piece cur, nxt;
@@ -544,12 +545,13 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
             return;
         bool ahead = false;  // the copies are in nxt, not in cur
         bool q_due = false;  // nxt's query rows are not on their way yet
-        bool has = false;    // there is a next tile, nt
-        int made = 0;        // tiles of the piece being copied that nt has come to
+        bool has = false;    // there is a next tile, from key nt_key on
+        int made = 0;        // tiles of the piece being copied, the next one among them
         int flying = 0;      // tiles whose copies have begun, not yet multiplied
         int in_stage = 0, out_stage = 0;
         int bad_cur = INT32_MAX, bad_nxt = INT32_MAX;
-        Next nt;
+        int nt_key = 0;
+        Ids nt;  // their pages (on their way)
         // of the piece being copied
         int src_base = cur.base, src_n = cur.n, src_limit = cur.rt.limit;
         ids_ptr src_pages = pages_of(cur);
@@ -568,7 +570,8 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
                 if (src_n == 0)
                     return;
             }
-            find_ids(src_pages, src_limit, key_of(src_base, src_n, made), nt);
+            nt_key = key_of(src_base, src_n, made);
+            find_ids(src_pages, src_limit, nt_key, nt);
             ++made;
             has = true;
         };
@@ -583,15 +586,15 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
             send_q();
             if (!has)
                 return;
-            const int bad = check_ids(src_limit, nt);
+            const int bad = check_ids(src_limit, nt_key, nt);
             bad_nxt = ahead ? min(bad_nxt, bad) : bad_nxt;
             bad_cur = ahead ? bad_cur : min(bad_cur, bad);
-            copy_part(src_limit, nt, in_stage, K{});
+            copy_part(src_limit, nt_key, nt, in_stage, K{});
         };
         auto produce_v = [&]() TA_INLINE {
             if (!has)
                 return;
-            copy_part(src_limit, nt, in_stage, V{});
+            copy_part(src_limit, nt_key, nt, in_stage, V{});
             in_stage = in_stage + 1 == S::STAGES ? 0 : in_stage + 1;
             ++flying;
             advance();
@@ -654,21 +657,16 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
             auto tile = [&](int key0, unsigned char *kt, auto careful, auto &&between)
                             TA_INLINE {
                 constexpr bool CAREFUL = decltype(careful)::value;
-                // K's scale of this lane's key; V's as fp32 for the weights, 0 for
-                // a key that no row keeps
+                // V's scales as fp32, 0 for a key that no row keeps
                 static_assert(S::TK == 64, "a key a lane");
                 unsigned char *raw = kt + 2 * S::TILE_BYTES;
-                float kscale[S::NKB];
-#pragma unroll
-                for (int kb = 0; kb < S::NKB; ++kb)
-                    kscale[kb] = q8_scale_bits(raw[kb * 32 + rows_perm(rb.col)]);
                 const uint32_t byte = raw[S::TK + lane];
                 const bool on = key0 + lane < rt.limit;
                 float *vscale = reinterpret_cast<float *>(raw + 256);
                 vscale[lane] = on ? q8_scale(byte) : 0.f;
-                f32x16 s[S::NKB];
-                bf16x8 p[S::NKB][2];
-                rb.products8(kt, kscale, s);
+                typename decltype(rb)::Scores s;
+                typename decltype(rb)::Probs p;
+                rb.products8(kt, raw, s);
                 between();
                 rb.modify(s, a.score);
                 const bool masked = key0 + S::TK - 1 > first_last;
@@ -676,16 +674,7 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
                     asm volatile("");  // a branch: most tiles have no mask
                     rb.mask_above(s, last - key0);
                 }
-                f32x4r w[S::NKB][4];  // V's scales of this lane's keys (rows_key_of_reg)
-#pragma unroll
-                for (int kb = 0; kb < S::NKB; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        w[kb][i] = *reinterpret_cast<const f32x4r *>(
-                            vscale + 32 * kb + 16 * (i >> 1) + 8 * rb.half + 4 * (i & 1));
-                rb.softmax(s, a.score, slope, key0 - dist_row, p, fresh,
-                           [&](int kb, int v, float x)
-                               TA_INLINE { return x * w[kb][v / 4][v % 4]; });
+                rb.softmax8(s, a.score, slope, key0 - dist_row, p, fresh, vscale);
                 fresh = false;
                 if constexpr (CAREFUL) {
                     rb.accumulate8_by_key(kt + S::TILE_BYTES, s, p);
@@ -694,7 +683,7 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
                     if (__builtin_expect(masked, 0)) {
                         asm volatile("");
                         odd |= __builtin_amdgcn_ballot_w64(on && byte == 255) != 0 ||
-                               rb.odd_elements(kt + S::TILE_BYTES, lane);
+                               rows8_odd_elements<S::TILE_BYTES>(kt + S::TILE_BYTES, lane);
                     }
                     rb.accumulate8(kt + S::TILE_BYTES, p);
                 }
@@ -723,13 +712,12 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
 
             // The waves join, each finishing half of the d blocks: it leaves the
             // other half of its sums in its free stage.
-            static_assert(HALF * 4096 <= S::STAGE_BYTES, "half of the sums fit a stage");
-            float own_l = 0.f;
+            static_assert(HALF * 1024 <= S::STAGE_BYTES, "half of the sums fit a stage");
             auto leave = [&](int odd_values) TA_INLINE {
-                own_l = rows_pair_sum(rb.l_run);
-                if (rb.half == 0) {
+                const float l = rb.row_sum(rb.l_run);
+                if (rb.first()) {
                     s_ml[wave][rb.col][0] = rb.m_ref;
-                    s_ml[wave][rb.col][1] = own_l;
+                    s_ml[wave][rb.col][1] = l;
                 }
                 if (lane == 0) {
                     s_end[wave][0] = bad_cur;
@@ -739,15 +727,9 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
                 if (cur.n == 0)
                     return;
 #pragma unroll
-                for (int b = 0; b < HALF; ++b)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        f32x4r x;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            x[e] = wave ? rb.oacc[b][4 * c + e] : rb.oacc[HALF + b][4 * c + e];
-                        *reinterpret_cast<f32x4r *>(scratch + ((b * 4 + c) * 64 + lane) * 16) = x;
-                    }
+                for (int c = 0; c < HALF; ++c)
+                    *reinterpret_cast<f32x4r *>(scratch + (c * 64 + lane) * 16) =
+                        wave ? rb.chunk(c) : rb.chunk(HALF + c);
             };
             leave(odd);
             if (!ahead && !has)
@@ -762,14 +744,15 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
                 fresh = true;
                 rb.reset();
                 for (int i = 0; i < cur.n; ++i) {
-                    Next x;
-                    find_ids(pages_of(cur), rt.limit, key_of(cur.base, cur.n, i), x);
+                    const int key0 = key_of(cur.base, cur.n, i);
+                    Ids id;
+                    find_ids(pages_of(cur), rt.limit, key0, id);
+                    check_ids(rt.limit, key0, id);
                     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
-                    check_ids(rt.limit, x);
-                    copy_part(rt.limit, x, free_stage, K{});
-                    copy_part(rt.limit, x, free_stage, V{});
+                    copy_part(rt.limit, key0, id, free_stage, K{});
+                    copy_part(rt.limit, key0, id, free_stage, V{});
                     rows_wait_copies<0>();
-                    tile(x.key, scratch, std::true_type{}, []() {});
+                    tile(key0, scratch, std::true_type{}, []() {});
                 }
                 leave(0);
                 barrier_no_fence();
@@ -793,32 +776,25 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
             const bool other = (wave ? m0 : m1) != -INFINITY;
             if (rb.col < rt.rows) {
 #pragma unroll
-                for (int b = 0; b < HALF; ++b)
+                for (int c = 0; c < HALF; ++c) {
+                    f32x4r x{};
+                    if (other)
+                        x = *reinterpret_cast<const f32x4r *>(theirs + (c * 64 + lane) * 16);
+                    const f32x4r mine = wave ? rb.chunk(HALF + c) : rb.chunk(c);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        f32x4r x{};
-                        if (other)
-                            x = *reinterpret_cast<const f32x4r *>(theirs +
-                                                                  ((b * 4 + c) * 64 + lane) * 16);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float mine =
-                                wave ? rb.oacc[HALF + b][4 * c + e] : rb.oacc[b][4 * c + e];
-                            x[e] = (f0 * (wave ? x[e] : mine) + f1 * (wave ? mine : x[e])) * inv;
-                        }
-                        const int d0 = 32 * (wave * HALF + b) + 8 * c + 4 * rb.half;
-                        if (to_o && !a.o_f32)
-                            *reinterpret_cast<bf16x4r *>(static_cast<__bf16 *>(a.o) + orow * D +
-                                                         d0) = __builtin_convertvector(x, bf16x4r);
-                        else if (to_o)
-                            *reinterpret_cast<f32x4r *>(static_cast<float *>(a.o) + orow * D +
-                                                        d0) = x;
-                        else
-                            *reinterpret_cast<f32x4r *>(cur.slot < 0 ? a.row_o + orow * D + d0
-                                                                     : a.slot_o + srow * D + d0) =
-                                x;
-                    }
-                if (wave == 0 && rb.half == 0) {
+                    for (int e = 0; e < 4; ++e)
+                        x[e] = (f0 * (wave ? x[e] : mine[e]) + f1 * (wave ? mine[e] : x[e])) * inv;
+                    const int d0 = rb.chunk_d(wave * HALF + c);
+                    if (to_o && !a.o_f32)
+                        *reinterpret_cast<bf16x4r *>(static_cast<__bf16 *>(a.o) + orow * D + d0) =
+                            __builtin_convertvector(x, bf16x4r);
+                    else if (to_o)
+                        *reinterpret_cast<f32x4r *>(static_cast<float *>(a.o) + orow * D + d0) = x;
+                    else
+                        *reinterpret_cast<f32x4r *>(cur.slot < 0 ? a.row_o + orow * D + d0
+                                                                 : a.slot_o + srow * D + d0) = x;
+                }
+                if (wave == 0 && rb.first()) {
                     float lse = (den == 0.f ? -INFINITY : (m + __log2f(den)) * kRowsLn2) + nan;
                     if (to_o) {
                         if constexpr ((SCORE & kScoreSlope) != 0)
@@ -1367,7 +1343,7 @@ struct JoinArgs {
 // many rows at once matter more than wide ones (prompt pieces: 22 us, with a wave
 // to a row 50).  Where few requests share the chip a row has many partials: WIDE
 // then gives it `ways` groups of sixteen lanes, which take every ways-th partial each
-// and join in LDS (three requests of 128K keys, 43 partials a row: WIDE_FIGURES).
+// and join in LDS (three requests of 128K keys, 43 partials a row: 6.4 us, one way 22).
 template <int D, bool WIDE>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(JoinArgs a)
 {
@@ -1545,10 +1521,15 @@ struct PagedLayout {
 template <bool Q8>
 int wgs_per_cu(int rb, int d)
 {
+    if (Q8 && rb == 0)
+        return d == 128 ? PagedShape<128, 0, true>::WGS_PER_CU : PagedShape<64, 0, true>::WGS_PER_CU;
     if (d == 128)
         return rb == 4 ? PagedShape<128, 4, Q8>::WGS_PER_CU : PagedShape<128, 1, Q8>::WGS_PER_CU;
     return rb == 4 ? PagedShape<64, 4, Q8>::WGS_PER_CU : PagedShape<64, 1, Q8>::WGS_PER_CU;
 }
+
+// Rows of a tile.
+int form_rows(int rb) { return rb == 0 ? 16 : 32 * rb; }
 
 PagedLayout paged_layout(int32_t batch, int64_t total_tokens, bool ragged, bool prefix, int32_t hq,
                          int32_t hkv, int32_t d, bool q8)
@@ -1566,9 +1547,15 @@ PagedLayout paged_layout(int32_t batch, int64_t total_tokens, bool ragged, bool 
     // 255 single tokens and one piece of 1024 915 (as chosen) and 823.
     p.own_rb = !ragged || total_tokens * group <= (int64_t)batch * 32 ? 1 : 4;
     p.pre_rb = total_tokens * group <= 32 ? 1 : 4;
+    if (q8 && !ragged)
+        p.own_rb = 0;
+    else if (q8 && p.own_rb == 1 && total_tokens * group <= (int64_t)batch * 16)
+        p.own_rb = 0;
+    if (q8 && total_tokens * group <= 16)
+        p.pre_rb = 0;
     p.own_slots = std::max(1, kCus * per_cu(p.own_rb) / hkv);
     p.pre_slots = std::max(1, kCus * per_cu(p.pre_rb) / hkv);
-    const int64_t rows = 32 * p.own_rb;
+    const int64_t rows = form_rows(p.own_rb);
     p.max_tiles = (int)std::min<int64_t>(
         kMaxTiles + 1, ragged ? total_tokens * group / rows + batch : (int64_t)batch);
     size_t at = 0;
@@ -1578,7 +1565,7 @@ PagedLayout paged_layout(int32_t batch, int64_t total_tokens, bool ragged, bool 
         return here;
     };
     // 8-bit: one a row tile where that is fewer, or where shares cut by charges too
-    p.by_tile = prefix || (q8 && (p.own_rb == 1 || p.max_tiles <= p.own_slots));
+    p.by_tile = prefix || (q8 && (p.own_rb <= 1 || p.max_tiles <= p.own_slots));
     p.n_records = p.by_tile ? p.max_tiles : p.own_slots;
     p.records = take((size_t)p.n_records * kRecordWords * 4);
     const size_t own = (size_t)2 * p.own_slots * hkv * rows;
@@ -1586,7 +1573,7 @@ PagedLayout paged_layout(int32_t batch, int64_t total_tokens, bool ragged, bool 
     p.own_slot_lse = take(own * 4);
     if (prefix) {
         const size_t all = (size_t)total_tokens * hq;
-        const size_t pre = (size_t)2 * p.pre_slots * hkv * 32 * p.pre_rb;
+        const size_t pre = (size_t)2 * p.pre_slots * hkv * form_rows(p.pre_rb);
         p.own_row_o = take(all * d * 4);
         p.own_row_lse = take(all * 4);
         p.pre_slot_o = take(pre * d * 4);
@@ -1623,6 +1610,14 @@ template <bool PREFIX, bool Q8>
 hipError_t launch_pass(int d, int rb, int score, hipStream_t s, const PagedArgs &a)
 {
     const dim3 grid((uint32_t)(a.slots * a.hkv));
+    if constexpr (Q8)
+        if (rb == 0) {
+            if (d == 128)
+                launch_scores<128, 0, PREFIX, Q8>(score, grid, s, a);
+            else
+                launch_scores<64, 0, PREFIX, Q8>(score, grid, s, a);
+            return hipGetLastError();
+        }
     if (d == 128 && rb == 1)
         launch_scores<128, 1, PREFIX, Q8>(score, grid, s, a);
     else if (d == 128)
@@ -1699,11 +1694,12 @@ ta_status paged_attn(const char *fn, bool q8, const void *q, const void *k_cache
                     "tokens at a time)", fn, kMaxTiles);
     // steps are counted in 32 bits
     const int64_t steps = (int64_t)p.max_tiles * ((int64_t)table_width * page_size / 64 + 1);
-    const int64_t pre_tiles = (total_tokens * group + 32 * p.pre_rb - 1) / (32 * p.pre_rb);
+    const int pre_rows = form_rows(p.pre_rb);
+    const int64_t pre_tiles = (total_tokens * group + pre_rows - 1) / pre_rows;
     if (steps > INT32_MAX / 2 || pre_tiles * (prefix_len / 64 + 1) > INT32_MAX / 2)
         return fail(TA_ERR_UNSUPPORTED, "%s: too many steps", fn);
     // the join: workgroups of a row tile, rows of each
-    const int join_rows = cu_q ? 32 * p.own_rb : (int)group;
+    const int join_rows = cu_q ? form_rows(p.own_rb) : (int)group;
     // 8-bit: as many ways as a row has partials on average, at most
     int ways = 1;
     while (q8 && ways < kJoinThreads / 16 && 2 * ways * p.max_tiles <= p.own_slots)
@@ -1810,8 +1806,8 @@ ta_status paged_attn(const char *fn, bool q8, const void *q, const void *k_cache
         j.records = a.records;
         j.slot_o = a.slot_o;
         j.slot_lse = a.slot_lse;
-        j.tile_rows = 32 * p.own_rb;
-        j.charge = q8 && p.own_rb == 1 ? PagedShape<128, 1, true>::CHARGE : 0;
+        j.tile_rows = form_rows(p.own_rb);
+        j.charge = q8 && p.own_rb <= 1 ? PagedShape<128, 1, true>::CHARGE : 0;
         j.chunk_rows = chunk_rows;
         j.ways = ways;
         j.chunks = chunks;
@@ -1822,7 +1818,7 @@ ta_status paged_attn(const char *fn, bool q8, const void *q, const void *k_cache
         j.pre_row_o = part(p.pre_row_o);
         j.pre_row_lse = part(p.pre_row_lse);
         j.prefix_len = prefix_len;
-        j.pre_rows = 32 * p.pre_rb;
+        j.pre_rows = pre_rows;
         // (steps are as long for either head_dim)
         const int step = p.pre_rb == 4 ? PagedShape<128, 4, false>::STEP
                          : q8          ? PagedShape<128, 1, true>::STEP
