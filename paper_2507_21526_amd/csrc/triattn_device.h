@@ -100,6 +100,13 @@ __device__ __forceinline__ void copy_burst_to_lds16(const void *gbase, const uin
                      : "v"(off[0]), "v"(off[1]), "s"(gbase), "{m0}"(lds_addr));
 }
 
+// Sixteen bytes of a lane into LDS, unordered with the compiler's own LDS reads (of
+// another stage): a barrier with its wait orders them against the readers.
+__device__ __forceinline__ void write_lds16(uint32_t lds_addr, bf16x8 x)
+{
+    asm volatile("ds_write_b128 %0, %1" : : "v"(lds_addr), "v"(x));
+}
+
 // Workgroup barrier without a memory fence: this wave's LDS reads are
 // complete (lgkmcnt 0); copies into LDS are synchronised by vmcnt waits.
 __device__ __forceinline__ void barrier_no_fence()

@@ -77,13 +77,15 @@ struct PagedArgs {
 //     requests with offsets on at d = 128, from 280 (700 without) at d = 64.
 //   RB = 4: four waves of 32 rows each over the same 64-key tiles, in two stages.
 //   RB = 0 (8-bit caches): as RB = 1, up to 16 rows.
+//   RB = 8 (8-bit caches): as RB = 4 with two groups of four waves, one wave of each on
+//     a SIMD, in turns: the matrix products of one beside the softmax of the other.
 template <int D, int RB, bool Q8>
 struct PagedShape {
     static constexpr bool TILES8 = Q8 && RB <= 1;  // tiles in LDS hold 8 bits too
-    static constexpr int NKB = RB == 4 || TILES8 ? 2 : 1;
+    static constexpr int NKB = RB >= 4 || TILES8 ? 2 : 1;
     static constexpr int TK = 32 * NKB;      // keys of a tile
-    static constexpr int KS = RB == 4 ? 1 : 2;  // key splits of a workgroup
-    static constexpr int THREADS = 64 * (RB == 4 ? 4 : 1) * KS;
+    static constexpr int KS = RB >= 4 ? 1 : 2;  // key splits of a workgroup
+    static constexpr int THREADS = 64 * (RB >= 4 ? RB : 1) * KS;
     static constexpr int STEP = TK * KS;     // keys of a step
     static constexpr int ROWS = RB == 0 ? 16 : 32 * RB;
     static constexpr int TILE_BYTES = TK * (TILES8 ? D : 2 * D);
@@ -102,8 +104,8 @@ struct PagedShape {
     // 128): the last 64 tokens of 2000 27, 25, 29, of four times 1000 29, 25, 28,
     // 128 single tokens behind a prefix of 2048 47, 43, 44, the last 100 tokens of
     // 500 17, 24, 29; from 3000 keys on the same.
-    static constexpr int LEAST = RB == 4 ? 4 : 1;
-    static constexpr int WGS_PER_CU = RB <= 1 && D == 64 ? 4 : 2;
+    static constexpr int LEAST = RB >= 4 ? 4 : 1;
+    static constexpr int WGS_PER_CU = RB == 8 ? 1 : RB <= 1 && D == 64 ? 4 : 2;
     static constexpr int WAVES_PER_SIMD = (WGS_PER_CU * THREADS / 64 + 3) / 4;
 };
 
@@ -177,7 +179,7 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
     constexpr int COPY_ROWS = 1024 / ROW_BYTES;          // keys of a 1 KB copy
     constexpr int GROUP = 16;  // keys that surely share a page
     constexpr int COPIES = GROUP / COPY_ROWS;              // 1 KB copies of a group
-    constexpr int GROUPS = S::TK / GROUP / (RB == 4 ? 4 : 1);  // of a wave and tile
+    constexpr int GROUPS = S::TK / GROUP / (RB >= 4 ? 4 : 1);  // of a wave and tile
     constexpr int D_BLOCKS = D / 32;
 
     __shared__ __attribute__((aligned(1024))) unsigned char smem[S::LDS_BYTES];
@@ -343,7 +345,7 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
         (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
     // this wave's buffers (RB = 1) or the workgroup's stages (RB = 4)
     const int wave_lds = RB <= 1 ? wave * S::BUFFER_BYTES : 0;
-    const int first_group = RB <= 1 ? 0 : wave * GROUPS;
+    const int first_group = RB <= 1 ? 0 : (wave & 3) * GROUPS;
     const int dma_row = lane / CHUNKS;
     // a copying lane's place in a group's first block; block m flips the K
     // swizzle's bits of m COPY_ROWS
@@ -968,55 +970,74 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
                     asm volatile("");
                     odd |= rb.odd_values(vt, lane, RB == 1 ? 0 : wave, RB);
                 }
-                __builtin_amdgcn_sched_barrier(0);
-                rb.accumulate(vt, p);
-                rb.template schedule<false, true>();
-                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (Q8) {
+                    __builtin_amdgcn_s_setprio(1);
+                    rb.template in_order<false, true>(vt, vt, s, p);
+                    __builtin_amdgcn_s_setprio(0);
+                } else {
+                    __builtin_amdgcn_sched_barrier(0);
+                    rb.accumulate(vt, p);
+                    rb.template schedule<false, true>();
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             };
             auto products = [&](const unsigned char *kt) TA_INLINE {
-                __builtin_amdgcn_sched_barrier(0);
-                rb.products(kt, s);
-                rb.template schedule<true, false>();
-                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (Q8) {
+                    rb.template in_order<true, false>(kt, kt, s, p);
+                } else {
+                    __builtin_amdgcn_sched_barrier(0);
+                    rb.products(kt, s);
+                    rb.template schedule<true, false>();
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             };
-            // An 8-bit cache's rows as bf16 tiles (RB = 4): a wave loads a group's
-            // rows and scales into registers, and later leaves them in LDS, each
-            // element times its scale.
+            // An 8-bit cache's rows as bf16 tiles: a wave loads a group's rows and
+            // scales into registers, and later leaves them in LDS, each element times
+            // its scale.  With eight waves the first four take K, the others V.
             constexpr int LOADS = Q8 ? GROUP * D / 1024 : 1;  // 16-byte loads of a lane, K or V
             constexpr int LOAD_ROWS = GROUP / LOADS;
-            u32x4 held[2][LOADS];
-            uint32_t held_scale[2][LOADS];
+            constexpr int TENSORS = RB == 8 ? 1 : 2;
+            const int group = wave & 3, tensor0 = RB == 8 ? wave >> 2 : 0;
+            u32x4 held[TENSORS][LOADS];
+            uint32_t held_scale[TENSORS][LOADS];
             const int load_row = lane / (D / 16), load_chunk = lane % (D / 16);
             auto load_rows = [&](int key0) TA_INLINE {
-                const int first = min(key0 + wave * GROUP, rt.limit - 1);
+                const int first = min(key0 + group * GROUP, rt.limit - 1);
                 const int lim = min(rt.limit - 1 - first, GROUP - 1);  // the group's last row
                 const int id = uni(s_page[(first >> a.page_log2) - page0]);
                 const int place = first & page_mask;
                 const int64_t off = (int64_t)id * page_stride + place * ROW_BYTES;
-                const unsigned char *kp = kc + off, *vp = vc + off;
-                const unsigned char *ksp = scale_at(a.ks, id, place);
-                const unsigned char *vsp = scale_at(a.vs, id, place);
 #pragma unroll
-                for (int m = 0; m < LOADS; ++m) {
-                    const uint32_t row = min(m * LOAD_ROWS + load_row, lim);
-                    const uint32_t at = row * D + load_chunk * 16;
-                    held[0][m] = *reinterpret_cast<const u32x4 *>(kp + at);
-                    held[1][m] = *reinterpret_cast<const u32x4 *>(vp + at);
-                    held_scale[0][m] = ksp[row];
-                    held_scale[1][m] = vsp[row];
+                for (int v = 0; v < TENSORS; ++v) {
+                    const unsigned char *rows = (tensor0 + v ? vc : kc) + off;
+                    const unsigned char *scale = scale_at(tensor0 + v ? a.vs : a.ks, id, place);
+#pragma unroll
+                    for (int m = 0; m < LOADS; ++m) {
+                        const uint32_t row = min(m * LOAD_ROWS + load_row, lim);
+                        held[v][m] = *reinterpret_cast<const u32x4 *>(
+                            rows + (row * D + load_chunk * 16));
+                        held_scale[v][m] = scale[row];
+                    }
                 }
             };
             auto leave_rows = [&](int c, int stage) TA_INLINE {
                 const int v = c / LOADS, m = c % LOADS;
                 const int row = m * LOAD_ROWS + load_row;  // in the group
-                const int swz = v ? rows_vswz<D>(row) : rows_kswz<D>(row);
-                unsigned char *to = smem + stage * S::STAGE_BYTES + v * S::TILE_BYTES +
-                                    (wave * GROUP + row) * 2 * D;
+                const int swz = tensor0 + v ? rows_vswz<D>(row) : rows_kswz<D>(row);
+                const uint32_t to = smem_addr + stage * S::STAGE_BYTES +
+                                    (tensor0 + v) * S::TILE_BYTES + (group * GROUP + row) * 2 * D;
                 const float f = q8_scale_bits(held_scale[v][m]);
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
-                    *reinterpret_cast<bf16x8 *>(to + (((2 * load_chunk + i) ^ swz) << 4)) =
-                        q8_fragment(held[v][m][2 * i], held[v][m][2 * i + 1], f);
+                    write_lds16(to + (((2 * load_chunk + i) ^ swz) << 4),
+                                q8_fragment(held[v][m][2 * i], held[v][m][2 * i + 1], f));
+            };
+            auto leave_all = [&](int stage) TA_INLINE {
+                asm volatile("" ::: "memory");
+#pragma unroll
+                for (int c = 0; c < TENSORS * LOADS; ++c)
+                    leave_rows(c, stage);
+                asm volatile("" ::: "memory");
             };
             if constexpr (CAREFUL) {
                 // tile by tile, in this wave's first stage (RB = 1) or the
@@ -1028,9 +1049,7 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
                     const bool on = key0 < key_end;
                     if constexpr (Q8) {
                         load_rows(key0);
-#pragma unroll
-                        for (int c = 0; c < 2 * LOADS; ++c)
-                            leave_rows(c, 0);
+                        leave_all(0);
                     } else if (on) {
                         copy(key0, wave_lds, K{});
                         copy(key0, wave_lds + S::TILE_BYTES, V{});
@@ -1084,35 +1103,93 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
                 }
                 if (i < n)
                     step(i, std::integral_constant<int, 0>{});
+            } else if constexpr (RB == 8) {
+                // M(j) = {S(j) = K(j) Q^T, O += V(j - 1) P(j - 1)} on the matrix cores
+                // beside the other group's X(j), scores to probabilities, on the vector
+                // units.  Both groups run the same program, group 1 a phase later:
+                // group 0 has M(j) in phase 2 j and X(j) in phase 2 j + 1.  Stage j & 1
+                // holds K(j) and V(j - 1) in the two phases of M(j).  In X(j), after the
+                // softmax, group 0 leaves K(j + 1) in stage (j + 1) & 1 and group 1
+                // V(j + 1) in stage j & 1, which no wave reads any more by then, and loads
+                // the rows of step j + 2; nothing but LDS reads stands between the matrix
+                // instructions of M(j).
+                const int n = (key_end - seg0 * S::STEP + S::STEP - 1) / S::STEP;
+                auto key_of = [&](int i) TA_INLINE -> int {
+                    i = min(i, n - 1);
+                    return (seg0 + (BACK ? n - 1 - i : i)) * S::STEP;
+                };
+                auto end_phase = [&]() TA_INLINE {
+                    __builtin_amdgcn_sched_barrier(0);
+                    barrier_no_fence();
+                    __builtin_amdgcn_sched_barrier(0);
+                };
+                auto matrix = [&](int j, auto stage) TA_INLINE {
+                    const unsigned char *kt = smem + decltype(stage)::value * S::STAGE_BYTES;
+                    if (__builtin_expect(key_of(j - 1) + S::TK - 1 > tile_first_last, 0)) {
+                        asm volatile("");
+                        odd |= rb.odd_values(kt + S::TILE_BYTES, lane, wave, RB);
+                    }
+                    __builtin_amdgcn_s_setprio(1);
+                    rb.template in_order<true, true>(kt, kt + S::TILE_BYTES, s, p);
+                    __builtin_amdgcn_s_setprio(0);
+                };
+                // (past the last step its rows once more, where nothing reads them)
+                auto vector = [&](int j) TA_INLINE {
+                    softmax(key_of(j));
+                    __builtin_amdgcn_sched_barrier(0);
+                    leave_all(tensor0 ? j & 1 : (j + 1) & 1);
+                    load_rows(key_of(j + 2));
+                };
+                load_rows(key_of(0));
+                leave_all(tensor0);
+                load_rows(key_of(1));
+                end_phase();
+                if (tensor0)
+                    end_phase();
+                products(smem);
+                end_phase();
+                vector(0);
+                end_phase();
+                auto step = [&](int j, auto stage) TA_INLINE {
+                    matrix(j, stage);
+                    end_phase();
+                    vector(j);
+                    end_phase();
+                };
+                int j = 1;
+                for (; j + 1 < n; j += 2) {
+                    step(j, std::integral_constant<int, 1>{});
+                    step(j + 1, std::integral_constant<int, 0>{});
+                }
+                if (j < n)
+                    step(j, std::integral_constant<int, 1>{});
+                values(key_of(n - 1), smem + (n & 1) * S::STAGE_BYTES + S::TILE_BYTES);
+                end_phase();
+                if (!tensor0)
+                    end_phase();
             } else if constexpr (Q8) {
                 // As below, but through registers: step i leaves the rows of step
-                // i + 1 in LDS between its matrix instructions, and then loads
-                // those of i + 2.
+                // i + 1 in LDS after its products, and then loads those of i + 2.
                 const int n = (key_end - seg0 * S::STEP + S::STEP - 1) / S::STEP;
                 auto key_of = [&](int i) TA_INLINE -> int {
                     return (seg0 + (BACK ? n - 1 - i : i)) * S::STEP;
                 };
                 load_rows(key_of(0));
-#pragma unroll
-                for (int c = 0; c < 2 * LOADS; ++c)
-                    leave_rows(c, 0);
+                leave_all(0);
                 load_rows(key_of(min(1, n - 1)));
-                constexpr int STRIDE = S::NKB * (D / 16) / (2 * LOADS);
                 auto step = [&](int i, auto stage) TA_INLINE {
                     constexpr int ST = decltype(stage)::value;
                     // this step's tile is there for every wave, and every wave is
                     // done with the other stage
                     __builtin_amdgcn_sched_barrier(0);
                     barrier_no_fence();
-                    __builtin_amdgcn_sched_barrier(0);
+                    const unsigned char *kt = smem + ST * S::STAGE_BYTES;
+                    __builtin_amdgcn_s_setprio(1);
+                    products(kt);
+                    __builtin_amdgcn_s_setprio(0);
                     // (after the last step its tile is left once more, in the stage
                     // that nothing reads any more)
-                    const unsigned char *kt = smem + ST * S::STAGE_BYTES;
-                    rb.products(kt, s, [&](int m) TA_INLINE {
-                        if (m % STRIDE == STRIDE - 1 && m / STRIDE < 2 * LOADS)
-                            leave_rows(m / STRIDE, 1 - ST);
-                    });
-                    __builtin_amdgcn_sched_barrier(0);
+                    leave_all(1 - ST);
                     load_rows(key_of(min(i + 2, n - 1)));
                     __builtin_amdgcn_sched_barrier(0);
                     softmax(key_of(i));
@@ -1351,7 +1428,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(JoinArgs a)
     constexpr int PER = D / LANES;   // values of a lane, in runs of four
     constexpr int RUNS = PER / 4;
     constexpr int GROUPS = kJoinThreads / LANES;
-    __shared__ float s_part[WIDE ? GROUPS : 1][WIDE ? D + 4 : 1];
+    __shared__ __attribute__((aligned(16))) float s_part[WIDE ? GROUPS : 1][WIDE ? D + 4 : 4];
     const int ways = WIDE ? a.ways : 1;
     const int g = blockIdx.x % a.hkv, at = blockIdx.x / a.hkv;
     const int chunk = at % a.chunks;
@@ -1521,6 +1598,8 @@ struct PagedLayout {
 template <bool Q8>
 int wgs_per_cu(int rb, int d)
 {
+    if (Q8 && rb == 8)
+        return PagedShape<128, 8, true>::WGS_PER_CU;
     if (Q8 && rb == 0)
         return d == 128 ? PagedShape<128, 0, true>::WGS_PER_CU : PagedShape<64, 0, true>::WGS_PER_CU;
     if (d == 128)
@@ -1547,12 +1626,21 @@ PagedLayout paged_layout(int32_t batch, int64_t total_tokens, bool ragged, bool 
     // 255 single tokens and one piece of 1024 915 (as chosen) and 823.
     p.own_rb = !ragged || total_tokens * group <= (int64_t)batch * 32 ? 1 : 4;
     p.pre_rb = total_tokens * group <= 32 ? 1 : 4;
-    if (q8 && !ragged)
-        p.own_rb = 0;
-    else if (q8 && p.own_rb == 1 && total_tokens * group <= (int64_t)batch * 16)
-        p.own_rb = 0;
-    if (q8 && total_tokens * group <= 16)
-        p.pre_rb = 0;
+    if (q8) {
+        // 8-bit: tiles of 16 rows for single tokens (us with 32 and with 16: 96
+        // requests of 64, of 955, of 3820 keys 19.6, 57, 152 and 16.2, 52, 148; a
+        // request of more rows would read its keys more than once), and at d = 128
+        // tiles of 256 for requests of more than 128 on average (us with 128 and with 256: five requests of 40 tokens, of
+        // 256, of 500 to 1800 79, 241, 744 and 74, 207, 620, the last with a cap 844
+        // and 767; d = 64: 411 and 401, with a cap 587 and 625; the prefix's pass of
+        // 160 tokens, whose tiles are few, takes 5 more).
+        if (!ragged || total_tokens <= batch)
+            p.own_rb = 0;
+        else if (d == 128 && total_tokens * group > (int64_t)batch * 128)
+            p.own_rb = 8;
+        if (total_tokens * group <= 16)
+            p.pre_rb = 0;
+    }
     p.own_slots = std::max(1, kCus * per_cu(p.own_rb) / hkv);
     p.pre_slots = std::max(1, kCus * per_cu(p.pre_rb) / hkv);
     const int64_t rows = form_rows(p.own_rb);
@@ -1610,6 +1698,11 @@ template <bool PREFIX, bool Q8>
 hipError_t launch_pass(int d, int rb, int score, hipStream_t s, const PagedArgs &a)
 {
     const dim3 grid((uint32_t)(a.slots * a.hkv));
+    if constexpr (Q8 && !PREFIX)
+        if (rb == 8) {
+            launch_scores<128, 8, PREFIX, Q8>(score, grid, s, a);
+            return hipGetLastError();
+        }
     if constexpr (Q8)
         if (rb == 0) {
             if (d == 128)
@@ -1686,8 +1779,8 @@ ta_status paged_attn(const char *fn, bool q8, const void *q, const void *k_cache
         (slopes && (int64_t)table_width * page_size + prefix_len > INT32_MAX - 256) ||
         (int64_t)total_tokens * hq > INT32_MAX)
         return fail(TA_ERR_UNSUPPORTED, "%s: positions, slots or rows past 32 bits", fn);
-    const PagedLayout p =
-        paged_layout(batch, total_tokens, cu_q != nullptr, prefix_len > 0, hq, hkv, head_dim, q8);
+    const PagedLayout p = paged_layout(batch, total_tokens, cu_q != nullptr, prefix_len > 0, hq,
+                                       hkv, head_dim, q8);
     const int64_t group = hq / hkv;
     if (p.max_tiles > kMaxTiles)
         return fail(TA_ERR_UNSUPPORTED, "%s: more than %d row tiles a kv head (pass fewer query "
@@ -1708,7 +1801,8 @@ ta_status paged_attn(const char *fn, bool q8, const void *q, const void *k_cache
     const int chunks = (join_rows + chunk_rows - 1) / chunk_rows;
     const int64_t wgs = std::max<int64_t>({p.own_slots, prefix_len > 0 ? p.pre_slots : 0,
                                            (int64_t)p.n_records * chunks}) * hkv;
-    if (wgs * kJoinThreads > UINT32_MAX)  // threads of a launch
+    const int threads = p.own_rb == 8 ? PagedShape<128, 8, true>::THREADS : kJoinThreads;
+    if (wgs * threads > UINT32_MAX)  // of a launch
         return fail(TA_ERR_UNSUPPORTED, "%s: grid too large", fn);
     if (total_tokens == 0 || batch == 0)
         return TA_OK;

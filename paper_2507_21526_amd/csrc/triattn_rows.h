@@ -351,6 +351,48 @@ struct RowBlock {
         accumulate(vt, pf, [](int) {});
     }
 
+    // products() of one tile (QK) and then accumulate() of another (PV), each
+    // fragment read AHEAD matrix instructions before its own, in this order as it
+    // stands: where registers are scarce the scheduler undoes the one that schedule()
+    // asks for, and every matrix instruction waits for its read.
+    template <bool QK, bool PV, int AHEAD = 4>
+    __device__ __forceinline__ void in_order(const unsigned char *kt, const unsigned char *vt,
+                                             f32x16 (&s)[NKB], const bf16x8 (&pf)[NKB][2])
+    {
+        constexpr int NQ = QK ? NKB * QK_STEPS : 0, N = NQ + (PV ? NKB * 2 * D_BLOCKS : 0);
+        auto read = [&](int i) TA_INLINE -> bf16x8 {
+            if (i < NQ)
+                return *reinterpret_cast<const bf16x8 *>(kt + koff[i / NKB] +
+                                                         i % NKB * 32 * ROW_BYTES);
+            const int j = i - NQ;
+            return v_fragment(vt, j / (2 * D_BLOCKS), j / D_BLOCKS % 2, j % D_BLOCKS);
+        };
+        __builtin_amdgcn_sched_barrier(0);
+        bf16x8 ahead[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            ahead[i] = read(i);
+        if constexpr (QK)
+#pragma unroll
+            for (int kb = 0; kb < NKB; ++kb)
+                s[kb] = f32x16{};
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (i < NQ) {
+                s[i % NKB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    ahead[i % AHEAD], qf[i / NKB], s[i % NKB], 0, 0, 0);
+            } else {
+                const int j = i - NQ, b = j % D_BLOCKS;
+                oacc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    ahead[i % AHEAD], pf[j / (2 * D_BLOCKS)][j / D_BLOCKS % 2], oacc[b], 0, 0, 0);
+            }
+            if (i + AHEAD < N)
+                ahead[i % AHEAD] = read(i + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+
     // Whether a tile holds an infinite or NaN value (this wave looks at part
     // `part` of `parts`).  In a masked step rows give keys probability zero that
     // other rows keep, and zero times such a value must not reach them:

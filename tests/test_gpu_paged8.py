@@ -1,6 +1,7 @@
 """GPU tests of attention over the 8-bit paged cache, against 64 bits over the
 held values."""
 import math
+import random
 
 import pytest
 import torch
@@ -420,6 +421,7 @@ def test_offsets_past_32_bits():
 
 @pytest.mark.parametrize("form,d,ql,n,prefix", [
     ("two waves", 128, [1], 70001, 0), ("four waves", 64, [100], 33001, 0),
+    ("two waves, 32 rows", 64, [20], 140001, 0), ("eight waves", 128, [200], 33001, 0),
     ("prefix, two waves", 128, [1] * 20, 40, 70001),
     ("prefix, four waves", 64, [1] * 40, 40, 33001)])
 @pytest.mark.parametrize("score", ["plain", "slopes"])
@@ -466,3 +468,23 @@ def test_every_form_past_the_held_ids(form, d, ql, n, prefix, score, odd):
     check(o[:, some], l[:, some], c.reference(q[:, some], ql, d ** -0.5, None,
                                               sl[some] if sl is not None else None),
           torch.float32, f"{form} {score} {odd}")
+
+
+@pytest.mark.parametrize("seed", range(10))
+def test_shares_that_end_anywhere(seed):
+    """Random lengths: shares end within row tiles, between them, and within
+    what a row tile is charged beside its steps."""
+    rng = random.Random(seed)
+    d, hkv = rng.choice([64, 128]), rng.choice([1, 2, 8, 32])
+    hq, page = hkv * rng.choice([1, 2, 4, 7]), rng.choice([16, 32, 256])
+    batch = rng.choice([1, 3, 17, 70])
+    lens = [rng.choice([0, 1, 64, 127, 128, 129, 300, rng.randrange(1, 4000)])
+            for _ in range(batch)]
+    prefix = rng.choice([0, 0, 200])
+    c = Cache8(lens, hkv, d, page, prefix, seed=seed)
+    ql = [1] * batch
+    if seed % 3 == 2:
+        ql = [rng.randrange(0, 5) for _ in range(batch)]
+    q = _q(sum(ql), hq, d, seed)
+    o, l = _call(c, q, ql, torch.float32, None, None, ragged=seed % 3 > 0)
+    check(o, l, c.reference(q, ql, d ** -0.5), torch.float32, f"seed {seed}")
