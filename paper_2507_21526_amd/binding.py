@@ -526,10 +526,11 @@ def _cache_shape(k_cache):
     return tuple(k_cache.shape)
 
 
-def _cache_operands(k_cache, v_cache, k_scale, v_scale):
+def _cache_operands(torch, k_cache, v_cache, k_scale, v_scale):
     """Operands of a cache [pages, heads, page_size, head_dim]: bf16, or
-    float8_e4m3fn with scales float8_e8m0fnu [pages, heads, page_size]."""
-    import torch
+    float8_e4m3fn with scales float8_e8m0fnu [pages, heads, page_size].  (The
+    module is handed in: an import statement of its own costs a short call a
+    quarter of a microsecond.)"""
     shape = _cache_shape(k_cache)
     if k_scale is None and v_scale is None:
         return shape, [("k_cache", k_cache, torch.bfloat16, shape),
@@ -540,27 +541,30 @@ def _cache_operands(k_cache, v_cache, k_scale, v_scale):
                    ("v_scale", v_scale, torch.float8_e8m0fnu, shape[:3])]
 
 
-def _check_rows(k, v):
-    """k, v [tokens, heads, head_dim] bf16 of any token and head stride."""
-    import torch
+def _rows(torch, k, v):
+    """Shape and (token, head) strides of k, v [tokens, heads, head_dim] bf16 of
+    any token and head stride."""
     for name, t in (("k", k), ("v", v)):
         if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16:
             raise ValueError(f"{name} must be a bfloat16 tensor")
         if t.dim() != 3:
             raise ValueError(f"{name} must be [tokens, heads, head_dim], got {tuple(t.shape)}")
-        if t.shape[2] > 1 and t.stride(2) != 1:
-            raise ValueError(f"the last dimension of {name} must be contiguous")
-    if k.shape != v.shape:
-        raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} differ")
+    shape = k.shape
+    if shape != v.shape:
+        raise ValueError(f"k {tuple(shape)} and v {tuple(v.shape)} differ")
+    total, heads, d = shape
+    ks, kh, kd = k.stride()
+    vs, vh, vd = v.stride()
+    if d > 1 and (kd != 1 or vd != 1):
+        raise ValueError(f"the last dimension of {'k' if kd != 1 else 'v'} must be contiguous")
     if v.device != k.device:
         raise ValueError(f"v is on {v.device}, k on {k.device}")
-
-
-def _row_strides(k, v):
     # (the stride of a dimension of one says nothing)
-    many, heads = k.shape[0] > 1, k.shape[1] > 1
-    return (k.stride(0) if many else 0, k.stride(1) if heads else 0,
-            v.stride(0) if many else 0, v.stride(1) if heads else 0)
+    if total < 2:
+        ks = vs = 0
+    if heads < 2:
+        kh = vh = 0
+    return shape, (ks, kh, vs, vh)
 
 
 def kv_cache_write(k, v, slots, k_cache, v_cache, stream=None, k_scale=None, v_scale=None):
@@ -574,10 +578,9 @@ def kv_cache_write(k, v, slots, k_cache, v_cache, stream=None, k_scale=None, v_s
     (kv_cache_write_q8).
     """
     import torch
-    _check_rows(k, v)
-    total, hkv, d = k.shape
+    (total, hkv, d), strides = _rows(torch, k, v)
     dev = k.device
-    shape, named = _cache_operands(k_cache, v_cache, k_scale, v_scale)
+    shape, named = _cache_operands(torch, k_cache, v_cache, k_scale, v_scale)
     pages, ch, page_size, cd = shape
     if (ch, cd) != (hkv, d):
         raise ValueError(f"the caches have {ch} heads of {cd}, k has {hkv} of {d}")
@@ -586,11 +589,11 @@ def kv_cache_write(k, v, slots, k_cache, v_cache, stream=None, k_scale=None, v_s
     _check_gpu(dev)
     if k_scale is None:
         _launch(dev, stream, lib().kv_cache_write, k.data_ptr(), v.data_ptr(),
-                *_row_strides(k, v), slots.data_ptr(), total, k_cache.data_ptr(),
+                *strides, slots.data_ptr(), total, k_cache.data_ptr(),
                 v_cache.data_ptr(), pages, hkv, page_size, d)
     else:
         _launch(dev, stream, lib().kv_cache_write_q8, k.data_ptr(), v.data_ptr(),
-                *_row_strides(k, v), slots.data_ptr(), total, k_cache.data_ptr(),
+                *strides, slots.data_ptr(), total, k_cache.data_ptr(),
                 k_scale.data_ptr(), v_cache.data_ptr(), v_scale.data_ptr(), pages, hkv, page_size,
                 d)
 
@@ -607,10 +610,9 @@ def kv_cache_read(k_cache, v_cache, block_table, cu, k, v, starts=None, stream=N
     rows that no page of the cache holds are NaN.
     """
     import torch
-    _check_rows(k, v)
-    total, hkv, d = k.shape
+    (total, hkv, d), strides = _rows(torch, k, v)
     dev = k.device
-    shape, named = _cache_operands(k_cache, v_cache, k_scale, v_scale)
+    shape, named = _cache_operands(torch, k_cache, v_cache, k_scale, v_scale)
     pages, ch, page_size, cd = shape
     if (ch, cd) != (hkv, d):
         raise ValueError(f"the caches have {ch} heads of {cd}, k has {hkv} of {d}")
@@ -625,7 +627,7 @@ def kv_cache_read(k_cache, v_cache, block_table, cu, k, v, starts=None, stream=N
     _check_table(block_table, b)
     _check_gpu(dev)
     rest = (block_table.data_ptr(), b, block_table.shape[1], cu.data_ptr(), _addr(starts),
-            k.data_ptr(), v.data_ptr(), *_row_strides(k, v), total, pages, hkv, page_size, d)
+            k.data_ptr(), v.data_ptr(), *strides, total, pages, hkv, page_size, d)
     if k_scale is None:
         _launch(dev, stream, lib().kv_cache_read, k_cache.data_ptr(), v_cache.data_ptr(), *rest)
     else:
@@ -666,7 +668,7 @@ def paged_attn_fwd(q, k_cache, v_cache, o, lse, kv_lens, cu_q, block_table, pref
     if not isinstance(o, torch.Tensor):
         raise ValueError("o must be a torch tensor")
     out = _out_dtype(o)
-    shape, caches = _cache_operands(k_cache, v_cache, k_scale, v_scale)
+    shape, caches = _cache_operands(torch, k_cache, v_cache, k_scale, v_scale)
     pages, hkv, page_size, cd = shape
     if cd != d:
         raise ValueError(f"the caches have head_dim {cd}, q {d}")
