@@ -16,6 +16,10 @@
 // together attend to the prefix's keys: each K/V tile is read once for up to
 // 128 rows instead of once a request; the join adds its partials to those of a
 // row's own keys.
+//
+// Both passes have a form for bf16 caches and forms for 8-bit ones (Q8): the latter
+// convert K and V to bf16 where they are used, in registers for up to 32 rows, on
+// their way into LDS for more, and multiply as the former do.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -76,7 +80,9 @@ struct PagedArgs {
 //     request with query offsets and 8 without: fewer share a CU from some 700
 //     requests with offsets on at d = 128, from 280 (700 without) at d = 64.
 //   RB = 4: four waves of 32 rows each over the same 64-key tiles, in two stages.
-//   RB = 0 (8-bit caches): as RB = 1, up to 16 rows.
+//   RB = 0 (8-bit caches): as RB = 1, up to 16 rows.  The 8-bit forms of both take
+//     64-key tiles (68 KB of stages, 34 KB at d = 64) and stream them through all row
+//     tiles of a share.
 //   RB = 8 (8-bit caches): as RB = 4 with two groups of four waves, one wave of each on
 //     a SIMD, in turns: the matrix products of one beside the softmax of the other.
 template <int D, int RB, bool Q8>
@@ -97,7 +103,8 @@ struct PagedShape {
     static constexpr int Q_BYTES = TILES8 ? ROWS * 2 * D : 0;  // the next piece's query rows
     static constexpr int LDS_BYTES = KS * BUFFER_BYTES + Q_BYTES;
     // What a row tile costs a share beside its steps, in steps (8-bit tiles): us of
-    // 96 requests of 150 to 15000 keys (32 heads over 8, d = 128) none 179, one 145, two 146, three 151
+    // 96 requests of 150 to 15000 keys (32 heads over 8, d = 128) with one 145, with
+    // two 146, three 151; without, 179 where two took 156.
     static constexpr int CHARGE = TILES8 ? 1 : 0;
     // Least steps of a share: one of a 128-row tile leaves partials of twice
     // its K and V tiles' bytes.  us with 1, 4 and 8 steps (32 heads over 8, d =

@@ -303,6 +303,22 @@ def test_read_past_32_bits():
     assert torch.equal(k, want[[4, 0, 1, 3]]) and torch.equal(v, -want[[4, 0, 1, 3]])
 
 
+def test_read_of_more_rows_than_workgroups():
+    """2^26 rows and more: workgroups take several blocks of rows."""
+    n, page = (1 << 26) + 37, 256
+    kc, vc, scales, hk, hv = _cache(8, 1, page, 64, True, 11)
+    table = torch.randint(0, 8, (1, -(-n // page)), dtype=torch.int32, device="cuda")
+    k = torch.zeros(n + 2, 1, 64, dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    B.kv_cache_read(kc, vc, table, _ints([0, n]), k, v, **scales)
+    for first in (0, 1 << 25, (1 << 26) - 70000, n - 70000):
+        row = torch.arange(first, first + 70000, device="cuda")
+        at = table[0, row // page].long()
+        assert torch.equal(k[row], hk[at, :, row % page])
+        assert torch.equal(v[row], hv[at, :, row % page])
+    assert not bool(k[n:].any()) and not bool(v[n:].any())
+
+
 def test_write_and_read_on_another_stream_and_captured():
     """Both calls captured in one graph, replayed with other rows and offsets
     between eager work; and on a stream of their own."""
