@@ -111,7 +111,11 @@ struct PagedShape {
     // 128): the last 64 tokens of 2000 27, 25, 29, of four times 1000 29, 25, 28,
     // 128 single tokens behind a prefix of 2048 47, 43, 44, the last 100 tokens of
     // 500 17, 24, 29; from 3000 keys on the same.
-    static constexpr int LEAST = RB >= 4 ? 4 : 1;
+    // The 8-bit forms gain by any cut where there is little work: five requests of 4
+    // to 14 tokens, 29 to 6462 keys behind a prefix of 76 (16 heads over 2, d = 128,
+    // capped) with 4, 2 and 1 47, 37, 35, 100 tokens of 3000 (8 over 1) 37, 34, 31, the
+    // 160 single tokens behind 10007 keys 88 with each.
+    static constexpr int LEAST = RB >= 4 && !Q8 ? 4 : 1;
     static constexpr int WGS_PER_CU = RB == 8 ? 1 : RB <= 1 && D == 64 ? 4 : 2;
     static constexpr int WAVES_PER_SIMD = (WGS_PER_CU * THREADS / 64 + 3) / 4;
 };
@@ -1926,8 +1930,9 @@ ta_status paged_attn(const char *fn, bool q8, const void *q, const void *k_cache
                                        : PagedShape<128, 1, false>::STEP;
         j.pre_steps = (prefix_len + step - 1) / step;
         j.pre_share =
-            (int32_t)std::max<int64_t>(p.pre_rb == 4 ? PagedShape<128, 4, false>::LEAST
-                                                     : PagedShape<128, 1, false>::LEAST,
+            (int32_t)std::max<int64_t>(p.pre_rb != 4 ? PagedShape<128, 1, false>::LEAST
+                                       : q8          ? PagedShape<128, 4, true>::LEAST
+                                                     : PagedShape<128, 4, false>::LEAST,
                                        (pre_tiles * j.pre_steps + p.pre_slots - 1) / p.pre_slots);
         j.slopes = slopes;
         j.total_tokens = (int32_t)total_tokens;
