@@ -498,8 +498,14 @@ ta_status paged_attn_fwd(const void *q, const void *k_cache,
  * The same over an 8-bit cache (kv_cache_write_q8): each held value takes part
  * as what it stands for, element times scale, and everything else is as for
  * paged_attn_fwd, the workspace apart: at least ta_paged_q8_workspace_bytes()
- * bytes.  Probabilities are rounded to bf16 there too, each times the scale of
- * its value (which rounds nothing); the sums of a softmax take them before.  A
+ * bytes.  Probabilities are rounded to bf16 there too, where requests have few
+ * query rows each times the scale of its value: a power of two, which rounds
+ * nothing, but weights below 2^-125 may be lost.  The sums of a softmax take
+ * them before.  All this holds for scale bytes of 27 to 247, those that the
+ * write makes, and 255.  Other bytes are taken as what they say, but where a
+ * value or such a weight leaves bf16's range, infinite or lost.
+ * On a cache of either form, values past 2^92 may make sums of a row infinite:
+ * their weights, before the last division, go up to 2^8 each.  A
  * call that mixes single tokens and long pieces takes up to 1.4 times as long as
  * two calls of their own.
  */

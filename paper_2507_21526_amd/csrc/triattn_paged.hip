@@ -670,13 +670,13 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
             auto tile = [&](int key0, unsigned char *kt, auto careful, auto &&between)
                             TA_INLINE {
                 constexpr bool CAREFUL = decltype(careful)::value;
-                // V's scales as fp32, 0 for a key that no row keeps
+                // V's scales as fp32 in kWeightUnit, 0 for a key that no row keeps
                 static_assert(S::TK == 64, "a key a lane");
                 unsigned char *raw = kt + 2 * S::TILE_BYTES;
                 const uint32_t byte = raw[S::TK + lane];
                 const bool on = key0 + lane < rt.limit;
                 float *vscale = reinterpret_cast<float *>(raw + 256);
-                vscale[lane] = on ? q8_scale(byte) : 0.f;
+                vscale[lane] = on ? kWeightUnit * q8_scale(byte) : 0.f;
                 typename decltype(rb)::Scores s;
                 typename decltype(rb)::Probs p;
                 rb.products8(kt, raw, s);
@@ -779,7 +779,7 @@ __global__ __launch_bounds__((PagedShape<D, RB, Q8>::THREADS),
             // NaN from the first page that is none on (earlier rows of the tile do
             // not keep its keys)
             const float nan = last >= bad_key ? __builtin_nanf("") : 0.f;
-            const float inv = (den == 0.f ? 0.f : 1.f / den) + nan;
+            const float inv = (den == 0.f ? 0.f : (1.f / kWeightUnit) / den) + nan;
             const bool to_o = cur.slot < 0 && !a.row_o;
             const int64_t orow = (int64_t)(rt.q0 + tq) * a.hq + head;
             const int64_t srow = ((int64_t)cur.slot * a.hkv + g) * S::ROWS + rb.col;

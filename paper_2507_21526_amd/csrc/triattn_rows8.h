@@ -21,6 +21,11 @@ typedef __bf16 bf16x2q __attribute__((ext_vector_type(2)));
 // Scales 2^e that are written: e in kLeastExp .. kMostExp.
 constexpr int kLeastExp = -100, kMostExp = 120;
 
+// What a weight is held in: a probability, 2^8 at most (kRowsRebase), times its value's
+// scale, 2^120 at most, would be infinite as 2^128; the rows' last factor takes the half
+// back.  A weight of 2^-25 of the row's largest is still normal under a scale of 2^-100.
+constexpr float kWeightUnit = 0.5f;
+
 // The fp32 number whose exponent field is a scale's byte, as the conversions take
 // a scale (they read 0 as 2^-127 and 255 as NaN).
 __device__ __forceinline__ float q8_scale_bits(uint32_t byte)
@@ -187,7 +192,8 @@ struct RowBlock8 : RowBlock<D, NKB, SCORE> {
             }
     }
 
-    // softmax() whose weights carry the values' scales (fp32, one a key of the tile).
+    // softmax() whose weights carry the values' scales (fp32 in kWeightUnit, one a key of
+    // the tile).
     __device__ __forceinline__ void softmax8(const Scores &s, const ScoreArgs &a, float slope_log2,
                                              int dist0, Probs &p, bool fresh, const float *scales)
     {
