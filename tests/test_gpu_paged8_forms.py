@@ -1,11 +1,13 @@
 """GPU tests of attention over the 8-bit paged cache: what each of its forms (row
 tiles of 16, 32, 128 and 256 rows) has to keep alike."""
+import math
+
 import pytest
 import torch
 
 from tests.cache8_ref import Cache8
-from tests.serving_ref import check
-from tests.test_gpu_paged8 import _call
+from tests.serving_ref import check, geometric_slopes
+from tests.test_gpu_paged8 import _call, _q
 
 pytestmark = pytest.mark.gpu
 
@@ -45,3 +47,73 @@ def test_the_largest_scale_under_the_largest_weight(d, ql, byte):
     c.k, c.v = c.k[:, some], c.v[:, some]
     check(o[:, some], l[:, some], c.reference(q[:, some], [ql] * batch, d ** -0.5), torch.float32,
           f"byte {byte} d {d} rows {ql}")
+
+
+@pytest.mark.parametrize("d,lens,ql,hq,hkv", [
+    (64, [100, 0, 70], [300, 200, 70], 4, 2),    # 128 rows
+    (128, [20, 0, 33], [50, 30, 33], 4, 2),      # 128 rows
+    (128, [100, 0, 70], [300, 200, 70], 4, 2),   # 256 rows
+    (128, [700, 130, 1], [900, 129, 400], 7, 1)])
+@pytest.mark.parametrize("prefix", [0, 77])
+@pytest.mark.parametrize("score", ["plain", "cap", "slopes", "both"])
+def test_rows_before_the_first_key_in_large_tiles(d, lens, ql, hq, hkv, prefix, score):
+    """More query rows than keys: rows without any, and whole row tiles of them."""
+    c = Cache8(lens, hkv, d, 16, prefix, seed=42)
+    q = _q(sum(ql), hq, d, 42)
+    cap = 20.0 if score in ("cap", "both") else None
+    sl = geometric_slopes(hq) if score in ("slopes", "both") else None
+    o, l = _call(c, q, ql, torch.float32, cap, sl, ragged=True)
+    check(o, l, c.reference(q, ql, d ** -0.5, cap, sl), torch.float32, f"{d} {ql} {score}")
+    none = max(0, ql[0] - lens[0])
+    assert bool((o[:none] == 0).all()) and bool((l[:none] == -math.inf).all())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("ql", [1, 4, 40, 150])  # 16, 32, 128 and (d = 128) 256 rows
+@pytest.mark.parametrize("prefix", [0, 50])
+def test_bad_pages_and_lengths_in_every_form(d, ql, prefix):
+    """A page id outside the cache and a length past the table give NaN in the
+    rows that need them, bit for bit nothing in the others; an entry behind
+    the last key is not read."""
+    lens = [200, 190, 180]
+    c = Cache8(lens, 2, d, 16, prefix, seed=43)
+    q = _q(3 * ql, 4, d, 43)
+    good, gl = _call(c, q, [ql] * 3, torch.float32, ragged=ql > 1)
+    check(good, gl, c.reference(q, [ql] * 3, d ** -0.5), torch.float32, f"{d} {ql} {prefix}")
+    rows = [torch.arange(b * ql, (b + 1) * ql, device="cuda") for b in range(3)]
+    table, kv = c.table.clone(), c.kv_lens.clone()
+
+    def others_stand(b):
+        rest = torch.cat([rows[i] for i in range(3) if i != b])
+        assert torch.equal(o[rest], good[rest]) and torch.equal(l[rest], gl[rest])
+
+    for page in (-1, c.k.shape[0], 2 ** 31 - 1, -2 ** 31):
+        c.table[1, 3] = page  # keys 48 .. 63
+        o, l = _call(c, q, [ql] * 3, torch.float32, ragged=ql > 1)
+        needs = torch.arange(190 - ql, 190, device="cuda") >= 48
+        assert bool(o[rows[1][needs]].isnan().all()) and bool(l[rows[1][needs]].isnan().all())
+        early = rows[1][~needs]
+        assert torch.equal(o[early], good[early]) and torch.equal(l[early], gl[early])
+        others_stand(1)
+        c.table.copy_(table)
+    c.table[1, 12] = -5
+    o, l = _call(c, q, [ql] * 3, torch.float32, ragged=ql > 1)
+    assert torch.equal(o, good) and torch.equal(l, gl)
+    c.table.copy_(table)
+    for n in (c.table.shape[1] * 16 + 1, 2 ** 31 - 1):
+        c.kv_lens[2] = n
+        o, l = _call(c, q, [ql] * 3, torch.float32, ragged=ql > 1)
+        assert bool(o[rows[2]].isnan().all()) and bool(l[rows[2]].isnan().all())
+        others_stand(2)
+        c.kv_lens.copy_(kv)
+    c.kv_lens[2] = -4  # no keys
+    o, l = _call(c, q, [ql] * 3, torch.float32, ragged=ql > 1)
+    assert bool((o[rows[2]] == 0).all()) and bool((l[rows[2]] == -math.inf).all())
+    others_stand(2)
+    c.kv_lens.copy_(kv)
+    if prefix:
+        keep = c.prefix_pages.clone()
+        c.prefix_pages[2] = c.k.shape[0]
+        o, l = _call(c, q, [ql] * 3, torch.float32, ragged=ql > 1)
+        assert bool(o.isnan().all()) and bool(l.isnan().all())
+        c.prefix_pages.copy_(keep)
