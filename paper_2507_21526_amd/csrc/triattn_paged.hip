@@ -77,12 +77,14 @@ struct PagedArgs {
 //     piece.  64 KB of stages at d = 128 (32 KB at d = 64) let two workgroups
 //     (four) share a CU, so that one loads while the other finds its next request
 //     or joins its waves.  The tables of lengths come on top, 16 to 20 bytes a
-//     request with query offsets and 8 without: fewer share a CU from some 700
-//     requests with offsets on at d = 128, from 280 (700 without) at d = 64.
+//     request with query offsets and 8 without: fewer bf16 workgroups share a CU from
+//     some 700 requests with offsets on at d = 128, from 280 (700 without) at d = 64.
 //   RB = 4: four waves of 32 rows each over the same 64-key tiles, in two stages.
 //   RB = 0 (8-bit caches): as RB = 1, up to 16 rows.  The 8-bit forms of both take
 //     64-key tiles (68 KB of stages, 34 KB at d = 64) and stream them through all row
-//     tiles of a share.
+//     tiles of a share.  With the query rows that leaves less for the tables: fewer
+//     share a CU from some 310 requests of four rows (group 4) on at d = 128, from 85
+//     (single tokens without offsets: 443) at d = 64, and there are fewer shares then.
 //   RB = 8 (8-bit caches): as RB = 4 with two groups of four waves, one wave of each on
 //     a SIMD, in turns: the matrix products of one beside the softmax of the other.
 template <int D, int RB, bool Q8>
@@ -118,6 +120,10 @@ struct PagedShape {
     static constexpr int LEAST = RB >= 4 && !Q8 ? 4 : 1;
     static constexpr int WGS_PER_CU = RB == 8 ? 1 : RB <= 1 && D == 64 ? 4 : 2;
     static constexpr int WAVES_PER_SIMD = (WGS_PER_CU * THREADS / 64 + 3) / 4;
+    // LDS of a workgroup beside the tables: stages and query rows, page ids, what the
+    // waves of a piece and of the scan leave, the two flags
+    static constexpr int FIXED_LDS = LDS_BYTES + 4 * (TILES8 ? 1 : kPageEntries) +
+                                     KS * (12 + 256) + THREADS / 16 + 8;
 };
 
 // Exclusive scan of val(i), i < n, into out[0 .. n] (out[n]: the total) by
@@ -1606,16 +1612,40 @@ struct PagedLayout {
         pre_row_o, pre_row_lse, bytes;
 };
 
+// Workgroups that share a CU, each with so many bytes of tables.  8-bit: as many as
+// fit its LDS; of more shares, all of one length, the rest would start when the others
+// end.  us with as many shares as without tables and with as many as fit (32 heads over
+// 8): at d = 64 100 requests of four tokens and 2000 keys 85 and 62, of 200 keys 25 and
+// 28, 400 of 200 keys 81 and 59, 480 single tokens of 2000 keys 270 and 200; at d = 128
+// 340 of four tokens and 1500 keys 415 and 399, where one workgroup is too few for a CU
+// (300, of which two fit, take 200).
+template <typename S>
+int wgs_of(bool q8, int64_t tables)
+{
+    constexpr int64_t kLds = 160 * 1024, kGranule = 1280;  // of a CU, and of an allocation
+    const int64_t each = (S::FIXED_LDS + tables + kGranule - 1) / kGranule * kGranule;
+    return q8 ? (int)std::max<int64_t>(1, std::min<int64_t>(S::WGS_PER_CU, kLds / each))
+              : S::WGS_PER_CU;
+}
 template <bool Q8>
-int wgs_per_cu(int rb, int d)
+int wgs_per_cu(int rb, int d, int64_t tables)
 {
     if (Q8 && rb == 8)
-        return PagedShape<128, 8, true>::WGS_PER_CU;
+        return wgs_of<PagedShape<128, 8, true>>(Q8, tables);
     if (Q8 && rb == 0)
-        return d == 128 ? PagedShape<128, 0, true>::WGS_PER_CU : PagedShape<64, 0, true>::WGS_PER_CU;
+        return d == 128 ? wgs_of<PagedShape<128, 0, true>>(Q8, tables)
+                        : wgs_of<PagedShape<64, 0, true>>(Q8, tables);
     if (d == 128)
-        return rb == 4 ? PagedShape<128, 4, Q8>::WGS_PER_CU : PagedShape<128, 1, Q8>::WGS_PER_CU;
-    return rb == 4 ? PagedShape<64, 4, Q8>::WGS_PER_CU : PagedShape<64, 1, Q8>::WGS_PER_CU;
+        return rb == 4 ? wgs_of<PagedShape<128, 4, Q8>>(Q8, tables)
+                       : wgs_of<PagedShape<128, 1, Q8>>(Q8, tables);
+    return rb == 4 ? wgs_of<PagedShape<64, 4, Q8>>(Q8, tables)
+                   : wgs_of<PagedShape<64, 1, Q8>>(Q8, tables);
+}
+
+// LDS of the own-keys pass's tables.
+int64_t table_bytes(int64_t max_tiles, int64_t batch, bool ragged)
+{
+    return 4 * (max_tiles + 1 + batch + (ragged ? 2 * (batch + 1) : 0));
 }
 
 // Rows of a tile.
@@ -1624,7 +1654,9 @@ int form_rows(int rb) { return rb == 0 ? 16 : 32 * rb; }
 PagedLayout paged_layout(int32_t batch, int64_t total_tokens, bool ragged, bool prefix, int32_t hq,
                          int32_t hkv, int32_t d, bool q8)
 {
-    auto per_cu = [&](int rb) { return q8 ? wgs_per_cu<true>(rb, d) : wgs_per_cu<false>(rb, d); };
+    auto per_cu = [&](int rb, int64_t tables) {
+        return q8 ? wgs_per_cu<true>(rb, d, tables) : wgs_per_cu<false>(rb, d, tables);
+    };
     PagedLayout p{};
     const int64_t group = hq / hkv;
     // Up to 32 rows a request on average: tiles of 32 rows, which a
@@ -1652,11 +1684,11 @@ PagedLayout paged_layout(int32_t batch, int64_t total_tokens, bool ragged, bool 
         if (total_tokens * group <= 16)
             p.pre_rb = 0;
     }
-    p.own_slots = std::max(1, kCus * per_cu(p.own_rb) / hkv);
-    p.pre_slots = std::max(1, kCus * per_cu(p.pre_rb) / hkv);
     const int64_t rows = form_rows(p.own_rb);
     p.max_tiles = (int)std::min<int64_t>(
         kMaxTiles + 1, ragged ? total_tokens * group / rows + batch : (int64_t)batch);
+    p.own_slots = std::max(1, kCus * per_cu(p.own_rb, table_bytes(p.max_tiles, batch, ragged)) / hkv);
+    p.pre_slots = std::max(1, kCus * per_cu(p.pre_rb, 0) / hkv);
     size_t at = 0;
     auto take = [&](size_t n) {
         const size_t here = at;
@@ -1684,18 +1716,11 @@ PagedLayout paged_layout(int32_t batch, int64_t total_tokens, bool ragged, bool 
     return p;
 }
 
-// LDS of the own-keys pass's tables.
-uint32_t table_bytes(const PagedArgs &a)
-{
-    return 4u * (uint32_t)(a.max_tiles + 1 + a.batch +
-                           (a.cu_q ? 2 * (a.batch + 1) : 0));
-}
-
 template <int D, int RB, bool PREFIX, bool Q8>
 void launch_scores(int score, dim3 grid, hipStream_t s, const PagedArgs &a)
 {
     const dim3 threads(PagedShape<D, RB, Q8>::THREADS);
-    const uint32_t lds = PREFIX ? 0 : table_bytes(a);
+    const uint32_t lds = PREFIX ? 0 : (uint32_t)table_bytes(a.max_tiles, a.batch, a.cu_q);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, threads, lds, s, a); };
     switch (score) {
     case 0: launch(paged_attn_kernel<D, RB, 0, PREFIX, Q8>); break;

@@ -117,3 +117,19 @@ def test_bad_pages_and_lengths_in_every_form(d, ql, prefix):
         o, l = _call(c, q, [ql] * 3, torch.float32, ragged=ql > 1)
         assert bool(o.isnan().all()) and bool(l.isnan().all())
         c.prefix_pages.copy_(keep)
+
+
+@pytest.mark.parametrize("d,batch,ql,hq,hkv", [
+    (64, 100, 4, 8, 2), (64, 480, 1, 8, 2), (64, 1024, 3, 2, 2), (128, 340, 4, 8, 2)])
+@pytest.mark.parametrize("prefix", [0, 33])
+def test_batches_whose_tables_take_workgroups_off_a_cu(d, batch, ql, hq, hkv, prefix):
+    lens = [ql + (11 * i) % 300 for i in range(batch)]
+    c = Cache8(lens, hkv, d, 64, prefix, seed=44)
+    q = _q(batch * ql, hq, d, 44)
+    o, l = _call(c, q, [ql] * batch, torch.float32, ragged=ql > 1)
+    some = list(range(0, batch, 29)) + [batch - 1]
+    at = torch.cat([torch.arange(i * ql, (i + 1) * ql) for i in some]).cuda()
+    c.lens, c.table = [lens[i] for i in some], c.table[some]
+    check(o[at], l[at], c.reference(q[at], [ql] * len(some), d ** -0.5), torch.float32,
+          f"{d} {batch} {ql} {prefix}")
+    assert bool(torch.isfinite(o).all())
