@@ -83,8 +83,8 @@ struct PagedArgs {
 //   RB = 0 (8-bit caches): as RB = 1, up to 16 rows.  The 8-bit forms of both take
 //     64-key tiles (68 KB of stages, 34 KB at d = 64) and stream them through all row
 //     tiles of a share.  With the query rows that leaves less for the tables: fewer
-//     share a CU from some 310 requests of four rows (group 4) on at d = 128, from 85
-//     (single tokens without offsets: 443) at d = 64, and there are fewer shares then.
+//     share a CU from some 310 requests of four tokens (group 4) on at d = 128, from 85
+//     (single tokens without offsets: 443) at d = 64.
 //   RB = 8 (8-bit caches): as RB = 4 with two groups of four waves, one wave of each on
 //     a SIMD, in turns: the matrix products of one beside the softmax of the other.
 template <int D, int RB, bool Q8>
@@ -1612,34 +1612,35 @@ struct PagedLayout {
         pre_row_o, pre_row_lse, bytes;
 };
 
-// Workgroups that share a CU, each with so many bytes of tables.  8-bit: as many as
-// fit its LDS; of more shares, all of one length, the rest would start when the others
-// end.  us with as many shares as without tables and with as many as fit (32 heads over
-// 8): at d = 64 100 requests of four tokens and 2000 keys 85 and 62, of 200 keys 25 and
-// 28, 400 of 200 keys 81 and 59, 480 single tokens of 2000 keys 270 and 200; at d = 128
-// 340 of four tokens and 1500 keys 415 and 399, where one workgroup is too few for a CU
-// (300, of which two fit, take 200).
+// Shares a CU, each with so many bytes of tables.  8-bit: as many as share it, or
+// a whole number of times as many as its LDS holds at once: of more, all of one length,
+// the rest would start when the others end.  us with four a CU and with the three that
+// fit (32 heads over 8, d = 64): 100 requests of four tokens and 2000 keys 85 and 62, of
+// 200 keys 25 and 28, 400 of 200 keys 81 and 59, 480 single tokens of 2000 keys 270 and
+// 200.  At d = 128 two shares a CU stay where one workgroup fits, one after the other
+// (which evens out calls that mix pieces and single tokens: 1023 of these beside 3070
+// tokens behind 30000 keys, 32 heads over 4, 8.1 ms, with one share a CU 9.3).
 template <typename S>
-int wgs_of(bool q8, int64_t tables)
+int shares_of(bool q8, int64_t tables)
 {
     constexpr int64_t kLds = 160 * 1024, kGranule = 1280;  // of a CU, and of an allocation
     const int64_t each = (S::FIXED_LDS + tables + kGranule - 1) / kGranule * kGranule;
-    return q8 ? (int)std::max<int64_t>(1, std::min<int64_t>(S::WGS_PER_CU, kLds / each))
-              : S::WGS_PER_CU;
+    const int fit = (int)std::max<int64_t>(1, std::min<int64_t>(S::WGS_PER_CU, kLds / each));
+    return q8 ? S::WGS_PER_CU / fit * fit : S::WGS_PER_CU;
 }
 template <bool Q8>
-int wgs_per_cu(int rb, int d, int64_t tables)
+int shares_per_cu(int rb, int d, int64_t tables)
 {
     if (Q8 && rb == 8)
-        return wgs_of<PagedShape<128, 8, true>>(Q8, tables);
+        return shares_of<PagedShape<128, 8, true>>(Q8, tables);
     if (Q8 && rb == 0)
-        return d == 128 ? wgs_of<PagedShape<128, 0, true>>(Q8, tables)
-                        : wgs_of<PagedShape<64, 0, true>>(Q8, tables);
+        return d == 128 ? shares_of<PagedShape<128, 0, true>>(Q8, tables)
+                        : shares_of<PagedShape<64, 0, true>>(Q8, tables);
     if (d == 128)
-        return rb == 4 ? wgs_of<PagedShape<128, 4, Q8>>(Q8, tables)
-                       : wgs_of<PagedShape<128, 1, Q8>>(Q8, tables);
-    return rb == 4 ? wgs_of<PagedShape<64, 4, Q8>>(Q8, tables)
-                   : wgs_of<PagedShape<64, 1, Q8>>(Q8, tables);
+        return rb == 4 ? shares_of<PagedShape<128, 4, Q8>>(Q8, tables)
+                       : shares_of<PagedShape<128, 1, Q8>>(Q8, tables);
+    return rb == 4 ? shares_of<PagedShape<64, 4, Q8>>(Q8, tables)
+                   : shares_of<PagedShape<64, 1, Q8>>(Q8, tables);
 }
 
 // LDS of the own-keys pass's tables.
@@ -1655,7 +1656,7 @@ PagedLayout paged_layout(int32_t batch, int64_t total_tokens, bool ragged, bool 
                          int32_t hkv, int32_t d, bool q8)
 {
     auto per_cu = [&](int rb, int64_t tables) {
-        return q8 ? wgs_per_cu<true>(rb, d, tables) : wgs_per_cu<false>(rb, d, tables);
+        return q8 ? shares_per_cu<true>(rb, d, tables) : shares_per_cu<false>(rb, d, tables);
     };
     PagedLayout p{};
     const int64_t group = hq / hkv;
@@ -1687,7 +1688,8 @@ PagedLayout paged_layout(int32_t batch, int64_t total_tokens, bool ragged, bool 
     const int64_t rows = form_rows(p.own_rb);
     p.max_tiles = (int)std::min<int64_t>(
         kMaxTiles + 1, ragged ? total_tokens * group / rows + batch : (int64_t)batch);
-    p.own_slots = std::max(1, kCus * per_cu(p.own_rb, table_bytes(p.max_tiles, batch, ragged)) / hkv);
+    const int64_t tables = table_bytes(p.max_tiles, batch, ragged);
+    p.own_slots = std::max(1, kCus * per_cu(p.own_rb, tables) / hkv);
     p.pre_slots = std::max(1, kCus * per_cu(p.pre_rb, 0) / hkv);
     size_t at = 0;
     auto take = [&](size_t n) {

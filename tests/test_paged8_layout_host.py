@@ -1,6 +1,6 @@
 """Host tests of how 8-bit paged attention cuts its work: as many shares as
-workgroups fit the chip with their tables of lengths, so that none starts only
-after another has ended."""
+workgroups fit the chip with their tables of lengths, or a whole number of times
+as many, so that it is never some of them that start when the others end."""
 import pytest
 
 from paper_2507_21526_amd import binding as B
@@ -8,8 +8,8 @@ from paper_2507_21526_amd import binding as B
 CUS, LDS, GRANULE = 256, 160 * 1024, 1280
 
 
-def workgroups_of_a_cu(batch, tokens, ragged, hq, hkv, d, rows):
-    """Counted on by the layout: a workgroup a share, two pieces of `rows` rows a
+def shares_of_a_cu(batch, tokens, ragged, hq, hkv, d, rows):
+    """Of the layout: two pieces of `rows` rows a
     share and kv head in the workspace (d values and a log-sum-exp each), beside
     32 bytes a row tile."""
     size = B.ta_paged_q8_workspace_bytes(batch, tokens, ragged, False, hq, hkv, d)
@@ -33,11 +33,12 @@ def fit(batch, tokens, ragged, hq, hkv, d, rows):
     (64, 80, 4, 32, 8, 4), (64, 100, 4, 32, 8, 3), (64, 300, 4, 32, 8, 3), (64, 1024, 3, 8, 8, 2),
     (64, 440, 1, 32, 8, 4), (64, 480, 1, 32, 8, 3), (64, 1024, 1, 32, 8, 3),
     (128, 1024, 1, 32, 8, 2), (128, 1, 1, 32, 8, 2), (64, 1, 1, 8, 1, 4)])
-def test_shares_are_the_workgroups_that_fit(d, batch, tokens, hq, hkv, want):
+def test_shares_come_in_whole_rounds(d, batch, tokens, hq, hkv, want):
     ragged = tokens > 1
     case = (batch, batch * tokens, ragged, hq, hkv, d, 32 if ragged else 16)
     assert fit(*case) == want
-    assert workgroups_of_a_cu(*case) == want
+    most = 2 if d == 128 else 4
+    assert shares_of_a_cu(*case) == most // want * want
 
 
 def test_bf16_shares_stand():
