@@ -411,7 +411,10 @@ ta_status kv_cache_write_q8(const void *k, const void *v, int64_t k_token_stride
 /*
  * Cached rows back as bf16, from a cache of either form: rows cu[b] .. cu[b + 1)
  * of k and v get positions starts[b], starts[b] + 1, .. of request b.  8-bit
- * rows come back exactly (values past bf16's range as infinities).
+ * rows come back exactly (under scale bytes that the write does not make, values
+ * past bf16's range as infinities, and those below its smallest number rounded).
+ * Positions are those of the block table: a shared prefix that it does not list is
+ * read by a call of its own.
  *   block_table  [batch, table_width] int32 device array.
  *   cu           [batch + 1] int32 device array; rows from cu[batch] on are
  *                left as they are.
@@ -471,9 +474,10 @@ ta_status kv_cache_read_q8(const void *k_cache, const void *k_scale,
  * cache in the rows that need it, a length past the block table in its
  * request's rows, and in every row a cu_q that does not start at 0, decreases
  * or passes total_tokens.  No access leaves the caller's buffers.
- * A call is laid out for the mean number of its requests' query rows: where
- * single tokens and long pieces share one, it takes up to 15 % longer than in
- * the layout that would suit them best.
+ * A call is laid out for the mean number of its requests' query rows.  Single
+ * tokens of up to 255 requests beside a long piece took 0.9 to 1.25 times as
+ * long as in two calls; a thousand beside 3070 tokens, whose mean hides the
+ * piece, 2.1 times, and 5.8 where the piece comes behind 30000 keys.
  * Unsupported: a table or a prefix (with slopes: both together) of more than
  * 2^31 - 257 keys, and more than 2048 row tiles a kv head, that is
  * total_tokens * (hq / hkv) / 128 + batch > 2048 where requests have more than 32
@@ -497,17 +501,21 @@ ta_status paged_attn_fwd(const void *q, const void *k_cache,
 /*
  * The same over an 8-bit cache (kv_cache_write_q8): each held value takes part
  * as what it stands for, element times scale, and everything else is as for
- * paged_attn_fwd, the workspace apart: at least ta_paged_q8_workspace_bytes()
- * bytes.  Probabilities are rounded to bf16 there too, where requests have few
- * query rows each times the scale of its value: a power of two, which rounds
- * nothing, but weights below 2^-125 may be lost.  The sums of a softmax take
- * them before.  All this holds for scale bytes of 27 to 247, those that the
- * write makes, and 255.  Other bytes are taken as what they say, but where a
- * value or such a weight leaves bf16's range, infinite or lost.
+ * paged_attn_fwd, but for the workspace (at least ta_paged_q8_workspace_bytes()
+ * bytes) and the limit of row tiles, which have 256 rows at head_dim 128 where
+ * requests have more than 128 query rows a kv head on average.
+ * Probabilities are rounded to bf16 there too, where requests have few query
+ * rows each times the scale of its value: a power of two, which rounds nothing,
+ * but weights below 2^-125 may be lost.  The sums of a softmax take them before.
+ * All this holds for scale bytes of 27 to 247, those that the write makes, and
+ * 255 (NaN).  Other bytes are taken as what they say, but a value or such a
+ * weight that leaves bf16's range becomes infinite or is lost.
  * On a cache of either form, values past 2^92 may make sums of a row infinite:
- * their weights, before the last division, go up to 2^8 each.  A
- * call that mixes single tokens and long pieces takes up to 1.4 times as long as
- * two calls of their own.
+ * their weights, before the last division, go up to 2^8 each.
+ * A call that mixes single tokens and a long piece is better given as two: up to
+ * 255 single tokens beside a piece took 1.1 to 1.9 times as long as the two calls,
+ * a thousand beside 3070 tokens (whose mean hides the piece) 2.5 times, and 6.4
+ * where the piece comes behind 30000 keys.
  */
 size_t ta_paged_q8_workspace_bytes(int32_t batch, int64_t total_tokens,
                                    int32_t ragged, int32_t prefix, int32_t hq,

@@ -1674,10 +1674,13 @@ PagedLayout paged_layout(int32_t batch, int64_t total_tokens, bool ragged, bool 
         // 8-bit: tiles of 16 rows for single tokens (us with 32 and with 16: 96
         // requests of 64, of 955, of 3820 keys 19.6, 57, 152 and 16.2, 52, 148; a
         // request of more rows would read its keys more than once), and at d = 128
-        // tiles of 256 for requests of more than 128 on average (us with 128 and with 256: five requests of 40 tokens, of
-        // 256, of 500 to 1800 79, 241, 744 and 74, 207, 620, the last with a cap 844
-        // and 767; d = 64: 411 and 401, with a cap 587 and 625; the prefix's pass of
-        // 160 tokens, whose tiles are few, takes 5 more).
+        // tiles of 256 for requests of more than 128 on average (us with 128 and with
+        // 256: five requests of 40 tokens, of 256, of 500 to 1800 79, 241, 744 and 74,
+        // 207, 620, the last with a cap 844 and 767; d = 64: 411 and 401, with a cap 587
+        // and 625; the prefix's pass of 160 tokens, whose tiles are few, takes 5 more).
+        // A call of unequal requests pays for the mean: 96 single tokens of 150 to 15000
+        // keys (285 us) and a prompt of 3200 (161) 855 in tiles of 256, 1023 of 200 keys
+        // (76) and 3070 tokens behind 30000 (1188; 32 heads over 4) 8078 in tiles of 32.
         if (!ragged || total_tokens <= batch)
             p.own_rb = 0;
         else if (d == 128 && total_tokens * group > (int64_t)batch * 128)
